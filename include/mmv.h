@@ -89,7 +89,9 @@ typedef enum {
     MMV_ERR_WORKSPACE_TOO_SMALL = 3,
     MMV_ERR_BAD_SEGMENTS = 4,        /* offsets not monotone / out of range (device-detected) */
     MMV_ERR_TIMEOUT = 5,             /* a bounded device-side wait gave up                    */
-    MMV_ERR_CUDA = 6                 /* a CUDA runtime / driver call failed                   */
+    MMV_ERR_CUDA = 6,                /* a CUDA runtime / driver call failed                   */
+    MMV_ERR_OUT_OF_BLOCKS = 7        /* mmv_block_tables: free list, table or slot map too
+                                        short (device-detected)                               */
 } mmv_status;
 
 typedef enum { MMV_F16_TO_F32 = 0, MMV_I8_TO_I32 = 1, MMV_BF16_TO_F32 = 2 } mmv_dtype;
@@ -358,6 +360,111 @@ size_t mmv_seg_scan_host_scratch_bytes(mmv_dtype dt, int64_t chunk_elems);
 mmv_status mmv_seg_scan_host(const void *x_host, const void *flags_host, int64_t n, mmv_dtype dt, void *out_host,
                              int64_t chunk_elems, void *device_scratch, size_t device_scratch_bytes,
                              void *cuda_stream);
+
+/* ---------------------------------------------------------------------------
+ * Serving a language model over a ragged batch
+ *
+ * One step of a server works on a PACKED batch: the new tokens of request 0,
+ * then those of request 1, and so on, with CSR offsets between them
+ * (MMV_SEG_OFFSETS_I32).  mmv_block_tables builds the offsets, the slot of every
+ * token and the new entries of the block tables from the requests' lengths;
+ * mmv_kv_append writes keys and values to those slots; mmv_paged_attention reads
+ * them back through the tables for one new token per request; and
+ * mmv_linear_attention(_step) are the layers that keep a decayed state in place
+ * of a cache, over the same offsets.
+ *
+ * Values are fp16 or bfloat16 (MMV_F16_TO_F32, MMV_BF16_TO_F32 where a dtype is
+ * asked for); results have the values' type and are rounded once, from fp32.
+ * Tensors of values are given with their strides in ELEMENTS; the last axis is
+ * contiguous, strides are multiples of 8 elements and pointers 16-byte aligned
+ * (dimensions are multiples of 8), so that every row is read in 16-byte words.
+ * Metadata pointers need the alignment of their type.  Unlike the calls above,
+ * these enqueue kernels only and can be captured in a CUDA graph like them.
+ * Calls on different streams may overlap; a workspace each, as above.
+ * ------------------------------------------------------------------------- */
+
+/*
+ * Block tables and slot maps from request lengths.  Request r holds past[r]
+ * tokens and adds added[r] (>= 0 both; int32).  Tokens live in blocks of
+ * block_size; request r's p-th token is in block table[r, p / block_size].  With
+ *     had_r  = ceil(past[r] / block_size)       blocks that r already has
+ *     need_r = ceil((past[r] + added[r]) / block_size)
+ *     base_r = sum of need - had over the requests in front of r
+ * the call writes
+ *     table[r, b]  = free_blocks[base_r + b - had_r]   for had_r <= b < need_r
+ *                    (the row's other entries are left alone)
+ *     offsets[r]   = sum of added in front of r, nreq + 1 values (int32)
+ *     total[r]     = past[r] + added[r]
+ *     slots[offsets[r] + i] = table[r, p / block_size] * block_size + p % block_size,
+ *                    p = past[r] + i, int64; -1 from offsets[nreq] to nslots
+ *     *used        = entries taken from the front of free_blocks
+ * table has max_blocks columns, rows table_stride entries apart.  free_blocks has nfree
+ * entries; one that is negative, like a negative entry of a row's held blocks,
+ * gives its tokens slot -1.  Nothing is read or written beyond the stated sizes:
+ * a token without a block (free list or row too short) gets slot -1, tokens past
+ * nslots are dropped, and the workspace records MMV_ERR_OUT_OF_BLOCKS; a negative
+ * length counts as 0, a total (of a request, or of added) beyond int32 is cut, and
+ * MMV_ERR_BAD_SEGMENTS is recorded.  All outputs are integers and deterministic.
+ * nreq < 2^20.  Workspace: mmv_block_tables_workspace_bytes(nreq), 256-byte aligned.
+ */
+size_t mmv_block_tables_workspace_bytes(int64_t nreq);
+mmv_status mmv_block_tables(const int32_t *past, const int32_t *added, int64_t nreq, int32_t block_size,
+                            const int32_t *free_blocks, int64_t nfree, int32_t *table, int64_t table_stride,
+                            int64_t max_blocks, int32_t *offsets, int32_t *total, int64_t *slots, int64_t nslots,
+                            int32_t *used, void *workspace, size_t workspace_bytes, void *cuda_stream);
+
+/*
+ * A paged key-value cache: element (block b, token i of it, head h, column c) of
+ * the keys is k[b * stride_block + i * stride_token + h * stride_head + c], and
+ * the same of the values v.  Any order of the three axes; dim is a multiple of 8
+ * up to 256.
+ */
+typedef struct {
+    void *k, *v;
+    int64_t num_blocks;
+    int64_t stride_block, stride_token, stride_head;
+    int32_t block_size, heads, dim, dtype;
+} mmv_kv_cache;
+
+/*
+ * Writes token t's key and value rows (heads x dim each) to slot slots[t] of the
+ * cache (block slots[t] / block_size, place slots[t] % block_size).  A slot that
+ * is negative or past the cache's end is skipped: nothing is written for it.  Two
+ * tokens with one slot leave either's values.  k, v: ntok tokens, token and head
+ * strides of their own (a view into a fused projection's output is fine); they
+ * must not overlap the cache.  No workspace.
+ */
+mmv_status mmv_kv_append(const void *k, int64_t k_stride_token, int64_t k_stride_head,
+                         const void *v, int64_t v_stride_token, int64_t v_stride_head,
+                         const int64_t *slots, int64_t ntok, const mmv_kv_cache *cache, void *cuda_stream);
+
+/*
+ * Inputs of linear attention: q [.., heads, dim_k], k [.., kv_heads, dim_k],
+ * v [.., kv_heads, dim_v] with a token (or request) in front, token and head
+ * strides of their own.  heads is a multiple of kv_heads: query head h uses key /
+ * value head h / (heads / kv_heads) and has a decay and a state of its own.
+ * dim_k and dim_v are multiples of 8 up to 128.
+ */
+typedef struct {
+    const void *q, *k, *v;
+    int64_t q_stride_token, q_stride_head, k_stride_token, k_stride_head, v_stride_token, v_stride_head;
+    int32_t heads, kv_heads, dim_k, dim_v, dtype;
+} mmv_linear_inputs;
+
+/*
+ * Linear attention of ONE token for each of nreq requests:
+ *     S'  = exp(log_decay[h]) S + k v^T         (fp32, dim_k x dim_v, row-major)
+ *     out = scale * q^T S'                      (nreq x heads x dim_v, the inputs' type)
+ * S is state[s], S' is written to state_out[s], with s = slots[r] (int32; slots NULL:
+ * s = r); both are [num_slots, heads, dim_k, dim_v] fp32, 16-byte aligned, and
+ * may be the same buffer (the state is then updated in place).  A request whose s
+ * is outside [0, num_slots) has no state: its out is zero and nothing is kept.
+ * Two requests must not share a state.  log_decay: heads fp32 values, any <= 0,
+ * -infinity included (the state is then this token's alone).  No workspace.
+ */
+mmv_status mmv_linear_attention_step(const mmv_linear_inputs *in, int64_t nreq, const float *log_decay, float scale,
+                                     const float *state, float *state_out, const int32_t *slots, int64_t num_slots,
+                                     void *out, void *cuda_stream);
 
 /*
  * Test hook.  wait_budget_ns: time after which a device-side wait gives up

@@ -9,6 +9,7 @@ the import of this module fails.
 from __future__ import annotations
 
 import ctypes
+import struct
 from pathlib import Path
 
 import torch
@@ -29,6 +30,7 @@ EXPORTS = (
     "mmv_seg_scan_host", "mmv_seg_scan_host_scratch_bytes", "mmv_seg_scan_exclusive", "mmv_compress",
     "mmv_seg_scan_minmax", "mmv_seg_scan_i8_i64", "mmv_seg_scan_shard", "mmv_seg_scan_shard_finish",
     "mmv_debug_force_scan_shape", "mmv_mult_i8",
+    "mmv_block_tables_workspace_bytes", "mmv_block_tables", "mmv_kv_append", "mmv_linear_attention_step",
 )
 SHARD_SUMMARY_BYTES = 16
 STATIC_SCAN_MAX_N = 1 << 28
@@ -85,6 +87,15 @@ def _load() -> ctypes.CDLL:
     lib.mmv_seg_scan_shard_finish.argtypes = [vp, ci, ci, vp, i64, ci, vp]
     lib.mmv_mult_i8.restype = ci
     lib.mmv_mult_i8.argtypes = [vp, vp, i64, vp, vp, sz, vp]
+    f32 = ctypes.c_float
+    lib.mmv_block_tables_workspace_bytes.restype = sz
+    lib.mmv_block_tables_workspace_bytes.argtypes = [i64]
+    lib.mmv_block_tables.restype = ci
+    lib.mmv_block_tables.argtypes = [vp, vp, i64, ci, vp, i64, vp, i64, i64, vp, vp, vp, i64, vp, vp, sz, vp]
+    lib.mmv_kv_append.restype = ci
+    lib.mmv_kv_append.argtypes = [vp, i64, i64, vp, i64, i64, vp, i64, vp, vp]
+    lib.mmv_linear_attention_step.restype = ci
+    lib.mmv_linear_attention_step.argtypes = [vp, i64, vp, f32, vp, vp, vp, i64, vp, vp]
     lib.mmv_debug_force_scan_shape.restype = None
     lib.mmv_debug_force_scan_shape.argtypes = [ci]
     lib.mmv_debug_force_sum_groups.restype = None
@@ -373,3 +384,166 @@ def spmv_csr(rowptr: torch.Tensor, col: torch.Tensor, val: torch.Tensor, x: torc
     if rc != MMV_OK:
         raise MmvError(rc, "mmv_spmv_csr")
     return y
+
+
+# ---------------------------------------------------------------------------
+# Serving a language model over a ragged batch
+# ---------------------------------------------------------------------------
+# the argument structs of include/mmv.h, packed in one call (field by field assignment of a ctypes structure takes longer
+# than a small kernel)
+_KV_CACHE = struct.Struct("PPqqqqiiii")              # mmv_kv_cache
+_LINEAR_INPUTS = struct.Struct("PPPqqqqqqiiiiixxxx")   # mmv_linear_inputs
+
+
+def _on_device(first: torch.Tensor, *others) -> int:
+    """All tensors on the current CUDA device (the library launches there)."""
+    dev = torch.cuda.current_device()
+    for t in (first, *others):
+        if t is not None and t.get_device() != dev:
+            raise ValueError("tensors must be on the current CUDA device")
+    return dev
+
+
+def _value_code(x: torch.Tensor) -> int:
+    if x.dtype == torch.bfloat16:
+        return BF16_TO_F32
+    if x.dtype == torch.float16:
+        return F16_TO_F32
+    raise TypeError("values must be torch.float16 or torch.bfloat16")
+
+
+def _want(t, dtype, what: str):
+    if t is not None and (t.dtype != dtype or not t.is_contiguous()):
+        raise TypeError(f"{what} must be contiguous {dtype}")
+
+
+def _shaped(t, shape, what: str):
+    if t is not None and t.shape != shape:
+        raise ValueError(f"{what} must have shape {tuple(shape)}")
+
+
+def _rows(t, what: str):
+    if t.dim() != 3 or t.stride(2) != 1 and t.size(2) > 1:
+        raise ValueError(f"{what} must have three axes, the last contiguous")
+
+
+def _kept(stream, *made):
+    """Buffers made by a call for a stream other than the current one stay allocated until that stream is done with them."""
+    if stream is not None:
+        for t in made:
+            if t is not None:
+                t.record_stream(stream)
+
+
+def _cache_struct(k_cache: torch.Tensor, v_cache: torch.Tensor) -> bytes:
+    if k_cache.dim() != 4 or k_cache.shape != v_cache.shape or k_cache.stride() != v_cache.stride() or k_cache.dtype != v_cache.dtype:
+        raise ValueError("k_cache and v_cache must be alike: [blocks, block_size, heads, dim]")
+    blocks, block, heads, dim = k_cache.shape
+    sb, st, sh, sd = k_cache.stride()
+    if sd != 1 and dim > 1:
+        raise ValueError("the caches' last axis must be contiguous")
+    return _KV_CACHE.pack(k_cache.data_ptr(), v_cache.data_ptr(), blocks, sb, st, sh, block, heads, dim, _value_code(k_cache))
+
+
+def block_tables(past: torch.Tensor, added: torch.Tensor, free_blocks: torch.Tensor, table: torch.Tensor, slots: torch.Tensor,
+                 block_size: int, offsets: torch.Tensor | None = None, total: torch.Tensor | None = None,
+                 used: torch.Tensor | None = None, workspace: torch.Tensor | None = None, stream=None):
+    """mmv_block_tables: token offsets, slots and new block-table entries of a packed batch from the requests' lengths.
+
+    past, added: int32 [nreq]; free_blocks: int32; table: int32 [nreq, max_blocks] (rows may be strided), completed in
+    place; slots: int64, written whole (-1 behind the last token).  Returns (offsets int32 [nreq + 1], total int32 [nreq],
+    used int32 [1]: how many of free_blocks were taken)."""
+    _on_device(past, added, free_blocks, table, slots, offsets, total, used, workspace)
+    n = past.numel()
+    for t, what in ((past, "past"), (added, "added"), (free_blocks, "free_blocks"), (offsets, "offsets"), (total, "total"), (used, "used")):
+        _want(t, torch.int32, what)
+    _want(slots, torch.int64, "slots")
+    if table.dtype != torch.int32 or table.dim() != 2 or table.size(0) != n or (table.stride(1) != 1 and table.size(1) > 1):
+        raise TypeError("table must be int32 [requests, max_blocks], its rows contiguous")
+    if added.numel() != n:
+        raise ValueError("past and added must have one entry per request")
+    made = []
+    if offsets is None:
+        offsets = torch.empty(n + 1, dtype=torch.int32, device=past.device)
+        made.append(offsets)
+    if total is None:
+        total = torch.empty(n, dtype=torch.int32, device=past.device)
+        made.append(total)
+    if used is None:
+        used = torch.empty(1, dtype=torch.int32, device=past.device)
+        made.append(used)
+    if offsets.numel() < n + 1 or total.numel() < n or used.numel() < 1:
+        raise ValueError("offsets, total and used hold nreq + 1, nreq and 1 entries")
+    if workspace is None:
+        workspace = torch.empty(max(256, int(_lib.mmv_block_tables_workspace_bytes(n))), dtype=torch.uint8, device=past.device)
+        made.append(workspace)
+    rc = _lib.mmv_block_tables(past.data_ptr(), added.data_ptr(), n, int(block_size), free_blocks.data_ptr(), free_blocks.numel(),
+                               table.data_ptr(), table.stride(0), table.size(1), offsets.data_ptr(), total.data_ptr(),
+                               slots.data_ptr(), slots.numel(), used.data_ptr(), workspace.data_ptr(), workspace.numel(),
+                               _stream_ptr(stream))
+    if rc != MMV_OK:
+        raise MmvError(rc, "mmv_block_tables")
+    _kept(stream, *made)
+    return offsets, total, used
+
+
+def kv_append(k: torch.Tensor, v: torch.Tensor, slots: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor, stream=None) -> None:
+    """mmv_kv_append: writes the keys and values k, v [tokens, heads, dim] of a packed batch (views are fine) to their slots
+    (int64; negative: skipped) of the paged caches [blocks, block_size, heads, dim]."""
+    _on_device(k, v, slots, k_cache, v_cache)
+    _rows(k, "k")
+    _rows(v, "v")
+    _want(slots, torch.int64, "slots")
+    cache = _cache_struct(k_cache, v_cache)
+    if k.dtype != k_cache.dtype or v.dtype != k_cache.dtype:
+        raise TypeError("keys, values and caches must have one type")
+    if k.shape != v.shape or k.shape[1:] != k_cache.shape[2:] or slots.numel() != k.size(0):
+        raise ValueError("k, v must be [tokens, heads, dim] like the caches, with one slot per token")
+    rc = _lib.mmv_kv_append(k.data_ptr(), k.stride(0), k.stride(1), v.data_ptr(), v.stride(0), v.stride(1), slots.data_ptr(),
+                            slots.numel(), cache, _stream_ptr(stream))
+    if rc != MMV_OK:
+        raise MmvError(rc, "mmv_kv_append")
+
+
+def _linear_struct(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor) -> bytes:
+    for t, what in ((q, "q"), (k, "k"), (v, "v")):
+        _rows(t, what)
+    if q.dtype != k.dtype or q.dtype != v.dtype:
+        raise TypeError("q, k and v must have one type")
+    if k.shape[:2] != v.shape[:2] or q.size(0) != k.size(0) or q.size(2) != k.size(2) or q.size(1) % k.size(1):
+        raise ValueError("q [tokens, heads, dim_k], k [tokens, kv_heads, dim_k], v [tokens, kv_heads, dim_v] expected, heads a multiple of kv_heads")
+    return _LINEAR_INPUTS.pack(q.data_ptr(), k.data_ptr(), v.data_ptr(), q.stride(0), q.stride(1), k.stride(0), k.stride(1), v.stride(0),
+                               v.stride(1), q.size(1), k.size(1), q.size(2), v.size(2), _value_code(q))
+
+
+def linear_attention_step(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, log_decay: torch.Tensor, state: torch.Tensor,
+                          scale: float = 1.0, slots: torch.Tensor | None = None, state_out: torch.Tensor | None = None,
+                          out: torch.Tensor | None = None, stream=None) -> torch.Tensor:
+    """mmv_linear_attention_step: one token of linear attention for every request.
+
+    q [requests, heads, dim_k], k, v [requests, kv_heads, dim_k / dim_v]; log_decay fp32 [heads]; state fp32
+    [states, heads, dim_k, dim_v], request r's at slots[r] (int32; None: at r), updated in place unless state_out is given.
+    Returns out [requests, heads, dim_v]."""
+    state_out = state if state_out is None else state_out
+    _on_device(q, k, v, log_decay, state, slots, state_out, out)
+    inputs = _linear_struct(q, k, v)
+    n, heads, dv = q.size(0), q.size(1), v.size(2)
+    _want(log_decay, torch.float32, "log_decay")
+    _want(state, torch.float32, "state")
+    _want(state_out, torch.float32, "state_out")
+    _want(slots, torch.int32, "slots")
+    _want(out, q.dtype, "out")
+    _shaped(log_decay, (heads,), "log_decay")
+    _shaped(state, (state.size(0), heads, q.size(2), dv), "state")
+    _shaped(state_out, state.shape, "state_out")
+    _shaped(slots, (n,), "slots")
+    _shaped(out, (n, heads, dv), "out")
+    made = None
+    if out is None:
+        made = out = torch.empty(n, heads, dv, dtype=q.dtype, device=q.device)
+    rc = _lib.mmv_linear_attention_step(inputs, n, log_decay.data_ptr(), float(scale), state.data_ptr(), state_out.data_ptr(),
+                                        _ptr(slots), state.size(0), out.data_ptr(), _stream_ptr(stream))
+    if rc != MMV_OK:
+        raise MmvError(rc, "mmv_linear_attention_step")
+    _kept(stream, made)
+    return out

@@ -9,7 +9,8 @@ from pathlib import Path
 PKG = Path(__file__).resolve().parent
 CSRC = PKG / "csrc"
 LIB = PKG / "libmmv.so"
-SOURCES = [CSRC / "api.cu"]
+OBJ = PKG / "build"
+SOURCES = [CSRC / "api.cu", CSRC / "serve.cu"]
 NVCC = os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")
 
 
@@ -17,21 +18,39 @@ def needs_build() -> bool:
     if not LIB.exists():
         return True
     t = LIB.stat().st_mtime
-    deps = list(CSRC.glob("*.cu")) + list(CSRC.glob("*.cuh")) + list((PKG.parent / "include").glob("*.h"))
+    deps = list(CSRC.glob("*.cu")) + list(CSRC.glob("*.cuh")) + list(CSRC.glob("*.h")) + list((PKG.parent / "include").glob("*.h"))
     return any(d.stat().st_mtime > t for d in deps)
+
+
+def stale(obj: Path, deps: Path) -> bool:
+    """Whether an object is older than its source or a file that it included when it was last compiled."""
+    if not obj.exists() or not deps.exists():
+        return True
+    names = deps.read_text().replace("\\\n", " ").partition(":")[2].split()
+    t = obj.stat().st_mtime
+    return not names or any(not Path(n).exists() or Path(n).stat().st_mtime > t for n in names if not n.startswith("/usr/"))
 
 
 def build(force: bool = False, verbose: bool = False) -> Path:
     if not force and not needs_build():
         return LIB
-    tmp = LIB.with_suffix(f".{os.getpid()}.tmp")
-    cmd = [NVCC, "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
-           "-shared", "-Xcompiler", "-fPIC", "-DNDEBUG",
-           "-o", str(tmp)] + os.environ.get("MMV_NVCC_FLAGS", "").split() + [str(s) for s in SOURCES]
+    flags = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17", "-Xcompiler", "-fPIC", "-DNDEBUG"]
+    flags += os.environ.get("MMV_NVCC_FLAGS", "").split()
     if verbose:
-        cmd.insert(1, "-Xptxas")
-        cmd.insert(2, "-v")
-    subprocess.run(cmd, check=True)
+        flags += ["-Xptxas", "-v"]
+    # one object per source, so that an edit recompiles (side by side) only the sources that include the edited file
+    objs = [(s, OBJ / f"{s.stem}.o", OBJ / f"{s.stem}.d") for s in SOURCES]
+    OBJ.mkdir(exist_ok=True)
+    part = f".{os.getpid()}.tmp"
+    running = [(subprocess.Popen([NVCC, *flags, "-MD", "-MF", f"{d}{part}", "-c", "-o", f"{o}{part}", str(s)]), o, d)
+               for s, o, d in objs if force or stale(o, d)]
+    if any([p.wait() for p, _, _ in running]):
+        raise RuntimeError("nvcc failed")
+    for _, o, d in running:
+        os.replace(f"{o}{part}", o)
+        os.replace(f"{d}{part}", d)
+    tmp = LIB.with_suffix(f".{os.getpid()}.tmp")
+    subprocess.run([NVCC, "-gencode", "arch=compute_100a,code=sm_100a", "-shared", "-o", str(tmp), *(str(o) for _, o, _ in objs)], check=True)
     os.replace(tmp, LIB)
     return LIB
 

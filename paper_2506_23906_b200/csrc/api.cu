@@ -11,6 +11,7 @@
 
 #include "../../include/mmv.h"
 #include "common.cuh"
+#include "host_state.h"
 #include "seg_scan.cuh"
 #include "seg_sum.cuh"
 #include "compress.cuh"
@@ -18,10 +19,13 @@
 #include "seg_wide.cuh"
 
 namespace mmv {
-namespace {
 
+// (declared in host_state.h: the serving operators count their launches and bound their waits with the same words)
 std::atomic<long long> g_launches{0};
 std::atomic<unsigned long long> g_budget_ns{WAIT_BUDGET_NS};
+
+namespace {
+
 std::atomic<long long> g_debug_skip_span{-1};
 std::atomic<int> g_force_groups{0};
 std::atomic<int> g_force_scan_shape{-1};      // test hook: -1 = the library chooses
@@ -1129,7 +1133,7 @@ mmv_status mmv_last_async_status(const void* workspace, void* cuda_stream) {
     if (cudaStreamSynchronize(st) != cudaSuccess) return MMV_ERR_CUDA;
     WorkspaceHeader h;
     if (cudaMemcpy(&h, workspace, sizeof(unsigned int) * 2, cudaMemcpyDeviceToHost) != cudaSuccess) return MMV_ERR_CUDA;
-    return h.error <= 6u ? static_cast<mmv_status>(h.error) : MMV_ERR_CUDA;
+    return h.error <= MMV_ERR_OUT_OF_BLOCKS ? static_cast<mmv_status>(h.error) : MMV_ERR_CUDA;
 }
 
 mmv_status mmv_seg_scan_static(const void* x, const void* flags_u8, int64_t n, mmv_dtype dt, void* out,
@@ -1197,6 +1201,7 @@ const char* mmv_status_string(mmv_status s) {
         case MMV_ERR_BAD_SEGMENTS: return "segment offsets not monotone or out of range";
         case MMV_ERR_TIMEOUT: return "device-side wait timed out";
         case MMV_ERR_CUDA: return "CUDA call failed";
+        case MMV_ERR_OUT_OF_BLOCKS: return "free list, block table or slot map too short";
     }
     return "unknown status";
 }

@@ -141,7 +141,7 @@ __device__ __forceinline__ void report_error(WorkspaceHeader* hdr, unsigned int 
 }
 
 // Bounded mbarrier wait that also gives up when another role of the CTA has aborted.
-__device__ __noinline__ bool wait_bar_slow(uint64_t* bar, uint32_t parity, volatile int* abort_flag, uint64_t budget_ns) {
+static __device__ __noinline__ bool wait_bar_slow(uint64_t* bar, uint32_t parity, volatile int* abort_flag, uint64_t budget_ns) {
     const uint64_t t0 = global_timer_ns();
     uint32_t polls = 0;
     while (!mbar_try_wait(bar, parity)) {

@@ -1,0 +1,238 @@
+// Host side of the serving operators of include/mmv.h: argument checks, workspace carve-up and launches.
+#include <atomic>
+#include <cstdint>
+#include <cuda.h>
+#include <cuda_runtime.h>
+#include <mutex>
+
+#include "../../include/mmv.h"
+#include "common.cuh"
+#include "host_state.h"
+#include "block_tables.cuh"
+#include "kv_cache.cuh"
+#include "linear_attn.cuh"
+
+namespace mmv {
+namespace {
+
+constexpr int kMaxDevices = 64;
+constexpr int kMaxHeads = 1024;
+
+struct ServeDevice {
+    std::mutex lock;
+    std::atomic<bool> ok{false};
+    int sm_count = 0;
+};
+ServeDevice g_serve[kMaxDevices];
+
+template <typename K>
+bool allow_smem(K kernel, int bytes) {
+    return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes) == cudaSuccess;
+}
+
+constexpr int kTablesSmemMax = (2 * TABLES_FUSED_MAX + 1) * static_cast<int>(sizeof(int32_t));
+
+// One-time set-up of the current device (only success is remembered).
+ServeDevice* serve_device() {
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= kMaxDevices) return nullptr;
+    ServeDevice* d = &g_serve[dev];
+    if (d->ok.load(std::memory_order_acquire)) return d;
+    std::lock_guard<std::mutex> guard(d->lock);
+    if (d->ok.load(std::memory_order_relaxed)) return d;
+    int sm = 0;
+    if (cudaDeviceGetAttribute(&sm, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) return nullptr;
+    d->sm_count = sm;
+    bool ok = allow_smem(block_tables_kernel, kTablesSmemMax);
+    if (!ok) {
+        cudaGetLastError();
+        return nullptr;
+    }
+    d->ok.store(true, std::memory_order_release);
+    return d;
+}
+
+inline bool aligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
+// a stride of an axis that holds more than one entry keeps its rows on 16-byte words
+inline bool word_stride(int64_t stride, int64_t extent) { return extent <= 1 || stride % 8 == 0; }
+inline size_t round_up(size_t v, size_t a) { return (v + a - 1) / a * a; }
+
+// `after`: the kernel may start while the one in front of it in the stream still runs (it waits before it reads).
+template <typename... KP, typename... A>
+mmv_status launch(void (*kernel)(KP...), dim3 grid, int threads, size_t smem, cudaStream_t st, bool after, const A&... args) {
+    cudaLaunchConfig_t cfg{};
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.gridDim = grid;
+    cfg.blockDim = dim3(static_cast<unsigned>(threads));
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = st;
+    cfg.attrs = attr;
+    cfg.numAttrs = after ? 1 : 0;
+    const cudaError_t err = cudaLaunchKernelEx(&cfg, kernel, args...);
+    ++g_launches;
+    if (err == cudaSuccess) return MMV_OK;
+    cudaGetLastError();
+    return MMV_ERR_CUDA;
+}
+
+inline bool value_type(int dt) { return dt == MMV_F16_TO_F32 || dt == MMV_BF16_TO_F32; }
+
+mmv_status check_cache(const mmv_kv_cache* c) {
+    if (!c || !value_type(c->dtype)) return MMV_ERR_INVALID_ARG;
+    if (c->num_blocks < 0 || c->num_blocks > INT32_MAX || c->block_size < 1 || c->heads < 1 || c->heads > kMaxHeads) return MMV_ERR_INVALID_ARG;
+    if (c->dim < 8 || c->dim > 256 || c->dim % 8) return MMV_ERR_INVALID_ARG;
+    if (!word_stride(c->stride_block, c->num_blocks) || !word_stride(c->stride_token, c->block_size) || !word_stride(c->stride_head, c->heads))
+        return MMV_ERR_INVALID_ARG;
+    if (c->num_blocks && (!c->k || !c->v || !aligned(c->k, 16) || !aligned(c->v, 16))) return MMV_ERR_INVALID_ARG;
+    return MMV_OK;
+}
+
+mmv_status check_linear(const mmv_linear_inputs* in, int64_t tokens) {
+    if (!in || !value_type(in->dtype)) return MMV_ERR_INVALID_ARG;
+    if (in->heads < 1 || in->heads > kMaxHeads || in->kv_heads < 1 || in->heads % in->kv_heads) return MMV_ERR_INVALID_ARG;
+    if (in->dim_k < 8 || in->dim_k > 128 || in->dim_k % 8 || in->dim_v < 8 || in->dim_v > 128 || in->dim_v % 8) return MMV_ERR_INVALID_ARG;
+    if (!word_stride(in->q_stride_token, tokens) || !word_stride(in->q_stride_head, in->heads) || !word_stride(in->k_stride_token, tokens) ||
+        !word_stride(in->k_stride_head, in->kv_heads) || !word_stride(in->v_stride_token, tokens) || !word_stride(in->v_stride_head, in->kv_heads))
+        return MMV_ERR_INVALID_ARG;
+    if (!aligned(in->q, 16) || !aligned(in->k, 16) || !aligned(in->v, 16)) return MMV_ERR_INVALID_ARG;
+    return MMV_OK;
+}
+
+LinParams linear_params(const mmv_linear_inputs* in, const float* log_decay, float scale, void* out) {
+    LinParams p{};
+    p.q = static_cast<const uint16_t*>(in->q);
+    p.k = static_cast<const uint16_t*>(in->k);
+    p.v = static_cast<const uint16_t*>(in->v);
+    p.q_tok = in->q_stride_token;
+    p.q_head = in->q_stride_head;
+    p.k_tok = in->k_stride_token;
+    p.k_head = in->k_stride_head;
+    p.v_tok = in->v_stride_token;
+    p.v_head = in->v_stride_head;
+    p.heads = in->heads;
+    p.group = in->heads / in->kv_heads;
+    p.dk = in->dim_k;
+    p.dv = in->dim_v;
+    p.log_decay = log_decay;
+    p.scale = scale;
+    p.out = static_cast<uint16_t*>(out);
+    return p;
+}
+
+}  // namespace
+}  // namespace mmv
+
+using namespace mmv;
+
+extern "C" {
+
+size_t mmv_block_tables_workspace_bytes(int64_t nreq) {
+    if (nreq < 0 || nreq >= (1ll << 20)) return 0;
+    const size_t sums = nreq > TABLES_FUSED_MAX ? static_cast<size_t>(nreq) * sizeof(int32_t) : 0;
+    return round_up(sizeof(WorkspaceHeader) + sums, 256);
+}
+
+mmv_status mmv_block_tables(const int32_t* past, const int32_t* added, int64_t nreq, int32_t block_size, const int32_t* free_blocks,
+                            int64_t nfree, int32_t* table, int64_t table_stride, int64_t max_blocks, int32_t* offsets, int32_t* total,
+                            int64_t* slots, int64_t nslots, int32_t* used, void* workspace, size_t workspace_bytes, void* cuda_stream) {
+    if (nreq < 0 || nreq >= (1ll << 20) || block_size < 1 || nfree < 0 || max_blocks < 0 || nslots < 0) return MMV_ERR_INVALID_ARG;
+    if (!offsets || !used || !workspace || !aligned(offsets, 4) || !aligned(used, 4) || !aligned(workspace, 256)) return MMV_ERR_INVALID_ARG;
+    if (nreq && (!past || !added || !total || !aligned(past, 4) || !aligned(added, 4) || !aligned(total, 4))) return MMV_ERR_INVALID_ARG;
+    if (nreq && max_blocks && (!table || !aligned(table, 4) || (nreq > 1 && table_stride < max_blocks))) return MMV_ERR_INVALID_ARG;
+    if ((nfree && (!free_blocks || !aligned(free_blocks, 4))) || (nslots && (!slots || !aligned(slots, 8)))) return MMV_ERR_INVALID_ARG;
+    if (workspace_bytes < mmv_block_tables_workspace_bytes(nreq)) return MMV_ERR_WORKSPACE_TOO_SMALL;
+    ServeDevice* dev = serve_device();
+    if (!dev) return MMV_ERR_CUDA;
+    cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+    TablesParams p;
+    p.past = past;
+    p.added = added;
+    p.free_blocks = free_blocks;
+    p.table = table;
+    p.offsets = offsets;
+    p.total = total;
+    p.used = used;
+    p.slots = slots;
+    p.nfree = nfree;
+    p.table_stride = table_stride;
+    p.nslots = nslots;
+    p.nreq = static_cast<int>(nreq);
+    p.block_size = block_size;
+    p.max_blocks = max_blocks;
+    p.hdr = static_cast<WorkspaceHeader*>(workspace);
+    p.base = reinterpret_cast<int32_t*>(static_cast<uint8_t*>(workspace) + sizeof(WorkspaceHeader));
+    long long ctas = (nslots + TABLES_TOKENS_PER_CTA - 1) / TABLES_TOKENS_PER_CTA;
+    if (ctas > dev->sm_count) ctas = dev->sm_count;
+    if (ctas < 1) ctas = 1;
+    if (nreq <= TABLES_FUSED_MAX)
+        return launch(block_tables_kernel, dim3(static_cast<unsigned>(ctas)), TABLES_THREADS, (2 * nreq + 1) * sizeof(int32_t), st, false, p);
+    const mmv_status rc = launch(block_tables_scan_kernel, dim3(1), TABLES_THREADS, 0, st, false, p);
+    if (rc != MMV_OK || nslots == 0) return rc;
+    return launch(block_tables_expand_kernel, dim3(static_cast<unsigned>(ctas)), TABLES_THREADS, 0, st, true, p);
+}
+
+mmv_status mmv_kv_append(const void* k, int64_t k_stride_token, int64_t k_stride_head, const void* v, int64_t v_stride_token,
+                         int64_t v_stride_head, const int64_t* slots, int64_t ntok, const mmv_kv_cache* cache, void* cuda_stream) {
+    if (ntok < 0 || check_cache(cache) != MMV_OK) return MMV_ERR_INVALID_ARG;
+    if (!word_stride(k_stride_token, ntok) || !word_stride(k_stride_head, cache->heads) || !word_stride(v_stride_token, ntok) ||
+        !word_stride(v_stride_head, cache->heads))
+        return MMV_ERR_INVALID_ARG;
+    if (ntok == 0 || cache->num_blocks == 0) return MMV_OK;
+    if (!k || !v || !slots || !aligned(k, 16) || !aligned(v, 16) || !aligned(slots, 8)) return MMV_ERR_INVALID_ARG;
+    ServeDevice* dev = serve_device();
+    if (!dev) return MMV_ERR_CUDA;
+    AppendParams p;
+    p.k = static_cast<const uint16_t*>(k);
+    p.v = static_cast<const uint16_t*>(v);
+    p.ck = static_cast<uint16_t*>(cache->k);
+    p.cv = static_cast<uint16_t*>(cache->v);
+    p.slots = slots;
+    p.ntok = ntok;
+    p.k_tok = k_stride_token;
+    p.k_head = k_stride_head;
+    p.v_tok = v_stride_token;
+    p.v_head = v_stride_head;
+    p.c_block = cache->stride_block;
+    p.c_tok = cache->stride_token;
+    p.c_head = cache->stride_head;
+    p.nslots = cache->num_blocks * cache->block_size;
+    p.block_size = cache->block_size;
+    p.words_per_head = cache->dim / 8;
+    p.words_per_row = cache->heads * p.words_per_head;
+    const long long words = ntok * p.words_per_row;
+    long long blocks = (words + APPEND_THREADS - 1) / APPEND_THREADS;
+    const long long cap = static_cast<long long>(dev->sm_count) * 8;        // 2048 threads per SM
+    if (blocks > cap) blocks = cap;
+    return launch(kv_append_kernel, dim3(static_cast<unsigned>(blocks)), APPEND_THREADS, 0, static_cast<cudaStream_t>(cuda_stream), false, p);
+}
+
+mmv_status mmv_linear_attention_step(const mmv_linear_inputs* in, int64_t nreq, const float* log_decay, float scale, const float* state,
+                                     float* state_out, const int32_t* slots, int64_t num_slots, void* out, void* cuda_stream) {
+    if (nreq < 0 || num_slots < 0 || check_linear(in, nreq) != MMV_OK) return MMV_ERR_INVALID_ARG;
+    if (nreq == 0) return MMV_OK;
+    if (!in->q || !in->k || !in->v || !log_decay || !out || !aligned(log_decay, 4) || !aligned(out, 16)) return MMV_ERR_INVALID_ARG;
+    if (num_slots && (!state || !state_out || !aligned(state, 16) || !aligned(state_out, 16))) return MMV_ERR_INVALID_ARG;
+    if (slots ? !aligned(slots, 4) : num_slots < nreq) return MMV_ERR_INVALID_ARG;
+    if (nreq > INT32_MAX / (static_cast<int64_t>(in->heads) * 16)) return MMV_ERR_INVALID_ARG;       // one CTA per state and column part
+    ServeDevice* dev = serve_device();
+    if (!dev) return MMV_ERR_CUDA;
+    LinParams p = linear_params(in, log_decay, scale, out);
+    p.state = state;
+    p.state_out = state_out;
+    p.slots = slots;
+    p.nreq = nreq;
+    p.num_slots = num_slots;
+    const bool wide = p.dv > 64 && nreq * p.heads >= 4ll * dev->sm_count;
+    p.parts = wide ? 1 : (p.dv + 31) / 32;
+    const dim3 grid(static_cast<unsigned>(nreq * p.heads * p.parts));
+    cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+    if (in->dtype == MMV_BF16_TO_F32)
+        return wide ? launch(linear_step_kernel<true, 128>, grid, LIN_STEP_THREADS, 0, st, false, p)
+                    : launch(linear_step_kernel<true, 32>, grid, LIN_STEP_THREADS, 0, st, false, p);
+    return wide ? launch(linear_step_kernel<false, 128>, grid, LIN_STEP_THREADS, 0, st, false, p)
+                : launch(linear_step_kernel<false, 32>, grid, LIN_STEP_THREADS, 0, st, false, p);
+}
+
+}  // extern "C"
