@@ -439,6 +439,31 @@ mmv_status mmv_kv_append(const void *k, int64_t k_stride_token, int64_t k_stride
                          const int64_t *slots, int64_t ntok, const mmv_kv_cache *cache, void *cuda_stream);
 
 /*
+ * Attention of one new token per request over a paged cache: request r attends
+ * with q[r] (heads x cache->dim; request and head strides of its own) to its
+ * tokens j in [max(0, lens[r] - window), lens[r]) (window 0: all of them), token j
+ * in block table[r, j / block_size]:
+ *     s_j = scale * q . k_j,  out = sum_j softmax(s)_j v_j,  lse = log sum_j exp(s_j)
+ * heads is a multiple of cache->heads; query head h reads key / value head
+ * h / (heads / cache->heads).  The new token's own key and value are expected in the
+ * cache (mmv_kv_append) and counted in lens.  out: nreq x heads x dim, the
+ * cache's type; lse: nreq x heads fp32, or NULL.  A request of length 0 gives out 0
+ * and lse -infinity.  Scores, weights and sums are fp32 (weights enter the second
+ * product as sums of two 16-bit values); results do not depend on timing.
+ * Entries of the cache outside the stated tokens are never read, whatever they
+ * hold.  Never dereferenced, and recorded as MMV_ERR_INVALID_ARG in the workspace
+ * (outputs of that request are then unspecified): a table entry outside
+ * [0, num_blocks), a length that is negative or beyond max_blocks * block_size.
+ * nreq < 2^20.  Workspace: mmv_paged_attention_workspace_bytes(heads, cache),
+ * 256-byte aligned (up to 8 MB).
+ */
+size_t mmv_paged_attention_workspace_bytes(int32_t heads, const mmv_kv_cache *cache);
+mmv_status mmv_paged_attention(const void *q, int64_t q_stride_request, int64_t q_stride_head, int32_t heads,
+                               const mmv_kv_cache *cache, const int32_t *table, int64_t table_stride,
+                               int64_t max_blocks, const int32_t *lens, int64_t nreq, float scale, int64_t window,
+                               void *out, float *lse, void *workspace, size_t workspace_bytes, void *cuda_stream);
+
+/*
  * Inputs of linear attention: q [.., heads, dim_k], k [.., kv_heads, dim_k],
  * v [.., kv_heads, dim_v] with a token (or request) in front, token and head
  * strides of their own.  heads is a multiple of kv_heads: query head h uses key /

@@ -31,6 +31,7 @@ EXPORTS = (
     "mmv_seg_scan_minmax", "mmv_seg_scan_i8_i64", "mmv_seg_scan_shard", "mmv_seg_scan_shard_finish",
     "mmv_debug_force_scan_shape", "mmv_mult_i8",
     "mmv_block_tables_workspace_bytes", "mmv_block_tables", "mmv_kv_append", "mmv_linear_attention_step",
+    "mmv_paged_attention_workspace_bytes", "mmv_paged_attention",
 )
 SHARD_SUMMARY_BYTES = 16
 STATIC_SCAN_MAX_N = 1 << 28
@@ -94,6 +95,10 @@ def _load() -> ctypes.CDLL:
     lib.mmv_block_tables.argtypes = [vp, vp, i64, ci, vp, i64, vp, i64, i64, vp, vp, vp, i64, vp, vp, sz, vp]
     lib.mmv_kv_append.restype = ci
     lib.mmv_kv_append.argtypes = [vp, i64, i64, vp, i64, i64, vp, i64, vp, vp]
+    lib.mmv_paged_attention_workspace_bytes.restype = sz
+    lib.mmv_paged_attention_workspace_bytes.argtypes = [ci, vp]
+    lib.mmv_paged_attention.restype = ci
+    lib.mmv_paged_attention.argtypes = [vp, i64, i64, ci, vp, vp, i64, i64, vp, i64, f32, i64, vp, vp, vp, sz, vp]
     lib.mmv_linear_attention_step.restype = ci
     lib.mmv_linear_attention_step.argtypes = [vp, i64, vp, f32, vp, vp, vp, i64, vp, vp]
     lib.mmv_debug_force_scan_shape.restype = None
@@ -503,6 +508,49 @@ def kv_append(k: torch.Tensor, v: torch.Tensor, slots: torch.Tensor, k_cache: to
                             slots.numel(), cache, _stream_ptr(stream))
     if rc != MMV_OK:
         raise MmvError(rc, "mmv_kv_append")
+
+
+def paged_attention(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor, table: torch.Tensor, lens: torch.Tensor,
+                    scale: float | None = None, window: int = 0, out: torch.Tensor | None = None, lse: torch.Tensor | None = None,
+                    workspace: torch.Tensor | None = None, stream=None):
+    """mmv_paged_attention: attention of one new token per request, q [requests, heads, dim], over the paged caches
+    [blocks, block_size, kv_heads, dim] through table int32 [requests, max_blocks] (rows may be strided) and lens int32
+    [requests].  scale None: dim ** -0.5; window > 0: the last `window` tokens only.  Returns (out [requests, heads, dim],
+    lse fp32 [requests, heads])."""
+    _on_device(q, k_cache, v_cache, table, lens, out, lse, workspace)
+    _rows(q, "q")
+    n, heads, dim = q.shape
+    cache = _cache_struct(k_cache, v_cache)
+    _want(lens, torch.int32, "lens")
+    _want(out, q.dtype, "out")
+    _want(lse, torch.float32, "lse")
+    _shaped(lens, (n,), "lens")
+    _shaped(out, q.shape, "out")
+    _shaped(lse, (n, heads), "lse")
+    if table.dtype != torch.int32 or table.dim() != 2 or table.size(0) != n or (table.stride(1) != 1 and table.size(1) > 1):
+        raise TypeError("table must be int32 [requests, max_blocks], its rows contiguous")
+    if q.dtype != k_cache.dtype:
+        raise TypeError("queries and caches must have one type")
+    if dim != k_cache.size(3) or heads % k_cache.size(2):
+        raise ValueError("q must be [requests, heads, dim] with the caches' dim and a multiple of their heads")
+    made = []
+    if out is None:
+        out = torch.empty(n, heads, dim, dtype=q.dtype, device=q.device)
+        made.append(out)
+    if lse is None:
+        lse = torch.empty(n, heads, dtype=torch.float32, device=q.device)
+        made.append(lse)
+    if workspace is None:
+        nbytes = int(_lib.mmv_paged_attention_workspace_bytes(heads, cache))
+        workspace = torch.empty(max(nbytes, 256), dtype=torch.uint8, device=q.device)
+        made.append(workspace)
+    rc = _lib.mmv_paged_attention(q.data_ptr(), q.stride(0), q.stride(1), heads, cache, table.data_ptr(), table.stride(0), table.size(1),
+                                  lens.data_ptr(), n, dim ** -0.5 if scale is None else float(scale), int(window), out.data_ptr(),
+                                  lse.data_ptr(), workspace.data_ptr(), workspace.numel(), _stream_ptr(stream))
+    if rc != MMV_OK:
+        raise MmvError(rc, "mmv_paged_attention")
+    _kept(stream, *made)
+    return out, lse
 
 
 def _linear_struct(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor) -> bytes:

@@ -11,6 +11,7 @@
 #include "block_tables.cuh"
 #include "kv_cache.cuh"
 #include "linear_attn.cuh"
+#include "paged_attn.cuh"
 
 namespace mmv {
 namespace {
@@ -44,6 +45,12 @@ ServeDevice* serve_device() {
     if (cudaDeviceGetAttribute(&sm, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) return nullptr;
     d->sm_count = sm;
     bool ok = allow_smem(block_tables_kernel, kTablesSmemMax);
+    ok &= allow_smem(paged_attention_kernel<false, 64>, PagedCfg<64>::smem_bytes(PA_ROWS));
+    ok &= allow_smem(paged_attention_kernel<true, 64>, PagedCfg<64>::smem_bytes(PA_ROWS));
+    ok &= allow_smem(paged_attention_kernel<false, 128>, PagedCfg<128>::smem_bytes(PA_ROWS));
+    ok &= allow_smem(paged_attention_kernel<true, 128>, PagedCfg<128>::smem_bytes(PA_ROWS));
+    ok &= allow_smem(paged_attention_kernel<false, 256>, PagedCfg<256>::smem_bytes(PA_ROWS));
+    ok &= allow_smem(paged_attention_kernel<true, 256>, PagedCfg<256>::smem_bytes(PA_ROWS));
     if (!ok) {
         cudaGetLastError();
         return nullptr;
@@ -119,6 +126,43 @@ LinParams linear_params(const mmv_linear_inputs* in, const float* log_decay, flo
     p.scale = scale;
     p.out = static_cast<uint16_t*>(out);
     return p;
+}
+
+// Query heads of one key head in parts of up to PA_ROWS, of nearly equal size.
+struct PagedHeads {
+    int group, parts, rows;
+};
+PagedHeads paged_heads(int heads, int kv_heads) {
+    PagedHeads h;
+    h.group = heads / kv_heads;
+    h.parts = (h.group + PA_ROWS - 1) / PA_ROWS;
+    h.rows = (h.group + h.parts - 1) / h.parts;
+    return h;
+}
+int paged_padded(int dim) { return dim <= 64 ? 64 : dim <= 128 ? 128 : 256; }
+// Resident CTAs per SM: what the shared memory of PA_ROWS rows allows (111, 57 and 220 KB of 227).
+int paged_per_sm(int padded) { return padded == 64 ? 3 : padded == 128 ? 2 : 1; }
+constexpr int kPagedMaxSms = 160;
+
+struct PagedPlan {
+    size_t desc_off, ml_off, o_off, total;
+};
+PagedPlan paged_plan(const PagedHeads& h, int dim) {
+    const size_t ctas = static_cast<size_t>(kPagedMaxSms) * paged_per_sm(paged_padded(dim));
+    PagedPlan w;
+    w.desc_off = sizeof(WorkspaceHeader);
+    w.ml_off = round_up(w.desc_off + ctas * 4 * sizeof(int32_t), 256);
+    w.o_off = round_up(w.ml_off + ctas * 4 * PA_ROWS * sizeof(float), 256);
+    w.total = round_up(w.o_off + ctas * 2 * h.rows * dim * sizeof(float), 256);
+    return w;
+}
+
+template <bool BF16, int DP>
+mmv_status launch_paged(const PagedParams& p, int ctas, cudaStream_t st) {
+    const mmv_status rc = launch(paged_attention_kernel<BF16, DP>, dim3(static_cast<unsigned>(ctas)), PA_THREADS,
+                                 static_cast<size_t>(PagedCfg<DP>::smem_bytes(p.rows)), st, false, p);
+    if (rc != MMV_OK) return rc;
+    return launch(paged_join_kernel<BF16>, dim3(static_cast<unsigned>(ctas), static_cast<unsigned>(p.rows)), PA_JOIN_THREADS, 0, st, true, p, ctas);
 }
 
 }  // namespace
@@ -206,6 +250,73 @@ mmv_status mmv_kv_append(const void* k, int64_t k_stride_token, int64_t k_stride
     const long long cap = static_cast<long long>(dev->sm_count) * 8;        // 2048 threads per SM
     if (blocks > cap) blocks = cap;
     return launch(kv_append_kernel, dim3(static_cast<unsigned>(blocks)), APPEND_THREADS, 0, static_cast<cudaStream_t>(cuda_stream), false, p);
+}
+
+size_t mmv_paged_attention_workspace_bytes(int32_t heads, const mmv_kv_cache* cache) {
+    if (check_cache(cache) != MMV_OK || heads < 1 || heads > kMaxHeads || heads % cache->heads) return 0;
+    return paged_plan(paged_heads(heads, cache->heads), cache->dim).total;
+}
+
+mmv_status mmv_paged_attention(const void* q, int64_t q_stride_request, int64_t q_stride_head, int32_t heads, const mmv_kv_cache* cache,
+                               const int32_t* table, int64_t table_stride, int64_t max_blocks, const int32_t* lens, int64_t nreq,
+                               float scale, int64_t window, void* out, float* lse, void* workspace, size_t workspace_bytes,
+                               void* cuda_stream) {
+    if (nreq < 0 || nreq >= (1ll << 20) || max_blocks < 0 || window < 0 || check_cache(cache) != MMV_OK) return MMV_ERR_INVALID_ARG;
+    if (heads < 1 || heads > kMaxHeads || heads % cache->heads) return MMV_ERR_INVALID_ARG;
+    if (!word_stride(q_stride_request, nreq) || !word_stride(q_stride_head, heads)) return MMV_ERR_INVALID_ARG;
+    if (!workspace || !aligned(workspace, 256)) return MMV_ERR_INVALID_ARG;
+    if (nreq && (!q || !aligned(q, 16) || !lens || !aligned(lens, 4) || !out || !aligned(out, 16) || (lse && !aligned(lse, 4))))
+        return MMV_ERR_INVALID_ARG;
+    if (nreq && max_blocks && (!table || !aligned(table, 4) || (nreq > 1 && table_stride < max_blocks))) return MMV_ERR_INVALID_ARG;
+    const PagedHeads h = paged_heads(heads, cache->heads);
+    const PagedPlan plan = paged_plan(h, cache->dim);
+    if (workspace_bytes < plan.total) return MMV_ERR_WORKSPACE_TOO_SMALL;
+    cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+    if (nreq == 0) return cudaMemsetAsync(workspace, 0, sizeof(WorkspaceHeader), st) == cudaSuccess ? MMV_OK : MMV_ERR_CUDA;
+    ServeDevice* dev = serve_device();
+    if (!dev) return MMV_ERR_CUDA;
+    uint8_t* ws = static_cast<uint8_t*>(workspace);
+    PagedParams p;
+    p.q = static_cast<const uint16_t*>(q);
+    p.k = static_cast<const uint16_t*>(cache->k);
+    p.v = static_cast<const uint16_t*>(cache->v);
+    p.q_req = q_stride_request;
+    p.q_head = q_stride_head;
+    p.c_block = cache->stride_block;
+    p.c_tok = cache->stride_token;
+    p.c_head = cache->stride_head;
+    p.table = table;
+    p.lens = lens;
+    p.table_stride = table_stride;
+    p.num_blocks = cache->num_blocks;
+    const int64_t longest = INT32_MAX - 4 * PA_TILE;                 // (positions past a tile's end stay within 32 bits)
+    p.capacity = max_blocks > longest / cache->block_size ? longest : max_blocks * cache->block_size;
+    p.window = window;
+    p.nreq = static_cast<int>(nreq);
+    p.block_size = cache->block_size;
+    p.dim = cache->dim;
+    p.heads = heads;
+    p.kv_heads = cache->heads;
+    p.group = h.group;
+    p.parts = h.parts;
+    p.rows = h.rows;
+    p.scale_log2 = scale * 1.4426950408889634f;
+    p.out = static_cast<uint16_t*>(out);
+    p.lse = lse;
+    p.hdr = reinterpret_cast<WorkspaceHeader*>(ws);
+    p.desc = reinterpret_cast<int32_t*>(ws + plan.desc_off);
+    p.part_ml = reinterpret_cast<float*>(ws + plan.ml_off);
+    p.part_o = reinterpret_cast<float*>(ws + plan.o_off);
+    const int padded = paged_padded(p.dim);
+    // one CTA per tile that the tables could hold, up to all that are resident at once
+    const int sms = dev->sm_count < kPagedMaxSms ? dev->sm_count : kPagedMaxSms;
+    const double most = static_cast<double>(nreq) * p.kv_heads * p.parts * (static_cast<double>(p.capacity) / PA_TILE + 2.0);
+    int ctas = sms * paged_per_sm(padded);
+    if (most < ctas) ctas = static_cast<int>(most);
+    const bool bf16 = cache->dtype == MMV_BF16_TO_F32;
+    if (padded == 64) return bf16 ? launch_paged<true, 64>(p, ctas, st) : launch_paged<false, 64>(p, ctas, st);
+    if (padded == 128) return bf16 ? launch_paged<true, 128>(p, ctas, st) : launch_paged<false, 128>(p, ctas, st);
+    return bf16 ? launch_paged<true, 256>(p, ctas, st) : launch_paged<false, 256>(p, ctas, st);
 }
 
 mmv_status mmv_linear_attention_step(const mmv_linear_inputs* in, int64_t nreq, const float* log_decay, float scale, const float* state,

@@ -283,3 +283,156 @@ def test_linear_step_own_index_and_nothing(mmv):
     assert torch.equal(mmv.linear_attention_step(q, q, q, g, state, state_out=s1), mmv.linear_attention_step(q, q, q, g, state, slots=a, state_out=s2))
     assert torch.equal(s1, s2)
     assert mmv.linear_attention_step(q[:0], q[:0], q[:0], g, state).shape == (0, 2, 16)
+
+
+# ---------------------------------------------------------------------------------------------------------------------
+# attention of one token over the paged cache
+# ---------------------------------------------------------------------------------------------------------------------
+def paged_case(seed, lens, heads, kv, dim, block, dtype, order="bthd", pad=0, spare=3, garbage=float("nan"), far=0):
+    """Caches filled with `garbage` except at the requests' own tokens, pages in random order, the rest of the table out of range."""
+    gen = torch.Generator("cuda").manual_seed(seed)
+    pages = [-(-n // block) for n in lens]
+    blocks = sum(pages) + spare + far
+    kc, vc = paged(blocks, block, kv, dim, dtype, order, pad)
+    ids = (far + torch.randperm(sum(pages) + spare, device="cuda", generator=gen)).tolist()
+    table = torch.full((len(lens), max(pages + [1]) + 1), -7, dtype=torch.int32, device="cuda")
+    wide = torch.full((len(lens), table.size(1) + 3), 2 ** 31 - 1, dtype=torch.int32, device="cuda")
+    keep = torch.zeros(blocks, block, dtype=torch.bool, device="cuda")
+    at = 0
+    for r, n in enumerate(lens):
+        mine = torch.tensor(ids[at:at + pages[r]], dtype=torch.int64, device="cuda")
+        at += pages[r]
+        table[r, :pages[r]] = mine.to(torch.int32)
+        j = torch.arange(n, device="cuda")
+        keep[mine[j // block], j % block] = True
+    wide[:, :table.size(1)] = table
+    for c in (kc, vc):
+        c.masked_fill_(~keep[:, :, None, None], garbage)
+    q = torch.randn(len(lens), heads, dim + 16, device="cuda", generator=gen).to(dtype)[..., :dim]
+    return q, kc, vc, wide[:, :table.size(1)], torch.tensor(lens, dtype=torch.int32, device="cuda")
+
+
+def paged_plain(q, kc, vc, table, lens, scale, window):
+    """Definition in 64 bits, with the magnitudes that the bound needs."""
+    n, heads, dim = q.shape
+    kv, block = kc.size(2), kc.size(1)
+    group = heads // kv
+    out = torch.zeros(n, heads, dim, dtype=torch.float64, device="cuda")
+    mag, lse, big = torch.zeros_like(out), torch.full((n, heads), -float("inf"), dtype=torch.float64, device="cuda"), torch.zeros(n, heads, device="cuda").double()
+    for r, length in enumerate(lens.tolist()):
+        if length <= 0:
+            continue
+        lo = max(0, length - window) if window else 0
+        pages = table[r, :-(-length // block)].long()
+        for h in range(kv):
+            k, v = (c[pages, :, h].reshape(-1, dim)[lo:length].double() for c in (kc, vc))
+            rows = slice(h * group, (h + 1) * group)
+            x = scale * q[r, rows].double() @ k.T
+            w = torch.softmax(x, 1)
+            out[r, rows], mag[r, rows], lse[r, rows] = w @ v, w @ v.abs(), torch.logsumexp(x, 1)
+            # (a token whose score is -infinity has weight 0 whatever its rounding: it has no part in the bound)
+            big[r, rows] = scale * torch.where(torch.isfinite(x), q[r, rows].double().abs() @ k.abs().T, 0.0).amax(1)
+    return out, mag, lse, big
+
+
+def check_paged(mmv, case, dtype, scale, window=0):
+    """Scores: a sum of dim products in fp32, (dim + 8) e S with S the largest scale sum |q k|, the base-2 exponent's rounding among it;
+    weights: that relative error twice (weight and sum), 2^-16 for the pair of 16-bit values, and the running sums' roundings, one per 16
+    tokens of a warp and one per partial result."""
+    q, kc, vc, table, lens = case
+    n, heads, dim = q.shape
+    ws = torch.empty(16 << 20, dtype=torch.uint8, device="cuda")
+    guard = torch.full((n * heads * dim + 64,), 3.0, dtype=dtype, device="cuda")
+    out, lse = mmv.paged_attention(q, kc, vc, table, lens, scale=scale, window=window, out=guard[:n * heads * dim].view(n, heads, dim), workspace=ws)
+    assert mmv.last_async_status(ws) == 0 and (guard[n * heads * dim:] == 3.0).all()
+    want, mag, wlse, big = paged_plain(q, kc, vc, table, lens, scale, window)
+    chain = (lens.double() / 16 + 700)[:, None]
+    score = (dim + 16) * E * big
+    inside(out, want, U[dtype] * want.abs() + mag * (2.0 ** -16 + 3 * score + chain * E)[..., None] + TINY[dtype])
+    inside(lse, wlse, torch.nan_to_num(2 * score + chain * E + 8 * E * wlse.abs(), posinf=0.0))
+    again, _ = mmv.paged_attention(q, kc, vc, table, lens, scale=scale, window=window)
+    assert torch.equal(out, again)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("heads,kv,dim,block,order,pad", [
+    (1, 1, 8, 16, "bthd", 0), (4, 4, 64, 16, "bthd", 0), (8, 1, 40, 7, "bthd", 8), (32, 8, 128, 16, "bthd", 0), (12, 2, 80, 1, "bhtd", 0),
+    (71, 1, 64, 64, "hbtd", 0), (48, 2, 128, 48, "bhtd", 16), (16, 2, 256, 16, "bthd", 0), (5, 5, 136, 24, "bthd", 0)])
+@pytest.mark.parametrize("lens", [[1], [0, 1, 2, 15, 16, 17, 0], [63, 64, 65, 127, 128, 129], [1000, 3, 0, 517, 2048, 1]])
+def test_paged_attention(mmv, dtype, heads, kv, dim, block, order, pad, lens):
+    check_paged(mmv, paged_case(dim + len(lens), lens, heads, kv, dim, block, dtype, order, pad), dtype, dim ** -0.5)
+
+
+@pytest.mark.parametrize("window", [1, 15, 16, 17, 64, 100, 1000, 10 ** 6])
+def test_paged_attention_window(mmv, window):
+    lens = [1, 16, 17, 100, 101, 640, 999, 0, 1500]
+    check_paged(mmv, paged_case(window, lens, 8, 2, 64, 16, torch.float16), torch.float16, 0.125, window)
+    check_paged(mmv, paged_case(window + 1, lens, 2, 2, 128, 9, torch.bfloat16), torch.bfloat16, 0.1, window)
+
+
+@pytest.mark.parametrize("dtype,lens,heads,kv,dim,block", [
+    (torch.bfloat16, [70001], 8, 1, 128, 16), (torch.float16, [50000, 1, 0, 2], 4, 2, 64, 64), (torch.bfloat16, [30011], 1, 1, 256, 16),
+    (torch.float16, [5] * 700 + [20000] + [0] * 50 + [64] * 300, 16, 4, 64, 16)])
+def test_paged_attention_split(mmv, dtype, lens, heads, kv, dim, block):
+    """Few long requests over many ranges, and many short ones in each."""
+    check_paged(mmv, paged_case(sum(lens), lens, heads, kv, dim, block, dtype), dtype, 1.5 * dim ** -0.5)
+
+
+def test_paged_attention_large_scores(mmv):
+    """Scores of hundreds: the running maximum carries the sum; and equal ones (q = 0): the mean."""
+    q, kc, vc, table, lens = paged_case(3, [300, 5000], 8, 2, 64, 16, torch.float16)
+    check_paged(mmv, (q * 8, kc, vc, table, lens), torch.float16, 2.0)
+    check_paged(mmv, (q * 0, kc, vc, table, lens), torch.float16, 2.0)
+
+
+def test_paged_attention_not_finite_inside(mmv):
+    """A NaN among a request's own values stays in that request and head group; scores of -infinity weigh nothing."""
+    q, kc, vc, table, lens = paged_case(5, [300, 200, 9000], 4, 2, 64, 16, torch.float16, garbage=0.0)
+    vc[table[1, 3], 2, 1, 7] = float("nan")
+    kc[table[2, 100], 1, 0, 3] = float("nan")
+    out, lse = mmv.paged_attention(q, kc, vc, table, lens)
+    bad = torch.isnan(out)
+    assert bad[1, 2:, 7].all() and bad[2, :2].all() and int(bad.sum()) == 2 + 2 * 64
+    q, kc, vc, table, lens = paged_case(6, [90, 5000], 2, 1, 64, 16, torch.float16, garbage=0.0)
+    q[:] = 1.0
+    for j in (0, 1, 17, 63, 64, 80):
+        for r in range(2):
+            kc[table[r, j // 16], j % 16] = -float("inf")
+    check_paged(mmv, (q, kc, vc, table, lens), torch.float16, 0.125)
+    kc[:] = -float("inf")
+    out, lse = mmv.paged_attention(q, kc, vc, table, lens)
+    assert (out == 0).all() and (lse == -float("inf")).all()
+
+
+def test_paged_attention_far_pages(mmv):
+    """Pages whose offsets pass 32 bits."""
+    far = (1 << 32) // (16 * 2 * 128) + 10
+    check_paged(mmv, paged_case(9, [100, 33], 8, 2, 128, 16, torch.float16, garbage=0.0, far=far), torch.float16, 0.1)
+
+
+def test_paged_attention_bad_metadata_is_reported(mmv):
+    q, kc, vc, table, lens = paged_case(11, [100, 50, 70], 4, 2, 64, 16, torch.float16)
+    ws = torch.empty(16 << 20, dtype=torch.uint8, device="cuda")
+    good, _ = mmv.paged_attention(q, kc, vc, table, lens)
+    for change in ("page", "negative page", "length", "negative length"):
+        t, n = table.clone(), lens.clone()
+        if change == "page":
+            t[1, 2] = kc.size(0)
+        elif change == "negative page":
+            t[1, 0] = -1
+        else:
+            n[1] = 10 ** 6 if change == "length" else -5
+        out, _ = mmv.paged_attention(q, kc, vc, t, n, workspace=ws)
+        assert mmv.last_async_status(ws) == 1
+        assert torch.equal(out[[0, 2]], good[[0, 2]])
+    mmv.paged_attention(q, kc, vc, table, lens, workspace=ws)
+    assert mmv.last_async_status(ws) == 0
+
+
+def test_paged_attention_without_requests(mmv):
+    q, kc, vc, table, lens = paged_case(12, [4], 2, 1, 64, 16, torch.float16)
+    ws = torch.empty(16 << 20, dtype=torch.uint8, device="cuda")
+    out, lse = mmv.paged_attention(q[:0], kc, vc, table[:0], lens[:0], workspace=ws)
+    assert out.shape == (0, 2, 64) and mmv.last_async_status(ws) == 0
+    out, lse = mmv.paged_attention(q, kc, vc, table[:, :0], lens * 0, workspace=ws)      # a table without columns
+    assert (out == 0).all() and (lse == -float("inf")).all() and mmv.last_async_status(ws) == 0
