@@ -492,6 +492,30 @@ mmv_status mmv_linear_attention_step(const mmv_linear_inputs *in, int64_t nreq, 
                                      void *out, void *cuda_stream);
 
 /*
+ * Linear attention over packed prompts: sequence s is the tokens
+ * [offsets[s], offsets[s + 1]) of q, k, v (MMV_SEG_OFFSETS_I32; empty sequences
+ * allowed), and for each head
+ *     S_t = exp(log_decay[h]) S_{t-1} + k_t v_t^T,   out_t = scale * q_t^T S_t
+ * in front of its first token S is state[s] (state NULL: zero) and behind its last
+ * one S is written to state_out[s] (if not NULL; an empty sequence's state is copied):
+ * [nseq, heads, dim_k, dim_v] fp32, 16-byte aligned, two buffers that do not
+ * overlap.  This is the segmented scan of Problem 2.1 with a decay between the
+ * elements, which here are the matrices k_t v_t^T, read out by q_t.
+ * Values are bfloat16 (MMV_BF16_TO_F32; another dtype answers MMV_ERR_INVALID_ARG): scores and
+ * states, which have no bound, are operands of the tensor core, and fp16's range
+ * does not hold them.  out: ntok x heads x dim_v; rows of tokens outside
+ * [offsets[0], offsets[nseq]) are not written.  log_decay: heads values, any
+ * <= 0, -infinity included.  Offsets that decrease or leave [0, ntok] are reported
+ * as MMV_ERR_BAD_SEGMENTS in the workspace; nothing outside the buffers is touched.
+ * ntok < 2^31, nseq < 2^20.  Workspace: mmv_linear_attention_workspace_bytes(in, nseq, ntok),
+ * 256-byte aligned.
+ */
+size_t mmv_linear_attention_workspace_bytes(const mmv_linear_inputs *in, int64_t nseq, int64_t ntok);
+mmv_status mmv_linear_attention(const mmv_linear_inputs *in, const int32_t *offsets, int64_t nseq, int64_t ntok,
+                                const float *log_decay, float scale, const float *state, float *state_out, void *out,
+                                void *workspace, size_t workspace_bytes, void *cuda_stream);
+
+/*
  * Test hook.  wait_budget_ns: time after which a device-side wait gives up
  * (<= 0 restores the default of 4 s).  skip_publish_span: index of one
  * 4096-element span of the scan that never publishes its carry, so that its

@@ -32,6 +32,7 @@ EXPORTS = (
     "mmv_debug_force_scan_shape", "mmv_mult_i8",
     "mmv_block_tables_workspace_bytes", "mmv_block_tables", "mmv_kv_append", "mmv_linear_attention_step",
     "mmv_paged_attention_workspace_bytes", "mmv_paged_attention",
+    "mmv_linear_attention_workspace_bytes", "mmv_linear_attention",
 )
 SHARD_SUMMARY_BYTES = 16
 STATIC_SCAN_MAX_N = 1 << 28
@@ -99,6 +100,10 @@ def _load() -> ctypes.CDLL:
     lib.mmv_paged_attention_workspace_bytes.argtypes = [ci, vp]
     lib.mmv_paged_attention.restype = ci
     lib.mmv_paged_attention.argtypes = [vp, i64, i64, ci, vp, vp, i64, i64, vp, i64, f32, i64, vp, vp, vp, sz, vp]
+    lib.mmv_linear_attention_workspace_bytes.restype = sz
+    lib.mmv_linear_attention_workspace_bytes.argtypes = [vp, i64, i64]
+    lib.mmv_linear_attention.restype = ci
+    lib.mmv_linear_attention.argtypes = [vp, vp, i64, i64, vp, f32, vp, vp, vp, vp, sz, vp]
     lib.mmv_linear_attention_step.restype = ci
     lib.mmv_linear_attention_step.argtypes = [vp, i64, vp, f32, vp, vp, vp, i64, vp, vp]
     lib.mmv_debug_force_scan_shape.restype = None
@@ -562,6 +567,53 @@ def _linear_struct(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor) -> bytes:
         raise ValueError("q [tokens, heads, dim_k], k [tokens, kv_heads, dim_k], v [tokens, kv_heads, dim_v] expected, heads a multiple of kv_heads")
     return _LINEAR_INPUTS.pack(q.data_ptr(), k.data_ptr(), v.data_ptr(), q.stride(0), q.stride(1), k.stride(0), k.stride(1), v.stride(0),
                                v.stride(1), q.size(1), k.size(1), q.size(2), v.size(2), _value_code(q))
+
+
+def linear_attention_workspace_bytes(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, sequences: int) -> int:
+    """mmv_linear_attention_workspace_bytes of a call with these inputs."""
+    return int(_lib.mmv_linear_attention_workspace_bytes(_linear_struct(q, k, v), int(sequences), q.size(0)))
+
+
+def linear_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, offsets: torch.Tensor, log_decay: torch.Tensor,
+                     scale: float = 1.0, state: torch.Tensor | None = None, out: torch.Tensor | None = None,
+                     state_out: torch.Tensor | None = None, workspace: torch.Tensor | None = None, stream=None):
+    """mmv_linear_attention: linear attention with a decay per head over packed sequences.
+
+    q [tokens, heads, dim_k], k, v [tokens, kv_heads, dim_k / dim_v], bfloat16 (views are fine); offsets int32
+    [sequences + 1]; log_decay fp32 [heads]; state fp32 [sequences, heads, dim_k, dim_v] in front of the first tokens (None:
+    zero).  Returns (out [tokens, heads, dim_v], state_out: the states behind the last tokens)."""
+    _on_device(q, k, v, offsets, log_decay, state, out, state_out, workspace)
+    inputs = _linear_struct(q, k, v)
+    tokens, heads, dk = q.shape
+    dv, nseq = v.size(2), offsets.numel() - 1
+    if nseq < 0:
+        raise ValueError("offsets holds one entry more than there are sequences")
+    _want(offsets, torch.int32, "offsets")
+    _want(log_decay, torch.float32, "log_decay")
+    _want(state, torch.float32, "state")
+    _want(state_out, torch.float32, "state_out")
+    _want(out, q.dtype, "out")
+    _shaped(log_decay, (heads,), "log_decay")
+    _shaped(state, (nseq, heads, dk, dv), "state")
+    _shaped(state_out, (nseq, heads, dk, dv), "state_out")
+    _shaped(out, (tokens, heads, dv), "out")
+    made = []
+    if out is None:
+        out = torch.empty(tokens, heads, dv, dtype=q.dtype, device=q.device)
+        made.append(out)
+    if state_out is None:
+        state_out = torch.empty(nseq, heads, dk, dv, dtype=torch.float32, device=q.device)
+        made.append(state_out)
+    if workspace is None:
+        nbytes = int(_lib.mmv_linear_attention_workspace_bytes(inputs, nseq, tokens))
+        workspace = torch.empty(max(nbytes, 256), dtype=torch.uint8, device=q.device)
+        made.append(workspace)
+    rc = _lib.mmv_linear_attention(inputs, offsets.data_ptr(), nseq, tokens, log_decay.data_ptr(), float(scale), _ptr(state),
+                                   state_out.data_ptr(), out.data_ptr(), workspace.data_ptr(), workspace.numel(), _stream_ptr(stream))
+    if rc != MMV_OK:
+        raise MmvError(rc, "mmv_linear_attention")
+    _kept(stream, *made)
+    return out, state_out
 
 
 def linear_attention_step(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, log_decay: torch.Tensor, state: torch.Tensor,

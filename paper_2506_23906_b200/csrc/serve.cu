@@ -346,4 +346,33 @@ mmv_status mmv_linear_attention_step(const mmv_linear_inputs* in, int64_t nreq, 
                 : launch(linear_step_kernel<false, 32>, grid, LIN_STEP_THREADS, 0, st, false, p);
 }
 
+size_t mmv_linear_attention_workspace_bytes(const mmv_linear_inputs* in, int64_t nseq, int64_t ntok) {
+    if (nseq < 0 || ntok < 0 || ntok > INT32_MAX || check_linear(in, ntok) != MMV_OK) return 0;
+    return sizeof(WorkspaceHeader);
+}
+
+mmv_status mmv_linear_attention(const mmv_linear_inputs* in, const int32_t* offsets, int64_t nseq, int64_t ntok, const float* log_decay,
+                                float scale, const float* state, float* state_out, void* out, void* workspace, size_t workspace_bytes,
+                                void* cuda_stream) {
+    if (nseq < 0 || nseq >= (1ll << 20) || ntok < 0 || ntok > INT32_MAX || check_linear(in, ntok) != MMV_OK || in->dtype != MMV_BF16_TO_F32)
+        return MMV_ERR_INVALID_ARG;
+    if (!workspace || !aligned(workspace, 256)) return MMV_ERR_INVALID_ARG;
+    if (nseq && (!offsets || !aligned(offsets, 4) || !log_decay || !aligned(log_decay, 4))) return MMV_ERR_INVALID_ARG;
+    if (ntok && (!in->q || !in->k || !in->v || !out || !aligned(out, 16))) return MMV_ERR_INVALID_ARG;
+    if ((state && !aligned(state, 16)) || (state_out && !aligned(state_out, 16))) return MMV_ERR_INVALID_ARG;
+    if (workspace_bytes < mmv_linear_attention_workspace_bytes(in, nseq, ntok)) return MMV_ERR_WORKSPACE_TOO_SMALL;
+    cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+    if (cudaMemsetAsync(workspace, 0, sizeof(WorkspaceHeader), st) != cudaSuccess) return MMV_ERR_CUDA;
+    if (nseq == 0) return MMV_OK;
+    LinParams p = linear_params(in, log_decay, scale, out);
+    p.state = state;
+    p.state_out = state_out;
+    p.offsets = offsets;
+    p.nseq = nseq;
+    p.ntok = ntok;
+    p.hdr = static_cast<WorkspaceHeader*>(workspace);
+    p.parts = (p.dv + 31) / 32;
+    return launch(linear_tokens_kernel<true>, dim3(static_cast<unsigned>(nseq * p.heads * p.parts)), LIN_TOKENS_THREADS, 0, st, false, p);
+}
+
 }  // extern "C"

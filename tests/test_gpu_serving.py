@@ -436,3 +436,130 @@ def test_paged_attention_without_requests(mmv):
     assert out.shape == (0, 2, 64) and mmv.last_async_status(ws) == 0
     out, lse = mmv.paged_attention(q, kc, vc, table[:, :0], lens * 0, workspace=ws)      # a table without columns
     assert (out == 0).all() and (lse == -float("inf")).all() and mmv.last_async_status(ws) == 0
+
+
+# ---------------------------------------------------------------------------------------------------------------------
+# linear attention over packed prompts
+# ---------------------------------------------------------------------------------------------------------------------
+def linear_plain(q, k, v, off, g, scale, state):
+    """The recurrence in 64 bits, token by token, and the same recurrence on magnitudes."""
+    t, heads, dk = q.shape
+    dv, rep, n = v.size(2), heads // k.size(1), len(off) - 1
+    q, k, v = q.double(), k.double().repeat_interleave(rep, 1), v.double().repeat_interleave(rep, 1)
+    fall = torch.exp(g.double())[:, None, None]
+    out, mag = torch.zeros(t, heads, dv, dtype=torch.float64, device="cuda"), torch.zeros(t, heads, dv, dtype=torch.float64, device="cuda")
+    last, size = [torch.zeros(n, heads, dk, dv, dtype=torch.float64, device="cuda") for _ in range(2)]
+    for s in range(n):
+        x = torch.zeros(heads, dk, dv, dtype=torch.float64, device="cuda") if state is None else state[s].double()
+        y = x.abs()
+        for i in range(off[s], off[s + 1]):
+            new = k[i][:, :, None] * v[i][:, None, :]
+            x = fall * x + new
+            y = fall * y + new.abs()
+            out[i] = scale * torch.einsum("hk,hkv->hv", q[i], x)
+            mag[i] = scale * torch.einsum("hk,hkv->hv", q[i].abs(), y)
+        last[s], size[s] = x, y
+    return out, mag, last, size
+
+
+def linear_case(seed, lens, heads, kv, dk, dv, state=True, first=0, behind=0):
+    gen = torch.Generator("cuda").manual_seed(seed)
+    off = [first]
+    for n in lens:
+        off.append(off[-1] + n)
+    t = off[-1] + behind
+    rand = lambda *s: torch.randn(*s, device="cuda", generator=gen)                                        # noqa: E731
+    qkv = rand(t, heads * dk + kv * (dk + dv)).bfloat16()
+    q = qkv[:, :heads * dk].view(t, heads, dk)
+    k = qkv[:, heads * dk:(heads + kv) * dk].view(t, kv, dk)
+    v = qkv[:, (heads + kv) * dk:].view(t, kv, dv)
+    g = torch.log1p(-torch.exp2(-torch.linspace(1, 11, heads, device="cuda")))
+    if heads > 2:
+        g[0], g[1] = 0.0, -float("inf")
+    if heads > 3:
+        g[2] = -60.0
+    return q, k, v, off, g, rand(len(lens), heads, dk, dv) if state else None
+
+
+def check_linear(mmv, case, scale=0.1, **more):
+    """Operands that are formed (scores, the state's copy, decayed keys) are held as sums of at least two bfloat16 values: 2^-16 relative for scores
+    and states, less for keys.  States: chains of fp32 sums over the tokens a decay reaches, each rounded or cut (<= 2 e), and decays whose
+    exponent and value are rounded (8 e): 2^-20 on the magnitudes covers 2^4 chunks' roundings of a unit each; results: 2^-14."""
+    q, k, v, off, g, state = case
+    t, heads, dk = q.shape
+    dv, n = v.size(2), len(off) - 1
+    guard = torch.full((t * heads * dv + 64,), 3.0, dtype=q.dtype, device="cuda")
+    out = guard[:t * heads * dv].view(t, heads, dv)
+    ws = torch.empty(max(256, mmv.linear_attention_workspace_bytes(q, k, v, n)), dtype=torch.uint8, device="cuda")
+    _, last = mmv.linear_attention(q, k, v, ints(off), g, scale=scale, state=state, out=out, workspace=ws, **more)
+    assert mmv.last_async_status(ws) == 0
+    assert (guard[t * heads * dv:] == 3.0).all() and (out[:off[0]] == 3.0).all() and (out[off[-1]:] == 3.0).all()
+    want, mag, wlast, size = linear_plain(q, k, v, off, g, scale, state)
+    rows = slice(off[0], off[-1])
+    inside(out[rows], want[rows], U[q.dtype] * want[rows].abs() + 2.0 ** -14 * mag[rows] + TINY[q.dtype])
+    inside(last, wlast, 2.0 ** -20 * size + 1e-37)
+    return out, last
+
+
+@pytest.mark.parametrize("heads,kv,dk,dv", [(1, 1, 8, 8), (4, 4, 64, 64), (6, 2, 128, 128), (5, 5, 40, 72), (3, 1, 128, 64), (4, 4, 96, 128), (2, 2, 16, 120)])
+@pytest.mark.parametrize("lens", [[1], [0, 1, 2, 0], [63, 64, 65], [127, 0, 128, 129, 1], [300, 5, 700]])
+@pytest.mark.parametrize("state", [False, True])
+def test_linear_attention(mmv, heads, kv, dk, dv, lens, state):
+    check_linear(mmv, linear_case(dk + dv + len(lens), lens, heads, kv, dk, dv, state))
+
+
+def test_linear_attention_rows_outside_the_sequences(mmv):
+    check_linear(mmv, linear_case(1, [70, 64, 3], 3, 3, 64, 64, first=37, behind=50))
+
+
+@pytest.mark.parametrize("lens,heads,dim", [([5000], 1, 128), ([3000, 1, 2500], 2, 64), ([1] * 150 + [900], 3, 128), ([4100, 64, 128, 3000], 4, 128)])
+def test_linear_attention_split(mmv, lens, heads, dim):
+    """Long sequences of few heads are cut over the CTAs; many short ones share one."""
+    check_linear(mmv, linear_case(sum(lens), lens, heads, heads, dim, dim))
+
+
+def test_linear_attention_neighbours_that_are_not_finite(mmv):
+    """Sequences share chunks of memory, not values: NaN and infinities of one stay out of the next and out of the rows in front."""
+    q, k, v, off, g, state = linear_case(2, [40, 70, 200], 4, 4, 64, 64)
+    want, last = mmv.linear_attention(q, k, v, ints(off), g, state=state)
+    q2, k2, v2 = q.clone(), k.clone(), v.clone()
+    for x in (q2, k2, v2):
+        x[40:110] = float("nan")
+    v2[60] = float("inf")
+    out, last2 = mmv.linear_attention(q2, k2, v2, ints(off), g, state=state)
+    assert torch.equal(out[:40], want[:40]) and torch.equal(out[110:], want[110:]) and torch.equal(last2[[0, 2]], last[[0, 2]])
+    assert torch.isnan(out[40:110]).all() and torch.isnan(last2[1]).all()
+
+
+def test_linear_attention_step_continues_a_prompt(mmv):
+    """The prompt form's state, taken on by single tokens, is the longer prompt's."""
+    q, k, v, off, g, state = linear_case(4, [65, 66], 4, 2, 64, 128)
+    want, mag, wlast, size = linear_plain(q, k, v, off, g, 0.2, state)
+    pick = torch.cat([torch.arange(0, 64), torch.arange(65, 129)])
+    out, s = mmv.linear_attention(q[pick].contiguous(), k[pick].contiguous(), v[pick].contiguous(), ints([0, 64, 128]), g, scale=0.2, state=state)
+    at = torch.tensor([64, 129], device="cuda")
+    o = mmv.linear_attention_step(q[at].contiguous(), k[at].contiguous(), v[at].contiguous(), g, s, scale=0.2)
+    inside(o, want[at], U[torch.bfloat16] * want[at].abs() + 2.0 ** -14 * mag[at])
+    o2 = mmv.linear_attention_step(q[130:131], k[130:131], v[130:131], g, s, scale=0.2, slots=ints([1]))
+    inside(o2, want[130:131], U[torch.bfloat16] * want[130:131].abs() + 2.0 ** -14 * mag[130:131])
+    inside(s[1], wlast[1], 2.0 ** -20 * size[1])
+
+
+def test_linear_attention_bad_offsets_are_reported(mmv):
+    q, k, v, off, g, state = linear_case(7, [64, 64, 64], 2, 2, 64, 64)
+    ws = torch.empty(max(256, mmv.linear_attention_workspace_bytes(q, k, v, 3)), dtype=torch.uint8, device="cuda")
+    for bad in ([0, 100, 64, 192], [-3, 64, 128, 192], [0, 64, 128, 193], [0, 2 ** 31 - 1, 128, 192]):
+        mmv.linear_attention(q, k, v, ints(bad), g, state=state, workspace=ws)
+        assert mmv.last_async_status(ws) == 4
+    mmv.linear_attention(q, k, v, ints(off), g, state=state, workspace=ws)
+    assert mmv.last_async_status(ws) == 0
+
+
+def test_linear_attention_nothing(mmv):
+    q, k, v, off, g, state = linear_case(8, [4], 2, 2, 64, 64)
+    out, last = mmv.linear_attention(q[:0], k[:0], v[:0], ints([0, 0]), g, state=state)
+    assert out.shape == (0, 2, 64) and torch.equal(last, state)
+    out, last = mmv.linear_attention(q[:0], k[:0], v[:0], ints([0, 0, 0]), g)
+    assert (last == 0).all()
+    out, last = mmv.linear_attention(q[:0], k[:0], v[:0], ints([0]), g)
+    assert last.shape == (0, 2, 64, 64)
