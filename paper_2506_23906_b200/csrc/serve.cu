@@ -51,6 +51,10 @@ ServeDevice* serve_device() {
     ok &= allow_smem(paged_attention_kernel<true, 128>, PagedCfg<128>::smem_bytes(PA_ROWS));
     ok &= allow_smem(paged_attention_kernel<false, 256>, PagedCfg<256>::smem_bytes(PA_ROWS));
     ok &= allow_smem(paged_attention_kernel<true, 256>, PagedCfg<256>::smem_bytes(PA_ROWS));
+    ok &= allow_smem(linear_chunks_kernel<64, true>, LinCfg<64, true>::kSmemBytes);
+    ok &= allow_smem(linear_chunks_kernel<64, false>, LinCfg<64, false>::kSmemBytes);
+    ok &= allow_smem(linear_chunks_kernel<128, true>, LinCfg<128, true>::kSmemBytes);
+    ok &= allow_smem(linear_chunks_kernel<128, false>, LinCfg<128, false>::kSmemBytes);
     if (!ok) {
         cudaGetLastError();
         return nullptr;
@@ -163,6 +167,45 @@ mmv_status launch_paged(const PagedParams& p, int ctas, cudaStream_t st) {
                                  static_cast<size_t>(PagedCfg<DP>::smem_bytes(p.rows)), st, false, p);
     if (rc != MMV_OK) return rc;
     return launch(paged_join_kernel<BF16>, dim3(static_cast<unsigned>(ctas), static_cast<unsigned>(p.rows)), PA_JOIN_THREADS, 0, st, true, p, ctas);
+}
+
+// One CTA per SM, fewer where there is less than LIN_MIN_UNITS chunks for each (the chunks' upper bound: every sequence ends in a short one).
+constexpr int kLinearMaxSms = 160;
+int linear_ctas(const mmv_linear_inputs* in, int64_t nseq, int64_t ntok, int sms) {
+    const int64_t units = (ntok / LIN_C + nseq) * in->heads;
+    int64_t ctas = units / LIN_MIN_UNITS;
+    if (ctas > sms) ctas = sms;
+    if (ctas > kLinearMaxSms) ctas = kLinearMaxSms;
+    return ctas < 1 ? 1 : static_cast<int>(ctas);
+}
+
+struct LinearMaps {
+    CUtensorMap q, k, v;
+};
+// [token][head][column] as boxes of 64 columns of one head of 64 tokens; what lies outside reads as zero.
+bool linear_map(CUtensorMap* map, const void* x, int dim, int heads, int64_t ntok, int64_t stride_head, int64_t stride_token) {
+    EncodeTiledFn enc = get_encode();
+    if (!enc) return false;
+    if (ntok == 0) {                                                  // never read
+        *map = CUtensorMap{};
+        return true;
+    }
+    const cuuint64_t row = static_cast<cuuint64_t>(dim) * 2;
+    const cuuint64_t dims[3] = {static_cast<cuuint64_t>(dim), static_cast<cuuint64_t>(heads), static_cast<cuuint64_t>(ntok)};
+    const cuuint64_t strides[2] = {heads > 1 ? static_cast<cuuint64_t>(stride_head) * 2 : row,
+                                   ntok > 1 ? static_cast<cuuint64_t>(stride_token) * 2 : row * static_cast<cuuint64_t>(heads)};
+    const cuuint32_t box[3] = {64, 1, LIN_C}, estr[3] = {1, 1, 1};
+    return enc(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(x), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+               CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <int DK>
+mmv_status launch_linear(const LinearMaps& m, const LinParams& p, int ctas, cudaStream_t st) {
+    const mmv_status rc = launch(linear_chunks_kernel<DK, true>, dim3(static_cast<unsigned>(ctas)), LIN_THREADS, LinCfg<DK, true>::kSmemBytes,
+                                 st, false, m.q, m.k, m.v, p);
+    if (rc != MMV_OK) return rc;
+    return launch(linear_chunks_kernel<DK, false>, dim3(static_cast<unsigned>(ctas)), LIN_THREADS, LinCfg<DK, false>::kSmemBytes, st, true,
+                  m.q, m.k, m.v, p);
 }
 
 }  // namespace
@@ -348,7 +391,7 @@ mmv_status mmv_linear_attention_step(const mmv_linear_inputs* in, int64_t nreq, 
 
 size_t mmv_linear_attention_workspace_bytes(const mmv_linear_inputs* in, int64_t nseq, int64_t ntok) {
     if (nseq < 0 || ntok < 0 || ntok > INT32_MAX || check_linear(in, ntok) != MMV_OK) return 0;
-    return sizeof(WorkspaceHeader);
+    return sizeof(WorkspaceHeader) + static_cast<size_t>(linear_ctas(in, nseq, ntok, kLinearMaxSms)) * (in->dim_k <= 64 ? 64 : 128) * 128 * sizeof(float);
 }
 
 mmv_status mmv_linear_attention(const mmv_linear_inputs* in, const int32_t* offsets, int64_t nseq, int64_t ntok, const float* log_decay,
@@ -362,8 +405,9 @@ mmv_status mmv_linear_attention(const mmv_linear_inputs* in, const int32_t* offs
     if ((state && !aligned(state, 16)) || (state_out && !aligned(state_out, 16))) return MMV_ERR_INVALID_ARG;
     if (workspace_bytes < mmv_linear_attention_workspace_bytes(in, nseq, ntok)) return MMV_ERR_WORKSPACE_TOO_SMALL;
     cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
-    if (cudaMemsetAsync(workspace, 0, sizeof(WorkspaceHeader), st) != cudaSuccess) return MMV_ERR_CUDA;
-    if (nseq == 0) return MMV_OK;
+    if (nseq == 0) return cudaMemsetAsync(workspace, 0, sizeof(WorkspaceHeader), st) == cudaSuccess ? MMV_OK : MMV_ERR_CUDA;
+    ServeDevice* dev = serve_device();
+    if (!dev) return MMV_ERR_CUDA;
     LinParams p = linear_params(in, log_decay, scale, out);
     p.state = state;
     p.state_out = state_out;
@@ -371,8 +415,15 @@ mmv_status mmv_linear_attention(const mmv_linear_inputs* in, const int32_t* offs
     p.nseq = nseq;
     p.ntok = ntok;
     p.hdr = static_cast<WorkspaceHeader*>(workspace);
-    p.parts = (p.dv + 31) / 32;
-    return launch(linear_tokens_kernel<true>, dim3(static_cast<unsigned>(nseq * p.heads * p.parts)), LIN_TOKENS_THREADS, 0, st, false, p);
+    p.carry = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + sizeof(WorkspaceHeader));
+    p.budget_ns = g_budget_ns.load();
+    LinearMaps maps;
+    if (!linear_map(&maps.q, in->q, in->dim_k, in->heads, ntok, in->q_stride_head, in->q_stride_token) ||
+        !linear_map(&maps.k, in->k, in->dim_k, in->kv_heads, ntok, in->k_stride_head, in->k_stride_token) ||
+        !linear_map(&maps.v, in->v, in->dim_v, in->kv_heads, ntok, in->v_stride_head, in->v_stride_token))
+        return MMV_ERR_INVALID_ARG;
+    const int ctas = linear_ctas(in, nseq, ntok, dev->sm_count);
+    return in->dim_k <= 64 ? launch_linear<64>(maps, p, ctas, st) : launch_linear<128>(maps, p, ctas, st);
 }
 
 }  // extern "C"
