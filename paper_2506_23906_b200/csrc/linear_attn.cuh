@@ -750,8 +750,30 @@ linear_chunks_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
             const uint32_t sm = smem_u32(smem);
             // (a descriptor's low word is an address in units of 16 bytes: 2 per step of 16 values along a row, 128 per 16 rows)
             constexpr uint32_t kBox = LIN_BOX >> 4;
+            const auto update = [&](int kv) {                // KV = V^T K', half a chunk
+                tc_fence_after_sync();
+                const int stage = (kv >> 1) % C::kStages, h = kv & 1;
+                const uint64_t dv = lin_desc_mn(sm + stage * C::kStage + C::kV + h * (LIN_BOX / 2), LIN_BOX);
+                uint64_t dk = lin_desc_mn(sm + C::kKp + h * C::kKpBytes, LIN_BOX / 2);
+#pragma unroll 1
+                for (int x = 0; x < 3; ++x, dk += C::kKpPart >> 4)
+#pragma unroll
+                    for (int k = 0; k < 2; ++k) mma_f16_ss(tmem + C::kColKV, dv + 128 * k, dk + 128 * k, kIdescKV, h > 0 || x > 0 || k > 0);
+                tc_commit(&bars.kv_done[h]);
+                if (h) {
+                    tc_commit(&bars.kv_full);
+                    tc_commit(&bars.empty[stage]);
+                }
+            };
+            if constexpr (CARRY) {
+                for (int kv = 0; ok && kv < 2 * count; ++kv) {
+                    ok = lin_wait_one(&bars.kp_full[kv & 1], (kv >> 1) & 1, abort_flag, budget);
+                    if (ok && !(kv & 1)) ok = lin_wait_one(&bars.kv_empty, (kv >> 1) & 1, abort_flag, budget);
+                    if (ok) update(kv);
+                }
+            }
             // Each of the four products goes out when its operands are there, whichever chunk it belongs to: the numbers of the next ones.
-            int at = CARRY ? count : 0, kv = 0, o1 = CARRY ? count : 0, o2 = CARRY ? count : 0;
+            int at = CARRY ? count : 0, kv = CARRY ? 2 * count : 0, o1 = CARRY ? count : 0, o2 = CARRY ? count : 0;
             uint64_t since = global_timer_ns();
             uint32_t polls = 0;
             while (at < count || kv < 2 * count || o1 < count || o2 < count) {
@@ -769,22 +791,8 @@ linear_chunks_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
                     tc_commit(&bars.at_full[at & 1]);
                     ++at;
                 }
-                if (kv < 2 * count && mbar_try_wait(&bars.kp_full[kv & 1], (kv >> 1) & 1) && ((kv & 1) || mbar_try_wait(&bars.kv_empty, (kv >> 1) & 1))) {
-                    tc_fence_after_sync();
-                    const int stage = (kv >> 1) % C::kStages, h = kv & 1;                  // (half a chunk at a time)
-                    const uint64_t dv = lin_desc_mn(sm + stage * C::kStage + C::kV + h * (LIN_BOX / 2), LIN_BOX);
-                    uint64_t dk = lin_desc_mn(sm + C::kKp + h * C::kKpBytes, LIN_BOX / 2);
-#pragma unroll 1
-                    for (int x = 0; x < 3; ++x, dk += C::kKpPart >> 4)                     // KV = V^T K'
-#pragma unroll
-                        for (int k = 0; k < 2; ++k) mma_f16_ss(tmem + C::kColKV, dv + 128 * k, dk + 128 * k, kIdescKV, h > 0 || x > 0 || k > 0);
-                    tc_commit(&bars.kv_done[h]);
-                    if (h) {
-                        tc_commit(&bars.kv_full);
-                        tc_commit(&bars.empty[stage]);
-                    }
-                    ++kv;
-                }
+                if (kv < 2 * count && mbar_try_wait(&bars.kp_full[kv & 1], (kv >> 1) & 1) && ((kv & 1) || mbar_try_wait(&bars.kv_empty, (kv >> 1) & 1)))
+                    update(kv++);
                 if (o1 < at && o1 < count && mbar_try_wait(&bars.s_full, o1 & 1) && (o1 == 0 || mbar_try_wait(&bars.o_empty, (o1 - 1) & 1))) {
                     tc_fence_after_sync();
                     const uint32_t st = sm + (o1 % C::kStages) * C::kStage;
