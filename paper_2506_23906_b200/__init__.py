@@ -1,15 +1,15 @@
 """Python binding of libmmv.so, the C-ABI CUDA library for segmented scan,
 segmented sum and CSR SpMV on B200 (sm_100a).
 
-The binding only marshals arguments: torch supplies device memory and the
-current CUDA stream, every step of the computation runs in the library's own
+The binding only marshals arguments (ctypes, and an extension for the serving
+operators): torch supplies device memory and the current CUDA stream, every step of the computation runs in the library's own
 kernels.  There is no CPU or PyTorch fallback: if the shared library is missing
 the import of this module fails.
 """
 from __future__ import annotations
 
 import ctypes
-import struct
+import importlib.util
 from pathlib import Path
 
 import torch
@@ -89,23 +89,6 @@ def _load() -> ctypes.CDLL:
     lib.mmv_seg_scan_shard_finish.argtypes = [vp, ci, ci, vp, i64, ci, vp]
     lib.mmv_mult_i8.restype = ci
     lib.mmv_mult_i8.argtypes = [vp, vp, i64, vp, vp, sz, vp]
-    f32 = ctypes.c_float
-    lib.mmv_block_tables_workspace_bytes.restype = sz
-    lib.mmv_block_tables_workspace_bytes.argtypes = [i64]
-    lib.mmv_block_tables.restype = ci
-    lib.mmv_block_tables.argtypes = [vp, vp, i64, ci, vp, i64, vp, i64, i64, vp, vp, vp, i64, vp, vp, sz, vp]
-    lib.mmv_kv_append.restype = ci
-    lib.mmv_kv_append.argtypes = [vp, i64, i64, vp, i64, i64, vp, i64, vp, vp]
-    lib.mmv_paged_attention_workspace_bytes.restype = sz
-    lib.mmv_paged_attention_workspace_bytes.argtypes = [ci, vp]
-    lib.mmv_paged_attention.restype = ci
-    lib.mmv_paged_attention.argtypes = [vp, i64, i64, ci, vp, vp, i64, i64, vp, i64, f32, i64, vp, vp, vp, sz, vp]
-    lib.mmv_linear_attention_workspace_bytes.restype = sz
-    lib.mmv_linear_attention_workspace_bytes.argtypes = [vp, i64, i64]
-    lib.mmv_linear_attention.restype = ci
-    lib.mmv_linear_attention.argtypes = [vp, vp, i64, i64, vp, f32, vp, vp, vp, vp, sz, vp]
-    lib.mmv_linear_attention_step.restype = ci
-    lib.mmv_linear_attention_step.argtypes = [vp, i64, vp, f32, vp, vp, vp, i64, vp, vp]
     lib.mmv_debug_force_scan_shape.restype = None
     lib.mmv_debug_force_scan_shape.argtypes = [ci]
     lib.mmv_debug_force_sum_groups.restype = None
@@ -398,61 +381,32 @@ def spmv_csr(rowptr: torch.Tensor, col: torch.Tensor, val: torch.Tensor, x: torc
 
 # ---------------------------------------------------------------------------
 # Serving a language model over a ragged batch
+#
+# These calls take a few microseconds on the GPU in a decoding step; their tensors' metadata is read and checked by a
+# small extension (csrc/torch_binding.cpp), which also allocates what is not handed in.
 # ---------------------------------------------------------------------------
-# the argument structs of include/mmv.h, packed in one call (field by field assignment of a ctypes structure takes longer
-# than a small kernel)
-_KV_CACHE = struct.Struct("PPqqqqiiii")              # mmv_kv_cache
-_LINEAR_INPUTS = struct.Struct("PPPqqqqqqiiiiixxxx")   # mmv_linear_inputs
+def _load_serve():
+    path = _PKG / "_serve.so"
+    if not path.exists():
+        raise ImportError(f"{path} is missing: build it with `python paper_2506_23906_b200/build.py`.  There is no fallback path.")
+    spec = importlib.util.spec_from_file_location(__name__ + "._serve", path)
+    mod = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(mod)
+    mod.set_error(MmvError)
+    return mod
 
 
-def _on_device(first: torch.Tensor, *others) -> int:
-    """All tensors on the current CUDA device (the library launches there)."""
-    dev = torch.cuda.current_device()
-    for t in (first, *others):
-        if t is not None and t.get_device() != dev:
-            raise ValueError("tensors must be on the current CUDA device")
-    return dev
+_serve = _load_serve()
 
 
-def _value_code(x: torch.Tensor) -> int:
-    if x.dtype == torch.bfloat16:
-        return BF16_TO_F32
-    if x.dtype == torch.float16:
-        return F16_TO_F32
-    raise TypeError("values must be torch.float16 or torch.bfloat16")
-
-
-def _want(t, dtype, what: str):
-    if t is not None and (t.dtype != dtype or not t.is_contiguous()):
-        raise TypeError(f"{what} must be contiguous {dtype}")
-
-
-def _shaped(t, shape, what: str):
-    if t is not None and t.shape != shape:
-        raise ValueError(f"{what} must have shape {tuple(shape)}")
-
-
-def _rows(t, what: str):
-    if t.dim() != 3 or t.stride(2) != 1 and t.size(2) > 1:
-        raise ValueError(f"{what} must have three axes, the last contiguous")
-
-
-def _kept(stream, *made):
-    """Buffers made by a call for a stream other than the current one stay allocated until that stream is done with them."""
-    if stream is not None:
-        for t in made:
-            if t is not None:
-                t.record_stream(stream)
-
-
-def _cache_struct(k_cache: torch.Tensor, v_cache: torch.Tensor) -> bytes:
-    if k_cache.dim() != 4 or k_cache.shape != v_cache.shape or k_cache.stride() != v_cache.stride() or k_cache.dtype != v_cache.dtype:
-        raise ValueError("k_cache and v_cache must be alike: [blocks, block_size, heads, dim]")
-    blocks, block, heads, dim = k_cache.shape
-    sb, st, sh, sd = k_cache.stride()
-    if sd != 1 and dim > 1:
-        raise ValueError("the caches' last axis must be contiguous")
-    return _KV_CACHE.pack(k_cache.data_ptr(), v_cache.data_ptr(), blocks, sb, st, sh, block, heads, dim, _value_code(k_cache))
+def _on_stream(call, stream, inputs, args):
+    """A call on a stream other than the current one: what it allocates (and is handed) stays until that stream is done with it."""
+    with torch.cuda.stream(stream):
+        made = call(*args, None)
+    for t in inputs:
+        if t is not None:
+            t.record_stream(stream)
+    return made
 
 
 def block_tables(past: torch.Tensor, added: torch.Tensor, free_blocks: torch.Tensor, table: torch.Tensor, slots: torch.Tensor,
@@ -463,56 +417,23 @@ def block_tables(past: torch.Tensor, added: torch.Tensor, free_blocks: torch.Ten
     past, added: int32 [nreq]; free_blocks: int32; table: int32 [nreq, max_blocks] (rows may be strided), completed in
     place; slots: int64, written whole (-1 behind the last token).  Returns (offsets int32 [nreq + 1], total int32 [nreq],
     used int32 [1]: how many of free_blocks were taken)."""
-    _on_device(past, added, free_blocks, table, slots, offsets, total, used, workspace)
-    n = past.numel()
-    for t, what in ((past, "past"), (added, "added"), (free_blocks, "free_blocks"), (offsets, "offsets"), (total, "total"), (used, "used")):
-        _want(t, torch.int32, what)
-    _want(slots, torch.int64, "slots")
-    if table.dtype != torch.int32 or table.dim() != 2 or table.size(0) != n or (table.stride(1) != 1 and table.size(1) > 1):
-        raise TypeError("table must be int32 [requests, max_blocks], its rows contiguous")
-    if added.numel() != n:
-        raise ValueError("past and added must have one entry per request")
-    made = []
-    if offsets is None:
-        offsets = torch.empty(n + 1, dtype=torch.int32, device=past.device)
-        made.append(offsets)
-    if total is None:
-        total = torch.empty(n, dtype=torch.int32, device=past.device)
-        made.append(total)
-    if used is None:
-        used = torch.empty(1, dtype=torch.int32, device=past.device)
-        made.append(used)
-    if offsets.numel() < n + 1 or total.numel() < n or used.numel() < 1:
-        raise ValueError("offsets, total and used hold nreq + 1, nreq and 1 entries")
-    if workspace is None:
-        workspace = torch.empty(max(256, int(_lib.mmv_block_tables_workspace_bytes(n))), dtype=torch.uint8, device=past.device)
-        made.append(workspace)
-    rc = _lib.mmv_block_tables(past.data_ptr(), added.data_ptr(), n, int(block_size), free_blocks.data_ptr(), free_blocks.numel(),
-                               table.data_ptr(), table.stride(0), table.size(1), offsets.data_ptr(), total.data_ptr(),
-                               slots.data_ptr(), slots.numel(), used.data_ptr(), workspace.data_ptr(), workspace.numel(),
-                               _stream_ptr(stream))
-    if rc != MMV_OK:
-        raise MmvError(rc, "mmv_block_tables")
-    _kept(stream, *made)
-    return offsets, total, used
+    args = (past, added, free_blocks, table, slots, block_size, offsets, total, used, workspace)
+    if stream is not None:
+        return _on_stream(_serve.block_tables, stream, (past, added, free_blocks, table, slots, offsets, total, used, workspace), args)
+    return _serve.block_tables(*args, None)
 
 
 def kv_append(k: torch.Tensor, v: torch.Tensor, slots: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor, stream=None) -> None:
     """mmv_kv_append: writes the keys and values k, v [tokens, heads, dim] of a packed batch (views are fine) to their slots
-    (int64; negative: skipped) of the paged caches [blocks, block_size, heads, dim]."""
-    _on_device(k, v, slots, k_cache, v_cache)
-    _rows(k, "k")
-    _rows(v, "v")
-    _want(slots, torch.int64, "slots")
-    cache = _cache_struct(k_cache, v_cache)
-    if k.dtype != k_cache.dtype or v.dtype != k_cache.dtype:
-        raise TypeError("keys, values and caches must have one type")
-    if k.shape != v.shape or k.shape[1:] != k_cache.shape[2:] or slots.numel() != k.size(0):
-        raise ValueError("k, v must be [tokens, heads, dim] like the caches, with one slot per token")
-    rc = _lib.mmv_kv_append(k.data_ptr(), k.stride(0), k.stride(1), v.data_ptr(), v.stride(0), v.stride(1), slots.data_ptr(),
-                            slots.numel(), cache, _stream_ptr(stream))
-    if rc != MMV_OK:
-        raise MmvError(rc, "mmv_kv_append")
+    (int64; negative: skipped) of the paged caches [blocks, block_size, heads, dim] (any order in memory, rows contiguous)."""
+    if stream is not None:
+        return _on_stream(_serve.kv_append, stream, (k, v, slots, k_cache, v_cache), (k, v, slots, k_cache, v_cache))
+    return _serve.kv_append(k, v, slots, k_cache, v_cache, None)
+
+
+def paged_attention_workspace_bytes(heads: int, k_cache: torch.Tensor, v_cache: torch.Tensor) -> int:
+    """mmv_paged_attention_workspace_bytes of a call with `heads` query heads over these caches."""
+    return _serve.paged_attention_workspace_bytes(heads, k_cache, v_cache)
 
 
 def paged_attention(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor, table: torch.Tensor, lens: torch.Tensor,
@@ -522,56 +443,15 @@ def paged_attention(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tenso
     [blocks, block_size, kv_heads, dim] through table int32 [requests, max_blocks] (rows may be strided) and lens int32
     [requests].  scale None: dim ** -0.5; window > 0: the last `window` tokens only.  Returns (out [requests, heads, dim],
     lse fp32 [requests, heads])."""
-    _on_device(q, k_cache, v_cache, table, lens, out, lse, workspace)
-    _rows(q, "q")
-    n, heads, dim = q.shape
-    cache = _cache_struct(k_cache, v_cache)
-    _want(lens, torch.int32, "lens")
-    _want(out, q.dtype, "out")
-    _want(lse, torch.float32, "lse")
-    _shaped(lens, (n,), "lens")
-    _shaped(out, q.shape, "out")
-    _shaped(lse, (n, heads), "lse")
-    if table.dtype != torch.int32 or table.dim() != 2 or table.size(0) != n or (table.stride(1) != 1 and table.size(1) > 1):
-        raise TypeError("table must be int32 [requests, max_blocks], its rows contiguous")
-    if q.dtype != k_cache.dtype:
-        raise TypeError("queries and caches must have one type")
-    if dim != k_cache.size(3) or heads % k_cache.size(2):
-        raise ValueError("q must be [requests, heads, dim] with the caches' dim and a multiple of their heads")
-    made = []
-    if out is None:
-        out = torch.empty(n, heads, dim, dtype=q.dtype, device=q.device)
-        made.append(out)
-    if lse is None:
-        lse = torch.empty(n, heads, dtype=torch.float32, device=q.device)
-        made.append(lse)
-    if workspace is None:
-        nbytes = int(_lib.mmv_paged_attention_workspace_bytes(heads, cache))
-        workspace = torch.empty(max(nbytes, 256), dtype=torch.uint8, device=q.device)
-        made.append(workspace)
-    rc = _lib.mmv_paged_attention(q.data_ptr(), q.stride(0), q.stride(1), heads, cache, table.data_ptr(), table.stride(0), table.size(1),
-                                  lens.data_ptr(), n, dim ** -0.5 if scale is None else float(scale), int(window), out.data_ptr(),
-                                  lse.data_ptr(), workspace.data_ptr(), workspace.numel(), _stream_ptr(stream))
-    if rc != MMV_OK:
-        raise MmvError(rc, "mmv_paged_attention")
-    _kept(stream, *made)
-    return out, lse
-
-
-def _linear_struct(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor) -> bytes:
-    for t, what in ((q, "q"), (k, "k"), (v, "v")):
-        _rows(t, what)
-    if q.dtype != k.dtype or q.dtype != v.dtype:
-        raise TypeError("q, k and v must have one type")
-    if k.shape[:2] != v.shape[:2] or q.size(0) != k.size(0) or q.size(2) != k.size(2) or q.size(1) % k.size(1):
-        raise ValueError("q [tokens, heads, dim_k], k [tokens, kv_heads, dim_k], v [tokens, kv_heads, dim_v] expected, heads a multiple of kv_heads")
-    return _LINEAR_INPUTS.pack(q.data_ptr(), k.data_ptr(), v.data_ptr(), q.stride(0), q.stride(1), k.stride(0), k.stride(1), v.stride(0),
-                               v.stride(1), q.size(1), k.size(1), q.size(2), v.size(2), _value_code(q))
+    args = (q, k_cache, v_cache, table, lens, scale, window, out, lse, workspace)
+    if stream is not None:
+        return _on_stream(_serve.paged_attention, stream, (q, k_cache, v_cache, table, lens, out, lse, workspace), args)
+    return _serve.paged_attention(*args, None)
 
 
 def linear_attention_workspace_bytes(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, sequences: int) -> int:
     """mmv_linear_attention_workspace_bytes of a call with these inputs."""
-    return int(_lib.mmv_linear_attention_workspace_bytes(_linear_struct(q, k, v), int(sequences), q.size(0)))
+    return _serve.linear_attention_workspace_bytes(q, k, v, sequences)
 
 
 def linear_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, offsets: torch.Tensor, log_decay: torch.Tensor,
@@ -582,38 +462,10 @@ def linear_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, offsets:
     q [tokens, heads, dim_k], k, v [tokens, kv_heads, dim_k / dim_v], bfloat16 (views are fine); offsets int32
     [sequences + 1]; log_decay fp32 [heads]; state fp32 [sequences, heads, dim_k, dim_v] in front of the first tokens (None:
     zero).  Returns (out [tokens, heads, dim_v], state_out: the states behind the last tokens)."""
-    _on_device(q, k, v, offsets, log_decay, state, out, state_out, workspace)
-    inputs = _linear_struct(q, k, v)
-    tokens, heads, dk = q.shape
-    dv, nseq = v.size(2), offsets.numel() - 1
-    if nseq < 0:
-        raise ValueError("offsets holds one entry more than there are sequences")
-    _want(offsets, torch.int32, "offsets")
-    _want(log_decay, torch.float32, "log_decay")
-    _want(state, torch.float32, "state")
-    _want(state_out, torch.float32, "state_out")
-    _want(out, q.dtype, "out")
-    _shaped(log_decay, (heads,), "log_decay")
-    _shaped(state, (nseq, heads, dk, dv), "state")
-    _shaped(state_out, (nseq, heads, dk, dv), "state_out")
-    _shaped(out, (tokens, heads, dv), "out")
-    made = []
-    if out is None:
-        out = torch.empty(tokens, heads, dv, dtype=q.dtype, device=q.device)
-        made.append(out)
-    if state_out is None:
-        state_out = torch.empty(nseq, heads, dk, dv, dtype=torch.float32, device=q.device)
-        made.append(state_out)
-    if workspace is None:
-        nbytes = int(_lib.mmv_linear_attention_workspace_bytes(inputs, nseq, tokens))
-        workspace = torch.empty(max(nbytes, 256), dtype=torch.uint8, device=q.device)
-        made.append(workspace)
-    rc = _lib.mmv_linear_attention(inputs, offsets.data_ptr(), nseq, tokens, log_decay.data_ptr(), float(scale), _ptr(state),
-                                   state_out.data_ptr(), out.data_ptr(), workspace.data_ptr(), workspace.numel(), _stream_ptr(stream))
-    if rc != MMV_OK:
-        raise MmvError(rc, "mmv_linear_attention")
-    _kept(stream, *made)
-    return out, state_out
+    args = (q, k, v, offsets, log_decay, scale, state, out, state_out, workspace)
+    if stream is not None:
+        return _on_stream(_serve.linear_attention, stream, (q, k, v, offsets, log_decay, state, out, state_out, workspace), args)
+    return _serve.linear_attention(*args, None)
 
 
 def linear_attention_step(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, log_decay: torch.Tensor, state: torch.Tensor,
@@ -624,26 +476,7 @@ def linear_attention_step(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, log
     q [requests, heads, dim_k], k, v [requests, kv_heads, dim_k / dim_v]; log_decay fp32 [heads]; state fp32
     [states, heads, dim_k, dim_v], request r's at slots[r] (int32; None: at r), updated in place unless state_out is given.
     Returns out [requests, heads, dim_v]."""
-    state_out = state if state_out is None else state_out
-    _on_device(q, k, v, log_decay, state, slots, state_out, out)
-    inputs = _linear_struct(q, k, v)
-    n, heads, dv = q.size(0), q.size(1), v.size(2)
-    _want(log_decay, torch.float32, "log_decay")
-    _want(state, torch.float32, "state")
-    _want(state_out, torch.float32, "state_out")
-    _want(slots, torch.int32, "slots")
-    _want(out, q.dtype, "out")
-    _shaped(log_decay, (heads,), "log_decay")
-    _shaped(state, (state.size(0), heads, q.size(2), dv), "state")
-    _shaped(state_out, state.shape, "state_out")
-    _shaped(slots, (n,), "slots")
-    _shaped(out, (n, heads, dv), "out")
-    made = None
-    if out is None:
-        made = out = torch.empty(n, heads, dv, dtype=q.dtype, device=q.device)
-    rc = _lib.mmv_linear_attention_step(inputs, n, log_decay.data_ptr(), float(scale), state.data_ptr(), state_out.data_ptr(),
-                                        _ptr(slots), state.size(0), out.data_ptr(), _stream_ptr(stream))
-    if rc != MMV_OK:
-        raise MmvError(rc, "mmv_linear_attention_step")
-    _kept(stream, made)
-    return out
+    args = (q, k, v, log_decay, state, scale, slots, state_out, out)
+    if stream is not None:
+        return _on_stream(_serve.linear_attention_step, stream, (q, k, v, log_decay, state, slots, state_out, out), args)
+    return _serve.linear_attention_step(*args, None)

@@ -1,4 +1,4 @@
-"""Builds libmmv.so (the C-ABI CUDA library) in-tree with nvcc for sm_100a."""
+"""Builds libmmv.so (the C-ABI CUDA library, nvcc for sm_100a) and _serve.so (its binding to torch tensors) in-tree."""
 from __future__ import annotations
 
 import os
@@ -11,11 +11,13 @@ CSRC = PKG / "csrc"
 LIB = PKG / "libmmv.so"
 OBJ = PKG / "build"
 SOURCES = [CSRC / "api.cu", CSRC / "serve.cu"]
+BINDING = PKG / "_serve.so"
+BINDING_SOURCE = CSRC / "torch_binding.cpp"
 NVCC = os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")
 
 
 def needs_build() -> bool:
-    if not LIB.exists():
+    if not LIB.exists() or not BINDING.exists() or BINDING_SOURCE.stat().st_mtime > BINDING.stat().st_mtime:
         return True
     t = LIB.stat().st_mtime
     deps = list(CSRC.glob("*.cu")) + list(CSRC.glob("*.cuh")) + list(CSRC.glob("*.h")) + list((PKG.parent / "include").glob("*.h"))
@@ -52,7 +54,24 @@ def build(force: bool = False, verbose: bool = False) -> Path:
     tmp = LIB.with_suffix(f".{os.getpid()}.tmp")
     subprocess.run([NVCC, "-gencode", "arch=compute_100a,code=sm_100a", "-shared", "-o", str(tmp), *(str(o) for _, o, _ in objs)], check=True)
     os.replace(tmp, LIB)
+    build_binding()
     return LIB
+
+
+def build_binding() -> Path:
+    """The extension is linked to libmmv.so beside it; torch's libraries are the ones that the process has loaded."""
+    import importlib.util
+    import sysconfig
+
+    torch = Path(importlib.util.find_spec("torch").origin).parent
+    cuda = Path(NVCC).resolve().parent.parent
+    include = [torch / "include", torch / "include/torch/csrc/api/include", sysconfig.get_paths()["include"], cuda / "include"]
+    tmp = BINDING.with_suffix(f".{os.getpid()}.tmp")
+    subprocess.run([os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-shared", "-fPIC", "-DNDEBUG", *(f"-I{i}" for i in include), "-o", str(tmp),
+                    str(BINDING_SOURCE), f"-L{torch / 'lib'}", f"-L{PKG}", "-l:libmmv.so", "-lc10", "-lc10_cuda", "-ltorch_cpu", "-ltorch_python",
+                    "-Wl,-rpath,$ORIGIN"], check=True)
+    os.replace(tmp, BINDING)
+    return BINDING
 
 
 if __name__ == "__main__":
