@@ -28,11 +28,17 @@ struct TablesParams {
     int nreq, block_size;
     long long max_blocks;
     int32_t* base;                 // per-request sums of new blocks (two-kernel form only)
+    int shift;                     // log2 of block_size, or -1
     WorkspaceHeader* hdr;
 };
+// n / block_size
+__device__ __forceinline__ unsigned tables_div(const TablesParams& p, unsigned n) {
+    return p.shift >= 0 ? n >> p.shift : n / static_cast<unsigned>(p.block_size);
+}
 
 struct TablesLen {
-    int past, added, total, fresh;
+    int past, added, total;
+    unsigned had, need;
     bool bad;
 };
 __device__ __forceinline__ TablesLen tables_len(const TablesParams& p, int r) {
@@ -49,14 +55,16 @@ __device__ __forceinline__ TablesLen tables_len(const TablesParams& p, int r) {
     x.total = x.past + x.added;
     const unsigned b = static_cast<unsigned>(p.block_size);
     // (ceil of an int32 by an int32, in unsigned arithmetic: no overflow)
-    x.fresh = static_cast<int>((static_cast<unsigned>(x.total) + b - 1u) / b - (static_cast<unsigned>(x.past) + b - 1u) / b);
+    x.need = tables_div(p, static_cast<unsigned>(x.total) + b - 1u);
+    x.had = tables_div(p, static_cast<unsigned>(x.past) + b - 1u);
     return x;
 }
 
-// Exclusive sums over all requests into off[0..nreq] and base[0..nreq) (shared or global memory) by one CTA.
+// Exclusive sums over all requests into off[0..nreq] and base[0..nreq) (shared or global memory) by one CTA; `keep`, if not
+// null, gets the requests' past lengths, and p.total is written if `totals`.
 // The token sum is carried in 64 bits and stored cut to int32; the block sum is at most the token sum.
 // Returns the number of new blocks; sets `code` (thread-wise) to what is wrong with the lengths.
-__device__ __forceinline__ long long tables_scan(const TablesParams& p, int32_t* off, int32_t* base, long long& tokens, unsigned& code) {
+__device__ __forceinline__ long long tables_scan(const TablesParams& p, int32_t* off, int32_t* base, int32_t* keep, bool totals, long long& tokens, unsigned& code) {
     __shared__ long long s_a[TABLES_THREADS / 32], s_b[TABLES_THREADS / 32];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     long long run_a = 0, run_b = 0;
@@ -66,9 +74,11 @@ __device__ __forceinline__ long long tables_scan(const TablesParams& p, int32_t*
         if (r < p.nreq) {
             const TablesLen x = tables_len(p, r);
             a = x.added;
-            b = x.fresh;
+            if (keep) keep[r] = x.past;
+            if (totals) p.total[r] = x.total;
+            b = x.need - x.had;
             if (x.bad) code = code ? code : 4u;                                       // MMV_ERR_BAD_SEGMENTS
-            if ((static_cast<unsigned>(x.total) + p.block_size - 1u) / p.block_size > p.max_blocks && b > 0)
+            if (x.need > p.max_blocks && b > 0)
                 code = code ? code : 7u;                                              // MMV_ERR_OUT_OF_BLOCKS
         }
         long long ia = a, ib = b;
@@ -122,7 +132,7 @@ __device__ __forceinline__ void tables_status(const TablesParams& p, unsigned co
 }
 
 // slots[t0 .. t0 + 8) and the table entries that open with these tokens.
-__device__ __forceinline__ void tables_expand(const TablesParams& p, const int32_t* off, const int32_t* base, long long t0) {
+__device__ __forceinline__ void tables_expand(const TablesParams& p, const int32_t* off, const int32_t* base, const int32_t* pasts, long long t0) {
     if (t0 >= p.nslots) return;
     const int tokens = off[p.nreq];
     int64_t out[TABLES_TOKENS_PER_THREAD];
@@ -145,11 +155,11 @@ __device__ __forceinline__ void tables_expand(const TablesParams& p, const int32
         const auto enter = [&](int t) {             // request r, whose token t is next
             begin = off[r];
             end = off[r + 1];
-            const int past = max(p.past[r], 0);
-            had = static_cast<int>((static_cast<unsigned>(past) + bs - 1u) / bs);
+            const int past = max(pasts[r], 0);
+            had = static_cast<int>(tables_div(p, static_cast<unsigned>(past) + bs - 1u));
             first = base[r];
             const unsigned pos = static_cast<unsigned>(past + (t - begin));
-            q = pos / bs;
+            q = tables_div(p, pos);
             rem = pos - q * bs;
         };
         const auto block = [&] {                    // the id of request r's block q
@@ -201,18 +211,18 @@ __device__ __forceinline__ void tables_expand(const TablesParams& p, const int32
 __global__ void __launch_bounds__(TABLES_THREADS) block_tables_kernel(TablesParams p) {
     extern __shared__ int32_t tables_smem[];
     int32_t* off = tables_smem;
-    int32_t* base = tables_smem + p.nreq + 1;
+    int32_t* base = off + p.nreq + 1;
+    int32_t* pasts = base + p.nreq;
     long long tokens;
     unsigned code = 0u;
-    const long long fresh = tables_scan(p, off, base, tokens, code);
-    if (blockIdx.x == 0) tables_status(p, code, tokens, fresh);
+    const long long fresh = tables_scan(p, off, base, pasts, blockIdx.x == 0, tokens, code);
     __syncthreads();
-    for (int r = blockIdx.x * TABLES_THREADS + threadIdx.x; r <= p.nreq; r += gridDim.x * TABLES_THREADS) {
-        p.offsets[r] = off[r];
-        if (r < p.nreq) p.total[r] = tables_len(p, r).total;
-    }
     for (long long c = blockIdx.x; c * TABLES_TOKENS_PER_CTA < p.nslots; c += gridDim.x)
-        tables_expand(p, off, base, c * TABLES_TOKENS_PER_CTA + threadIdx.x * TABLES_TOKENS_PER_THREAD);
+        tables_expand(p, off, base, pasts, c * TABLES_TOKENS_PER_CTA + threadIdx.x * TABLES_TOKENS_PER_THREAD);
+    if (blockIdx.x == 0) {
+        for (int r = threadIdx.x; r <= p.nreq; r += TABLES_THREADS) p.offsets[r] = off[r];
+        tables_status(p, code, tokens, fresh);
+    }
 }
 
 // Many requests: the sums by one CTA, in global memory ...
@@ -220,15 +230,14 @@ __global__ void __launch_bounds__(TABLES_THREADS) block_tables_scan_kernel(Table
     griddep_launch_dependents();
     long long tokens;
     unsigned code = 0u;
-    const long long fresh = tables_scan(p, p.offsets, p.base, tokens, code);
+    const long long fresh = tables_scan(p, p.offsets, p.base, nullptr, true, tokens, code);
     tables_status(p, code, tokens, fresh);
-    for (int r = threadIdx.x; r < p.nreq; r += TABLES_THREADS) p.total[r] = tables_len(p, r).total;
 }
 // ... and the look-ups by all.
 __global__ void __launch_bounds__(TABLES_THREADS) block_tables_expand_kernel(TablesParams p) {
     griddep_wait();
     for (long long c = blockIdx.x; c * TABLES_TOKENS_PER_CTA < p.nslots; c += gridDim.x)
-        tables_expand(p, p.offsets, p.base, c * TABLES_TOKENS_PER_CTA + threadIdx.x * TABLES_TOKENS_PER_THREAD);
+        tables_expand(p, p.offsets, p.base, p.past, c * TABLES_TOKENS_PER_CTA + threadIdx.x * TABLES_TOKENS_PER_THREAD);
 }
 
 }  // namespace mmv

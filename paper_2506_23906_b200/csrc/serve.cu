@@ -31,7 +31,7 @@ bool allow_smem(K kernel, int bytes) {
     return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes) == cudaSuccess;
 }
 
-constexpr int kTablesSmemMax = (2 * TABLES_FUSED_MAX + 1) * static_cast<int>(sizeof(int32_t));
+constexpr int kTablesSmemMax = (3 * TABLES_FUSED_MAX + 1) * static_cast<int>(sizeof(int32_t));
 
 // One-time set-up of the current device (only success is remembered).
 ServeDevice* serve_device() {
@@ -169,11 +169,10 @@ mmv_status launch_paged(const PagedParams& p, int ctas, cudaStream_t st) {
     return launch(paged_join_kernel<BF16>, dim3(static_cast<unsigned>(ctas), static_cast<unsigned>(p.rows)), PA_JOIN_THREADS, 0, st, true, p, ctas);
 }
 
-// One CTA per SM, fewer where there is less than LIN_MIN_UNITS chunks for each (the chunks' upper bound: every sequence ends in a short one).
+// One CTA per SM, fewer where there are fewer chunks (their upper bound: every sequence ends in a short one).
 constexpr int kLinearMaxSms = 160;
 int linear_ctas(const mmv_linear_inputs* in, int64_t nseq, int64_t ntok, int sms) {
-    const int64_t units = (ntok / LIN_C + nseq) * in->heads;
-    int64_t ctas = units / LIN_MIN_UNITS;
+    int64_t ctas = (ntok / LIN_C + nseq) * in->heads;
     if (ctas > sms) ctas = sms;
     if (ctas > kLinearMaxSms) ctas = kLinearMaxSms;
     return ctas < 1 ? 1 : static_cast<int>(ctas);
@@ -248,13 +247,14 @@ mmv_status mmv_block_tables(const int32_t* past, const int32_t* added, int64_t n
     p.nreq = static_cast<int>(nreq);
     p.block_size = block_size;
     p.max_blocks = max_blocks;
+    p.shift = (block_size & (block_size - 1)) ? -1 : __builtin_ctz(static_cast<unsigned>(block_size));
     p.hdr = static_cast<WorkspaceHeader*>(workspace);
     p.base = reinterpret_cast<int32_t*>(static_cast<uint8_t*>(workspace) + sizeof(WorkspaceHeader));
     long long ctas = (nslots + TABLES_TOKENS_PER_CTA - 1) / TABLES_TOKENS_PER_CTA;
     if (ctas > dev->sm_count) ctas = dev->sm_count;
     if (ctas < 1) ctas = 1;
     if (nreq <= TABLES_FUSED_MAX)
-        return launch(block_tables_kernel, dim3(static_cast<unsigned>(ctas)), TABLES_THREADS, (2 * nreq + 1) * sizeof(int32_t), st, false, p);
+        return launch(block_tables_kernel, dim3(static_cast<unsigned>(ctas)), TABLES_THREADS, (3 * nreq + 1) * sizeof(int32_t), st, false, p);
     const mmv_status rc = launch(block_tables_scan_kernel, dim3(1), TABLES_THREADS, 0, st, false, p);
     if (rc != MMV_OK || nslots == 0) return rc;
     return launch(block_tables_expand_kernel, dim3(static_cast<unsigned>(ctas)), TABLES_THREADS, 0, st, true, p);
