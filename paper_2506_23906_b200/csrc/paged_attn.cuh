@@ -67,6 +67,13 @@ __device__ __forceinline__ PagedSpan paged_span(const PagedParams& p, int r) {
     return s;
 }
 
+// 2^x for x <= 0 in one instruction (2 units in the last place, as exp2f; results under 2^-126 are 0)
+__device__ __forceinline__ float paged_exp2(float x) {
+    float r;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+    return r;
+}
+
 // first unit of CTA c's range, and the CTA whose range holds unit u (ranges [c W / G, (c + 1) W / G))
 __device__ __forceinline__ long long paged_first(long long c, long long units, int ctas) { return c * units / ctas; }
 __device__ __forceinline__ int paged_cta_of(long long u, long long units, int ctas) { return static_cast<int>(((u + 1) * ctas - 1) / units); }
@@ -153,9 +160,13 @@ __device__ __forceinline__ bool paged_next(const PagedParams& p, PagedIter& it) 
     return true;
 }
 
-template <bool BF16, int DP>
+// SMALL: up to 8 query heads per key head.  Their rows fill half of the product; the other half takes what rounding the
+// weights to 16 bits left of them, so that one product does for both (4 requests of 131072 tokens, 32/8 heads of 128: 419 -> 341 us; 64 requests
+// of up to 4096: 123 -> 100 us).
+template <bool BF16, int DP, bool SMALL>
 __global__ void __launch_bounds__(PA_THREADS) paged_attention_kernel(const PagedParams p) {
     using C = PagedCfg<DP>;
+    constexpr int HALVES = SMALL ? 1 : 2;                             // of the 16 rows that hold query heads
     extern __shared__ __align__(128) uint8_t smem[];
     __shared__ long long s_sum[PA_WARPS];
     __shared__ int s_start[2];
@@ -266,25 +277,18 @@ __global__ void __launch_bounds__(PA_THREADS) paged_attention_kernel(const Paged
     };
     long long u_ld = u0;
     bool fresh = true;                                                // the next tile to fetch begins a head
-#pragma unroll
-    for (int s = 0; s < PA_STAGES; ++s) {
-        if (u_ld < u1) {
-            if (fresh) fetch_q();
-            fetch(s);
-            if (++u_ld < u1) fresh = paged_next(p, ld);
-        }
-        cp_async_commit();
-    }
 
     uint32_t qf[DP / 16][4];
     float o[DP / 8][4];
     float m[2], l[2];
     int seg = 0, stage = 0;
     bool begins = true;
-    for (long long u = u0; u < u1; ++u) {
+    // (The first PA_STAGES turns only fetch: with one place in the code that does, its loop fits the instruction cache.)
+#pragma unroll 1
+    for (long long u = u0 - PA_STAGES; u < u1; ++u) {
         cp_async_wait<PA_STAGES - 1>();
         __syncwarp();
-        if (begins) {
+        if (begins && u >= u0) {
             __syncthreads();                                          // every warp's share of the query rows has landed
             const uint32_t src = sm_q + (seg % C::kQSlots) * C::kQ;
             const int row = lane & 15;
@@ -297,7 +301,7 @@ __global__ void __launch_bounds__(PA_THREADS) paged_attention_kernel(const Paged
             ++seg;
         }
         const int tok0 = it.first + it.tile * PA_TILE + warp * PA_TOKENS;
-        if (tok0 < it.len) {
+        if (u >= u0 && tok0 < it.len) {
             const uint32_t kb = sm_stage + stage * C::kStage, vb = kb + PA_TOKENS * C::kRow;
             float s[2][4] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
             {
@@ -315,39 +319,45 @@ __global__ void __launch_bounds__(PA_THREADS) paged_attention_kernel(const Paged
 #pragma unroll
             for (int n = 0; n < 2; ++n)
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
+                for (int i = 0; i < 2 * HALVES; ++i) {
                     s[n][i] *= p.scale_log2;
                     if (edge) {
                         const int tok = tok0 + n * 8 + (lane & 3) * 2 + (i & 1);
                         if (tok < it.begin || tok >= it.len) s[n][i] = -INFINITY;
                     }
                 }
-            uint32_t hi[4], lo[4];
+            uint32_t hi[4], lo[4];                                    // (SMALL: the low parts are hi[1] and hi[3], rows 8 to 15)
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {                             // rows lane / 4 and lane / 4 + 8
+            for (int h = 0; h < HALVES; ++h) {                        // rows lane / 4 and lane / 4 + 8
                 float top = fmaxf(fmaxf(s[0][2 * h], s[0][2 * h + 1]), fmaxf(s[1][2 * h], s[1][2 * h + 1]));
                 top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
                 top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
                 const float now = fmaxf(m[h], top);
                 const float base = now == -INFINITY ? 0.f : now;      // (no token yet: every weight is 2^-inf = 0)
-                const float fall = exp2f(m[h] - base);
+                const float fall = paged_exp2(m[h] - base);
                 m[h] = now;
                 float sum = 0.f;
 #pragma unroll
                 for (int n = 0; n < 2; ++n) {
-                    const float a = exp2f(s[n][2 * h] - base), b = exp2f(s[n][2 * h + 1] - base);
+                    const float a = paged_exp2(s[n][2 * h] - base), b = paged_exp2(s[n][2 * h + 1] - base);
                     sum += a + b;
                     // The weights enter the product as the sum of two 16-bit values: rounded to one, their error would be as
                     // large as the result's own rounding.
                     hi[n * 2 + h] = pack_pair<BF16>(a, b);
                     const float2 back = unpack_pair<BF16>(hi[n * 2 + h]);
-                    lo[n * 2 + h] = pack_pair<BF16>(a - back.x, b - back.y);
+                    (SMALL ? hi[n * 2 + 1] : lo[n * 2 + h]) = pack_pair<BF16>(a - back.x, b - back.y);
                 }
                 l[h] = l[h] * fall + sum;
+                if (__any_sync(0xffffffffu, fall != 1.f)) {           // (the maximum of a long context soon stands)
 #pragma unroll
-                for (int n = 0; n < DP / 8; ++n) {
-                    o[n][2 * h] *= fall;
-                    o[n][2 * h + 1] *= fall;
+                    for (int n = 0; n < DP / 8; ++n) {
+                        o[n][2 * h] *= fall;
+                        o[n][2 * h + 1] *= fall;
+                        if (SMALL) {
+                            o[n][2] *= fall;
+                            o[n][3] *= fall;
+                        }
+                    }
                 }
             }
             {
@@ -358,8 +368,10 @@ __global__ void __launch_bounds__(PA_THREADS) paged_attention_kernel(const Paged
                     ldsm_x4_t(b, vb + row * C::kRow + (((2 * d + (lane >> 4)) ^ (row & 7)) << 4));
                     mma_16816<BF16>(o[2 * d], hi, b[0], b[1]);
                     mma_16816<BF16>(o[2 * d + 1], hi, b[2], b[3]);
-                    mma_16816<BF16>(o[2 * d], lo, b[0], b[1]);
-                    mma_16816<BF16>(o[2 * d + 1], lo, b[2], b[3]);
+                    if (!SMALL) {
+                        mma_16816<BF16>(o[2 * d], lo, b[0], b[1]);
+                        mma_16816<BF16>(o[2 * d + 1], lo, b[2], b[3]);
+                    }
                 }
             }
         }
@@ -371,6 +383,7 @@ __global__ void __launch_bounds__(PA_THREADS) paged_attention_kernel(const Paged
         }
         cp_async_commit();
         stage = stage + 1 == PA_STAGES ? 0 : stage + 1;
+        if (u < u0) continue;
 
         const PagedIter done = it;
         const bool ends = it.tile + 1 == it.tiles;                    // of this (request, head part)
@@ -382,8 +395,14 @@ __global__ void __launch_bounds__(PA_THREADS) paged_attention_kernel(const Paged
         // ---- the warps meet --------------------------------------------------------------------------------------------
         const int head = done.hp / p.parts, part = done.hp - head * p.parts;
         const int rows = min(p.rows, p.group - part * p.rows);
+        if (SMALL)
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
+            for (int n = 0; n < DP / 8; ++n) {
+                o[n][0] += o[n][2];
+                o[n][1] += o[n][3];
+            }
+#pragma unroll
+        for (int h = 0; h < HALVES; ++h) {
             l[h] += __shfl_xor_sync(0xffffffffu, l[h], 1);
             l[h] += __shfl_xor_sync(0xffffffffu, l[h], 2);
             const int row = (lane >> 2) + 8 * h;
@@ -395,13 +414,13 @@ __global__ void __launch_bounds__(PA_THREADS) paged_attention_kernel(const Paged
         __syncthreads();
         float top[2];
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
+        for (int h = 0; h < HALVES; ++h) {
             const int row = (lane >> 2) + 8 * h;
             top[h] = s_m[0][row];
 #pragma unroll
             for (int w = 1; w < PA_WARPS; ++w) top[h] = fmaxf(top[h], s_m[w][row]);
             // (a warp without tokens has maximum -infinity, sum 0 and result 0, and contributes 2^-inf = 0 times that; a NaN stays one)
-            const float f = exp2f(m[h] - (top[h] == -INFINITY ? 0.f : top[h]));
+            const float f = paged_exp2(m[h] - (top[h] == -INFINITY ? 0.f : top[h]));
             if (row < rows) {
 #pragma unroll
                 for (int n = 0; n < DP / 8; ++n)
@@ -422,7 +441,7 @@ __global__ void __launch_bounds__(PA_THREADS) paged_attention_kernel(const Paged
             float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
             for (int w = 0; w < PA_WARPS; ++w) {
-                sum += s_l[w][row] * exp2f(s_m[w][row] - (t == -INFINITY ? 0.f : t));
+                sum += s_l[w][row] * paged_exp2(s_m[w][row] - (t == -INFINITY ? 0.f : t));
                 const float4 y = *reinterpret_cast<const float4*>(sm_o + (w * p.rows + row) * C::kPitch + c);
                 x.x += y.x;
                 x.y += y.y;
@@ -505,7 +524,7 @@ __global__ void __launch_bounds__(PA_JOIN_THREADS) paged_join_kernel(const Paged
         float w = 0.f;
         if (i < n) {
             const float mi = p.part_ml[place(i) * 2 * PA_ROWS + row], li = p.part_ml[(place(i) * 2 + 1) * PA_ROWS + row];
-            w = exp2f(mi - (top == -INFINITY ? 0.f : top));
+            w = paged_exp2(mi - (top == -INFINITY ? 0.f : top));
             sum += w * li;
         }
         s_w[tid] = w;

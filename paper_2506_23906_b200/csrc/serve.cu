@@ -31,6 +31,13 @@ bool allow_smem(K kernel, int bytes) {
     return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes) == cudaSuccess;
 }
 
+template <int DP>
+bool allow_paged() {
+    const int bytes = PagedCfg<DP>::smem_bytes(PA_ROWS);
+    return allow_smem(paged_attention_kernel<false, DP, false>, bytes) && allow_smem(paged_attention_kernel<false, DP, true>, bytes) &&
+           allow_smem(paged_attention_kernel<true, DP, false>, bytes) && allow_smem(paged_attention_kernel<true, DP, true>, bytes);
+}
+
 constexpr int kTablesSmemMax = (3 * TABLES_FUSED_MAX + 1) * static_cast<int>(sizeof(int32_t));
 
 // One-time set-up of the current device (only success is remembered).
@@ -45,12 +52,7 @@ ServeDevice* serve_device() {
     if (cudaDeviceGetAttribute(&sm, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) return nullptr;
     d->sm_count = sm;
     bool ok = allow_smem(block_tables_kernel, kTablesSmemMax);
-    ok &= allow_smem(paged_attention_kernel<false, 64>, PagedCfg<64>::smem_bytes(PA_ROWS));
-    ok &= allow_smem(paged_attention_kernel<true, 64>, PagedCfg<64>::smem_bytes(PA_ROWS));
-    ok &= allow_smem(paged_attention_kernel<false, 128>, PagedCfg<128>::smem_bytes(PA_ROWS));
-    ok &= allow_smem(paged_attention_kernel<true, 128>, PagedCfg<128>::smem_bytes(PA_ROWS));
-    ok &= allow_smem(paged_attention_kernel<false, 256>, PagedCfg<256>::smem_bytes(PA_ROWS));
-    ok &= allow_smem(paged_attention_kernel<true, 256>, PagedCfg<256>::smem_bytes(PA_ROWS));
+    ok &= allow_paged<64>() && allow_paged<128>() && allow_paged<256>();
     ok &= allow_smem(linear_chunks_kernel<64, true>, LinCfg<64, true>::kSmemBytes);
     ok &= allow_smem(linear_chunks_kernel<64, false>, LinCfg<64, false>::kSmemBytes);
     ok &= allow_smem(linear_chunks_kernel<128, true>, LinCfg<128, true>::kSmemBytes);
@@ -163,8 +165,10 @@ PagedPlan paged_plan(const PagedHeads& h, int dim) {
 
 template <bool BF16, int DP>
 mmv_status launch_paged(const PagedParams& p, int ctas, cudaStream_t st) {
-    const mmv_status rc = launch(paged_attention_kernel<BF16, DP>, dim3(static_cast<unsigned>(ctas)), PA_THREADS,
-                                 static_cast<size_t>(PagedCfg<DP>::smem_bytes(p.rows)), st, false, p);
+    const size_t smem = static_cast<size_t>(PagedCfg<DP>::smem_bytes(p.rows));
+    const dim3 grid(static_cast<unsigned>(ctas));
+    const mmv_status rc = p.rows <= 8 ? launch(paged_attention_kernel<BF16, DP, true>, grid, PA_THREADS, smem, st, false, p)
+                                      : launch(paged_attention_kernel<BF16, DP, false>, grid, PA_THREADS, smem, st, false, p);
     if (rc != MMV_OK) return rc;
     return launch(paged_join_kernel<BF16>, dim3(static_cast<unsigned>(ctas), static_cast<unsigned>(p.rows)), PA_JOIN_THREADS, 0, st, true, p, ctas);
 }
