@@ -378,7 +378,9 @@ mmv_status mmv_seg_scan_host(const void *x_host, const void *flags_host, int64_t
  * Tensors of values are given with their strides in ELEMENTS; the last axis is
  * contiguous, strides are multiples of 8 elements and pointers 16-byte aligned
  * (dimensions are multiples of 8), so that every row is read in 16-byte words.
- * Metadata pointers need the alignment of their type.  Unlike the calls above,
+ * Values that are not finite make the results they enter not finite; they never
+ * reach another request's or sequence's, nor results that a length or a window
+ * keeps them from.  Metadata pointers need the alignment of their type.  Unlike the calls above,
  * these enqueue kernels only and can be captured in a CUDA graph like them.
  * Calls on different streams may overlap; a workspace each, as above.
  * ------------------------------------------------------------------------- */
@@ -505,7 +507,9 @@ mmv_status mmv_linear_attention_step(const mmv_linear_inputs *in, int64_t nreq, 
  * states, which have no bound, are operands of the tensor core, and fp16's range
  * does not hold them.  out: ntok x heads x dim_v; rows of tokens outside
  * [offsets[0], offsets[nseq]) are not written.  log_decay: heads values, any
- * <= 0, -infinity included.  Offsets that decrease or leave [0, ntok] are reported
+ * <= 0, -infinity included.  Values of v that are not finite may reach results of
+ * up to 63 tokens in front of theirs in the same sequence.  Scores, states and decayed keys
+ * of 2^111 and more become NaN.  Offsets that decrease or leave [0, ntok] are reported
  * as MMV_ERR_BAD_SEGMENTS in the workspace; nothing outside the buffers is touched.
  * ntok < 2^31, nseq < 2^20.  Workspace: mmv_linear_attention_workspace_bytes(in, nseq, ntok),
  * 256-byte aligned.

@@ -563,3 +563,83 @@ def test_linear_attention_nothing(mmv):
     assert (last == 0).all()
     out, last = mmv.linear_attention(q[:0], k[:0], v[:0], ints([0]), g)
     assert last.shape == (0, 2, 64, 64)
+
+
+# ---------------------------------------------------------------------------------------------------------------------
+# the binding's checks, streams, graphs, the example
+# ---------------------------------------------------------------------------------------------------------------------
+def test_binding_refusals(mmv):
+    q, kc, vc, table, lens = paged_case(1, [5, 7], 4, 2, 64, 16, torch.float16)
+    for error, change in [(TypeError, dict(lens=lens.long())), (ValueError, dict(lens=lens[:1])), (TypeError, dict(table=table.long())), (TypeError, dict(q=q.bfloat16())),
+                          (ValueError, dict(q=q[:, :3])), (ValueError, dict(q=q[..., :32])), (ValueError, dict(q=q.cpu())), (TypeError, dict(q=3)),
+                          (ValueError, dict(q=q.transpose(1, 2))), (ValueError, dict(v_cache=vc[:, :8])), (ValueError, dict(out=torch.empty(2, 4, 32, dtype=q.dtype, device="cuda"))),
+                          (TypeError, dict(lse=torch.empty(2, 4, dtype=torch.float64, device="cuda"))), (TypeError, dict(scale="x")), (mmv.MmvError, dict(window=-1)),
+                          (mmv.MmvError, dict(workspace=torch.empty(256, dtype=torch.uint8, device="cuda")))]:
+        args = dict(q=q, k_cache=kc, v_cache=vc, table=table, lens=lens)
+        args.update(change)
+        with pytest.raises(error):
+            mmv.paged_attention(**args)
+    x = torch.zeros(3, 2, 64, dtype=torch.float16, device="cuda")
+    s, g = torch.zeros(3, 2, 64, 64, device="cuda"), torch.zeros(2, device="cuda")
+    with pytest.raises(mmv.MmvError):
+        mmv.linear_attention(x, x, x, ints([0, 3]), g)                   # the prompt form takes bfloat16
+    with pytest.raises(ValueError):
+        mmv.linear_attention_step(x, x, x, g, s[:, :1].contiguous())
+    with pytest.raises(ValueError):
+        mmv.linear_attention_step(x, x[:, :, :32], x, g, s)
+    with pytest.raises(mmv.MmvError):
+        mmv.linear_attention_step(x, x, x, g, s[:2])                     # fewer states than requests
+    with pytest.raises(TypeError):
+        mmv.kv_append(x, x, torch.zeros(3, dtype=torch.int32, device="cuda"), kc, vc)
+    with pytest.raises(mmv.MmvError):
+        mmv.block_tables(ints([1]), ints([1]), ints([0]), torch.zeros(1, 4, dtype=torch.int32, device="cuda"), torch.zeros(4, dtype=torch.int64, device="cuda"), 0)
+
+
+def test_calls_on_another_stream_and_in_a_graph(mmv):
+    """The same results on a side stream, and from a captured step replayed with new contents."""
+    q, kc, vc, table, lens = paged_case(21, [300, 77, 4000], 8, 2, 64, 16, torch.bfloat16, garbage=0.0)
+    lq, lk, lv, off, g, st = linear_case(22, [300, 77, 500], 4, 4, 64, 64)
+    offsets = ints(off)
+    want, _ = mmv.paged_attention(q, kc, vc, table, lens)
+    lwant, swant = mmv.linear_attention(lq, lk, lv, offsets, g, state=st)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    out, _ = mmv.paged_attention(q, kc, vc, table, lens, stream=side)
+    lout, sout = mmv.linear_attention(lq, lk, lv, offsets, g, state=st, stream=side)
+    torch.cuda.current_stream().wait_stream(side)
+    assert torch.equal(out, want) and torch.equal(lout, lwant) and torch.equal(sout, swant)
+    graph = torch.cuda.CUDAGraph()
+    q1, lq1 = torch.zeros_like(q), torch.zeros_like(lq)
+    with torch.cuda.graph(graph):
+        out, _ = mmv.paged_attention(q1, kc, vc, table, lens)
+        lout, sout = mmv.linear_attention(lq1, lk, lv, offsets, g, state=st)
+    q1.copy_(q)
+    lq1.copy_(lq)
+    for _ in range(2):
+        graph.replay()
+    assert torch.equal(out, want) and torch.equal(lout, lwant) and torch.equal(sout, swant)
+
+
+@pytest.mark.parametrize("order", ["head first", "padded"])
+def test_linear_attention_layouts(mmv, order):
+    """[head, token, column] in memory, and rows with other data between them."""
+    q, k, v, off, g, state = linear_case(31, [100, 3, 129], 4, 2, 64, 96)
+    want, last = mmv.linear_attention(q, k, v, ints(off), g, state=state)
+    if order == "head first":
+        q, k, v = (x.transpose(0, 1).contiguous().transpose(0, 1) for x in (q, k, v))
+    else:
+        q, k, v = (torch.cat([x, torch.full_like(x[..., :8], float("nan"))], -1)[..., :x.size(2)] for x in (q, k, v))
+    out, last2 = mmv.linear_attention(q, k, v, ints(off), g, state=state)
+    assert torch.equal(out, want) and torch.equal(last, last2)
+
+
+def test_example_serves_a_ragged_batch(mmv):
+    """The example's last logits against the dense fp32 model on the whole sequences: no further off than twice what the dense model itself
+    makes of rounding its activations to bfloat16 at the same places (the server's roundings are others, and as many)."""
+    import importlib.util
+    from pathlib import Path
+    spec = importlib.util.spec_from_file_location("serve_ragged_batch", Path(__file__).resolve().parent.parent / "examples" / "serve_ragged_batch.py")
+    ex = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(ex)
+    off, own = ex.difference(*ex.serve(5, 6, seed=3))
+    assert off < 2 * own
