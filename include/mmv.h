@@ -507,8 +507,7 @@ mmv_status mmv_linear_attention_step(const mmv_linear_inputs *in, int64_t nreq, 
  * states, which have no bound, are operands of the tensor core, and fp16's range
  * does not hold them.  out: ntok x heads x dim_v; rows of tokens outside
  * [offsets[0], offsets[nseq]) are not written.  log_decay: heads values, any
- * <= 0, -infinity included.  Values of v that are not finite may reach results of
- * up to 63 tokens in front of theirs in the same sequence.  Scores, states and decayed keys
+ * <= 0, -infinity included.  Scores, states and decayed keys
  * of 2^111 and more become NaN.  Offsets that decrease or leave [0, ntok] are reported
  * as MMV_ERR_BAD_SEGMENTS in the workspace; nothing outside the buffers is touched.
  * ntok < 2^31, nseq < 2^20.  Workspace: mmv_linear_attention_workspace_bytes(in, nseq, ntok),

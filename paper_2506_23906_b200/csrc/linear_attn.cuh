@@ -181,7 +181,7 @@ struct LinCfg {
     static constexpr int kA = kKp + 2 * kKpBytes;           // two parts of A
     static constexpr int kOPitch = 256;
     static constexpr int kO = kA + (CARRY ? 0 : 2 * LIN_BOX);
-    static constexpr int kSmemBytes = kO + (CARRY ? 0 : LIN_C * kOPitch) + 1024;      // (+ alignment)
+    static constexpr int kSmemBytes = kO + (CARRY ? 0 : LIN_C * kOPitch);
     static constexpr uint32_t kTmemCols = CARRY ? DK : 512;
     // columns of tensor memory
     static constexpr uint32_t kColKV = 0, kColS = 128, kColAT = 256, kColO1 = 384, kColO2 = 448;
@@ -294,6 +294,20 @@ static __device__ __noinline__ bool lin_wait_one(uint64_t* bar, uint32_t parity,
     }
     return true;
 }
+// sum_j scale exp(g (i - j)) (q_i . k_j) v_j over j <= i for one column of v, from the tiles in shared memory (of = scale exp(g (x + 1))).
+static __device__ __noinline__ float lin_repair(const uint8_t* q, const uint8_t* k, const uint8_t* v, int dk, int i, int col, float scale, const float* of) {
+    const auto at = [](const uint8_t* tile, int row, int c) {
+        const uint16_t x = *reinterpret_cast<const uint16_t*>(tile + (c >> 6) * LIN_BOX + swz_offset<128>(row, (c & 63) * 2));
+        return __uint_as_float(static_cast<uint32_t>(x) << 16);
+    };
+    float y = 0.f;
+    for (int j = 0; j <= i; ++j) {
+        float s = 0.f;
+        for (int d = 0; d < dk; ++d) s = fmaf(at(q, i, d), at(k, j, d), s);
+        y = fmaf(s * (i == j ? scale : of[i - j - 1]), at(v, j, col), y);
+    }
+    return y;
+}
 // A wait of a whole warp: all of its lanes get the same answer.
 __device__ __forceinline__ bool lin_wait(uint64_t* bar, uint32_t parity, volatile int* abort_flag, uint64_t budget_ns) {
     return __all_sync(0xffffffffu, lin_wait_one(bar, parity, abort_flag, budget_ns));
@@ -313,9 +327,8 @@ linear_chunks_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
                      const __grid_constant__ CUtensorMap map_v, const LinParams p) {
     using C = LinCfg<DK, CARRY>;
     constexpr int COLS = DK / (LIN_STATE / 4);              // state columns of a thread
-    extern __shared__ __align__(16) uint8_t lin_smem_raw[];
-    // (aligned by an offset: an address that went through an integer is accessed as a generic one, not as shared memory)
-    uint8_t* smem = lin_smem_raw + ((1024u - (smem_u32(lin_smem_raw) & 1023u)) & 1023u);
+    extern __shared__ __align__(1024) uint8_t lin_smem[];   // (the swizzle goes by the address: tiles start at multiples of 1024)
+    uint8_t* smem = lin_smem;
     __shared__ LinBars bars;
     __shared__ long long s_sum[LIN_THREADS / 32];
     __shared__ int s_most;
@@ -327,6 +340,10 @@ linear_chunks_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     volatile int* abort_flag = &s_abort;
     griddep_launch_dependents();
+    if (smem_u32(smem) & 1023u) {                           // (never: the declaration asks for it)
+        if (tid == 0) report_error(p.hdr, 6u);              // MMV_ERR_CUDA
+        return;
+    }
 
     // ---- the list, this CTA's range of it ---------------------------------------------------------------------------------
     const int nseq = static_cast<int>(p.nseq);
@@ -353,7 +370,7 @@ linear_chunks_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
         s_seq = -1;
         for (int i = 0; i < C::kStages; ++i) {
             mbar_init(&bars.full[i], 1);
-            mbar_init(&bars.empty[i], CARRY ? 1 : 3);       // the products that read the tile last
+            mbar_init(&bars.empty[i], CARRY ? 1 : 7);       // the products that read the tile last, and the results' warps
         }
         for (int i = 0; i < 2; ++i) {
             mbar_init(&bars.at_full[i], 1);
@@ -631,6 +648,7 @@ linear_chunks_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
                 ok = lin_out_all(ok);                       // (s_of is there, and the last chunk's results have left the staging rows)
                 if (!ok) break;
                 tc_fence_after_sync();
+                bool wild = false;
 #pragma unroll 1
                 for (int i0 = 0; i0 < LIN_C; i0 += 8) {
                     uint32_t x[8], y[8];
@@ -640,6 +658,7 @@ linear_chunks_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
 #pragma unroll
                     for (int i = 0; i < 8; i += 4) *reinterpret_cast<float4*>(f + i) = *reinterpret_cast<const float4*>(s_of + i0 + i);
                     tmem_ld_wait();
+                    if (i0 == 0) wild = t < p.dv && (y[0] & 0x7f800000u) == 0x7f800000u;
                     uint8_t* dst = stage + i0 * C::kOPitch + t * 2;
 #pragma unroll
                     for (int i = 0; i < 8; i += 2) {
@@ -649,9 +668,36 @@ linear_chunks_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
                         *reinterpret_cast<uint16_t*>(dst + (i + 1) * C::kOPitch) = static_cast<uint16_t>(o >> 16);
                     }
                 }
+                // The first token's sum has a weight of 0 for every later one.  Where it is not finite, a value of v may be to blame (0 times
+                // an infinity): the tokens in front of this column's first such value are summed up again, one by one.
+                if (__any_sync(0xffffffffu, wild)) {
+                    const uint8_t* tile = smem + (c % C::kStages) * C::kStage;
+                    int stop = 0;                           // first token whose value in this column is not finite
+                    if (wild) {
+                        const uint8_t* v = tile + C::kV + (t >> 6) * LIN_BOX;
+                        while (stop < n && (*reinterpret_cast<const uint16_t*>(v + swz_offset<128>(stop, (t & 63) * 2)) & 0x7f80u) != 0x7f80u) ++stop;
+                        if (stop == n) stop = 0;            // (none: the sum's own scores are not finite)
+                    }
+#pragma unroll 1
+                    for (int i0 = 0; i0 < LIN_C; i0 += 8) {
+                        uint32_t x[8];
+                        tmem_ld_32x8(lanes + C::kColO1 + i0, x);
+                        tmem_ld_wait();
+#pragma unroll
+                        for (int i = 0; i < 8; ++i)
+                            if (i0 + i < stop) {
+                                const float y = lin_repair(tile + C::kQ, tile + C::kK, tile + C::kV, p.dk, i0 + i, t, p.scale, s_of);
+                                *reinterpret_cast<uint16_t*>(stage + (i0 + i) * C::kOPitch + t * 2) =
+                                    lin_store<true>(fmaf(s_of[i0 + i], __uint_as_float(x[i]), y));
+                            }
+                    }
+                }
                 tc_fence_before_sync();
                 __syncwarp();
-                if (lane == 0) mbar_arrive(&bars.o_empty);
+                if (lane == 0) {
+                    mbar_arrive(&bars.o_empty);
+                    mbar_arrive(&bars.empty[c % C::kStages]);
+                }
                 lin_out_sync();
                 if (q < words) {                            // 16 threads to a row, rows r0, r0 + 8, ...
                     uint16_t* out = p.out + ((static_cast<long long>(it.tok) + it.chunk * LIN_C + r0) * p.heads + it.head) * p.dv + q * 8;

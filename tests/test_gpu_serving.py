@@ -531,6 +531,47 @@ def test_linear_attention_neighbours_that_are_not_finite(mmv):
     assert torch.isnan(out[40:110]).all() and torch.isnan(last2[1]).all()
 
 
+@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("bad", [float("nan"), float("inf"), -float("inf")])
+def test_linear_attention_later_tokens_do_not_reach_earlier_ones(mmv, dim, bad):
+    """A value of v, k or q that is not finite reaches no result in front of its token, and no other column, row or sequence: those stay
+    the same bit by bit, but for the tokens of v's column in front of it in its chunk of 64, which are summed up another way and stay
+    inside the bound."""
+    q, k, v, off, g, state = linear_case(12, [700, 90], 4, 4, dim, dim)
+    g[:] = -0.01
+    want, last = mmv.linear_attention(q, k, v, ints(off), g, state=state)
+    exact, mag, _, _ = linear_plain(q, k, v, off, g, 1.0, state)
+    for at in (0, 1, 37, 63, 64, 100, 447, 699):
+        x = v.clone()
+        x[at, 2, 11] = bad
+        x[min(at + 70, 699), 2, 12] = bad
+        out, s = mmv.linear_attention(q, k, x, ints(off), g, state=state)
+        hit = torch.zeros_like(out, dtype=torch.bool)
+        again = torch.zeros_like(hit)
+        for col, first in ((11, at), (12, min(at + 70, 699))):
+            hit[first:700, 2, col] = True
+            again[first // 64 * 64:first, 2, col] = True
+        same = ~hit & ~again
+        assert torch.equal(out[same], want[same]) and not torch.isfinite(out[hit]).any()
+        inside(out[again], exact[again], U[q.dtype] * exact[again].abs() + 2.0 ** -14 * mag[again] + TINY[q.dtype])
+        hit = torch.zeros_like(s, dtype=torch.bool)
+        hit[0, 2, :, 11:13] = True
+        assert torch.equal(s[~hit], last[~hit]) and not torch.isfinite(s[hit]).any()
+        x = k.clone()
+        x[at, 1, 5] = bad
+        out, s = mmv.linear_attention(q, x, v, ints(off), g, state=state)
+        hit = torch.zeros_like(out, dtype=torch.bool)
+        hit[at:700, 1] = True
+        assert torch.equal(out[~hit], want[~hit]) and not torch.isfinite(out[hit]).any()
+        assert not torch.isfinite(s[0, 1, 5]).any() and torch.equal(s[1], last[1]) and torch.equal(s[0, [0, 2, 3]], last[0, [0, 2, 3]])
+        x = q.clone()
+        x[at, 3, 6] = bad
+        out, s = mmv.linear_attention(x, k, v, ints(off), g, state=state)
+        hit = torch.zeros_like(out, dtype=torch.bool)
+        hit[at, 3] = True
+        assert torch.equal(out[~hit], want[~hit]) and not torch.isfinite(out[hit]).any() and torch.equal(s, last)
+
+
 def test_linear_attention_step_continues_a_prompt(mmv):
     """The prompt form's state, taken on by single tokens, is the longer prompt's."""
     q, k, v, off, g, state = linear_case(4, [65, 66], 4, 2, 64, 128)
