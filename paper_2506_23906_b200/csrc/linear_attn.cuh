@@ -182,14 +182,15 @@ struct LinCfg {
     static constexpr int kOPitch = 256;
     static constexpr int kO = kA + (CARRY ? 0 : 2 * LIN_BOX);
     static constexpr int kSmemBytes = kO + (CARRY ? 0 : LIN_C * kOPitch);
-    static constexpr uint32_t kTmemCols = CARRY ? DK : 512;
+    static constexpr int kUpdates = CARRY ? 2 : 1;          // accumulators of KV (there is room for a second without results)
+    static constexpr uint32_t kTmemCols = CARRY ? 2 * DK : 512;
     // columns of tensor memory
     static constexpr uint32_t kColKV = 0, kColS = 128, kColAT = 256, kColO1 = 384, kColO2 = 448;
 };
 
 struct LinBars {
     uint64_t full[3], empty[3], at_full[2], at_empty[2];
-    uint64_t kp_full[2], kv_done[2], kv_full, kv_empty, s_full, s_free, a_full, a_free, o_full, o_empty, drain;
+    uint64_t kp_full[2], kv_done[2], kv_full[2], kv_empty[2], s_full, s_free, a_full, a_free, o_full, o_empty, drain;
 };
 
 // A place in the list of (sequence, head, chunk).
@@ -378,8 +379,10 @@ linear_chunks_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
             mbar_init(&bars.kp_full[i], C::kKeyWarps);
             mbar_init(&bars.kv_done[i], 1);
         }
-        mbar_init(&bars.kv_full, 1);
-        mbar_init(&bars.kv_empty, LIN_STATE);
+        for (int i = 0; i < C::kUpdates; ++i) {
+            mbar_init(&bars.kv_full[i], 1);
+            mbar_init(&bars.kv_empty[i], LIN_STATE);
+        }
         mbar_init(&bars.s_full, LIN_STATE);
         mbar_init(&bars.s_free, 1);
         mbar_init(&bars.a_full, 2);
@@ -506,9 +509,6 @@ linear_chunks_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
                     }
                 }
             }
-            tc_fence_before_sync();
-            __syncwarp();
-            if (lane == 0) mbar_arrive(&bars.kv_empty);     // the update's columns are free for this chunk's
             if constexpr (!CARRY) {
                 if (c > 0) ok = lin_wait(&bars.s_free, (c - 1) & 1, abort_flag, budget);
                 if (!ok) break;
@@ -533,13 +533,13 @@ linear_chunks_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
             }
             const LinDecay d = n == LIN_C ? whole : lin_decay(g, n);
             const uint64_t dhi = lin_pair(d.hi, d.hi), dlo = lin_pair(d.lo, d.lo);
-            ok = lin_wait(&bars.kv_full, c & 1, abort_flag, budget);
+            ok = lin_wait(&bars.kv_full[c % C::kUpdates], (c / C::kUpdates) & 1, abort_flag, budget);
             if (!ok) break;
             tc_fence_after_sync();
 #pragma unroll
             for (int b = 0; b < COLS / 8; ++b) {
                 uint32_t r[8];
-                tmem_ld_32x8(cols + b * 8, r);
+                tmem_ld_32x8(cols + (c % C::kUpdates) * DK + b * 8, r);
                 tmem_ld_wait();
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
@@ -547,6 +547,9 @@ linear_chunks_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
                     s[b * 4 + i] = lin_fma2(s[b * 4 + i], dhi, lin_fma2(s[b * 4 + i], dlo, x));
                 }
             }
+            tc_fence_before_sync();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&bars.kv_empty[c % C::kUpdates]);
             if (!CARRY && it.chunk + 1 == it.chunks && p.state_out) {
                 float* dst = p.state_out + ((static_cast<long long>(it.seq) * p.heads + it.head) * p.dk + part * COLS) * p.dv + row;
 #pragma unroll
@@ -810,17 +813,17 @@ linear_chunks_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
 #pragma unroll 1
                 for (int x = 0; x < 3; ++x, dk += C::kKpPart >> 4)
 #pragma unroll
-                    for (int k = 0; k < 2; ++k) mma_f16_ss(tmem + C::kColKV, dv + 128 * k, dk + 128 * k, kIdescKV, h > 0 || x > 0 || k > 0);
+                    for (int k = 0; k < 2; ++k) mma_f16_ss(tmem + C::kColKV + ((kv >> 1) % C::kUpdates) * DK, dv + 128 * k, dk + 128 * k, kIdescKV, h > 0 || x > 0 || k > 0);
                 tc_commit(&bars.kv_done[h]);
                 if (h) {
-                    tc_commit(&bars.kv_full);
+                    tc_commit(&bars.kv_full[(kv >> 1) % C::kUpdates]);
                     tc_commit(&bars.empty[stage]);
                 }
             };
             if constexpr (CARRY) {
                 for (int kv = 0; ok && kv < 2 * count; ++kv) {
                     ok = lin_wait_one(&bars.kp_full[kv & 1], (kv >> 1) & 1, abort_flag, budget);
-                    if (ok && !(kv & 1)) ok = lin_wait_one(&bars.kv_empty, (kv >> 1) & 1, abort_flag, budget);
+                    if (ok && kv >= 4 && !(kv & 1)) ok = lin_wait_one(&bars.kv_empty[(kv >> 1) & 1], ((kv >> 2) - 1) & 1, abort_flag, budget);
                     if (ok) update(kv);
                 }
             }
@@ -843,7 +846,7 @@ linear_chunks_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
                     tc_commit(&bars.at_full[at & 1]);
                     ++at;
                 }
-                if (kv < 2 * count && mbar_try_wait(&bars.kp_full[kv & 1], (kv >> 1) & 1) && ((kv & 1) || mbar_try_wait(&bars.kv_empty, (kv >> 1) & 1)))
+                if (kv < 2 * count && mbar_try_wait(&bars.kp_full[kv & 1], (kv >> 1) & 1) && (kv == 0 || (kv & 1) || mbar_try_wait(&bars.kv_empty[0], ((kv >> 1) - 1) & 1)))
                     update(kv++);
                 if (o1 < at && o1 < count && mbar_try_wait(&bars.s_full, o1 & 1) && (o1 == 0 || mbar_try_wait(&bars.o_empty, (o1 - 1) & 1))) {
                     tc_fence_after_sync();
