@@ -420,7 +420,10 @@ linear_chunks_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
                 for (long long i = tid; i < n; i += LIN_THREADS) p.state_out[s * n + i] = p.state ? p.state[s * n + i] : 0.f;
             }
     }
-    if (cta >= ctas || units == 0) return;
+    if (cta >= ctas || units == 0) {
+        if constexpr (!CARRY) griddep_wait();               // (what follows in the stream waits for this kernel, and for the first one through it)
+        return;
+    }
     long long u0 = lin_first(cta, units, ctas);
     const long long u1 = lin_first(cta + 1ll, units, ctas);
     {
