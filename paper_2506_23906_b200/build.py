@@ -68,7 +68,7 @@ def build_binding() -> Path:
     include = [torch / "include", torch / "include/torch/csrc/api/include", sysconfig.get_paths()["include"], cuda / "include"]
     tmp = BINDING.with_suffix(f".{os.getpid()}.tmp")
     subprocess.run([os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-shared", "-fPIC", "-DNDEBUG", *(f"-I{i}" for i in include), "-o", str(tmp),
-                    str(BINDING_SOURCE), f"-L{torch / 'lib'}", f"-L{PKG}", "-l:libmmv.so", "-lc10", "-lc10_cuda", "-ltorch_cpu", "-ltorch_python",
+                    str(BINDING_SOURCE), f"-L{torch / 'lib'}", f"-L{PKG}", "-l:libmmv.so", "-lc10", "-lc10_cuda", "-ltorch_cpu", "-ltorch_cuda", "-ltorch_python",
                     "-Wl,-rpath,$ORIGIN"], check=True)
     os.replace(tmp, BINDING)
     return BINDING

@@ -7,8 +7,10 @@
 //
 // What bounds it: latency.  A decoding step of 256 requests moves a few KB, a million new tokens 8 MB.  So there is one
 // launch: every CTA forms both sums for itself in shared memory (8 bytes per request, from the L2) and then
-// serves its own 8192 tokens, eight consecutive ones per thread, of which only the first is searched for.  Beyond
-// TABLES_FUSED_MAX requests the sums no longer fit shared memory and one CTA leaves them in global memory for a second kernel.
+// serves its own tokens: one per thread as long as that fits the SMs (a thread's tokens wait for each other's table
+// entries: 256 requests of one token 3.7 against 6.8 us, 8192 of 18 tokens 13.5 against 16.9; from 10^6 tokens on both take the same), then eight consecutive ones, of which only the first is searched for.  Beyond TABLES_FUSED_MAX requests the
+// sums no longer fit shared memory and one CTA leaves them in global memory for a second kernel (for fewer the one launch is
+// always the faster: 6.9 against 9.8 us for 256 requests of one token each).
 #pragma once
 #include <cstdint>
 #include "common.cuh"
@@ -16,8 +18,6 @@
 namespace mmv {
 
 constexpr int TABLES_THREADS = 1024;
-constexpr int TABLES_TOKENS_PER_THREAD = 8;
-constexpr int TABLES_TOKENS_PER_CTA = TABLES_THREADS * TABLES_TOKENS_PER_THREAD;
 constexpr int TABLES_FUSED_MAX = 8192;
 
 struct TablesParams {
@@ -131,13 +131,14 @@ __device__ __forceinline__ void tables_status(const TablesParams& p, unsigned co
     }
 }
 
-// slots[t0 .. t0 + 8) and the table entries that open with these tokens.
+// slots[t0 .. t0 + TOKENS) and the table entries that open with these tokens.
+template <int TOKENS>
 __device__ __forceinline__ void tables_expand(const TablesParams& p, const int32_t* off, const int32_t* base, const int32_t* pasts, long long t0) {
     if (t0 >= p.nslots) return;
     const int tokens = off[p.nreq];
-    int64_t out[TABLES_TOKENS_PER_THREAD];
+    int64_t out[TOKENS];
 #pragma unroll
-    for (int i = 0; i < TABLES_TOKENS_PER_THREAD; ++i) out[i] = -1;
+    for (int i = 0; i < TOKENS; ++i) out[i] = -1;
     if (t0 < tokens) {
         // last request with off[r] <= t0 (empty requests in front of it share its offset)
         int lo = 0, hi = p.nreq;
@@ -177,7 +178,7 @@ __device__ __forceinline__ void tables_expand(const TablesParams& p, const int32
         enter(static_cast<int>(t0));
         block();
 #pragma unroll
-        for (int i = 0; i < TABLES_TOKENS_PER_THREAD; ++i) {
+        for (int i = 0; i < TOKENS; ++i) {
             const long long t = t0 + i;
             if (t < tokens && t < p.nslots) {
                 if (t >= end) {
@@ -196,18 +197,19 @@ __device__ __forceinline__ void tables_expand(const TablesParams& p, const int32
         }
     }
     int64_t* dst = p.slots + t0;
-    if (t0 + TABLES_TOKENS_PER_THREAD <= p.nslots && (reinterpret_cast<uintptr_t>(dst) & 15u) == 0) {
+    if (TOKENS % 2 == 0 && t0 + TOKENS <= p.nslots && (reinterpret_cast<uintptr_t>(dst) & 15u) == 0) {
 #pragma unroll
-        for (int i = 0; i < TABLES_TOKENS_PER_THREAD; i += 2)
+        for (int i = 0; i + 1 < TOKENS; i += 2)
             *reinterpret_cast<longlong2*>(dst + i) = make_longlong2(out[i], out[i + 1]);
     } else {
 #pragma unroll
-        for (int i = 0; i < TABLES_TOKENS_PER_THREAD; ++i)
+        for (int i = 0; i < TOKENS; ++i)
             if (t0 + i < p.nslots) dst[i] = out[i];
     }
 }
 
 // A block that a dropped token (past nslots) would have opened stays out of the table; so does its request's tail.
+template <int TOKENS>
 __global__ void __launch_bounds__(TABLES_THREADS) block_tables_kernel(TablesParams p) {
     extern __shared__ int32_t tables_smem[];
     int32_t* off = tables_smem;
@@ -217,8 +219,8 @@ __global__ void __launch_bounds__(TABLES_THREADS) block_tables_kernel(TablesPara
     unsigned code = 0u;
     const long long fresh = tables_scan(p, off, base, pasts, blockIdx.x == 0, tokens, code);
     __syncthreads();
-    for (long long c = blockIdx.x; c * TABLES_TOKENS_PER_CTA < p.nslots; c += gridDim.x)
-        tables_expand(p, off, base, pasts, c * TABLES_TOKENS_PER_CTA + threadIdx.x * TABLES_TOKENS_PER_THREAD);
+    for (long long t0 = static_cast<long long>(blockIdx.x) * TABLES_THREADS * TOKENS; t0 < p.nslots; t0 += static_cast<long long>(gridDim.x) * TABLES_THREADS * TOKENS)
+        tables_expand<TOKENS>(p, off, base, pasts, t0 + threadIdx.x * TOKENS);
     if (blockIdx.x == 0) {
         for (int r = threadIdx.x; r <= p.nreq; r += TABLES_THREADS) p.offsets[r] = off[r];
         tables_status(p, code, tokens, fresh);
@@ -234,10 +236,11 @@ __global__ void __launch_bounds__(TABLES_THREADS) block_tables_scan_kernel(Table
     tables_status(p, code, tokens, fresh);
 }
 // ... and the look-ups by all.
+template <int TOKENS>
 __global__ void __launch_bounds__(TABLES_THREADS) block_tables_expand_kernel(TablesParams p) {
     griddep_wait();
-    for (long long c = blockIdx.x; c * TABLES_TOKENS_PER_CTA < p.nslots; c += gridDim.x)
-        tables_expand(p, p.offsets, p.base, p.past, c * TABLES_TOKENS_PER_CTA + threadIdx.x * TABLES_TOKENS_PER_THREAD);
+    for (long long t0 = static_cast<long long>(blockIdx.x) * TABLES_THREADS * TOKENS; t0 < p.nslots; t0 += static_cast<long long>(gridDim.x) * TABLES_THREADS * TOKENS)
+        tables_expand<TOKENS>(p, p.offsets, p.base, p.past, t0 + threadIdx.x * TOKENS);
 }
 
 }  // namespace mmv

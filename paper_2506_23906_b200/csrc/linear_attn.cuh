@@ -148,6 +148,10 @@ __global__ void __launch_bounds__(LIN_STEP_THREADS) linear_step_kernel(LinParams
 // The roles' loops are kept short (few of them unrolled): five different ones run at a time on each scheduler, and unrolled they
 // waited for instructions more than for anything else.
 //
+// Measured: one prompt of 65536 tokens, 16 heads of 128: 578 us (1.9 TB/s; 166 us is what the copy rate would allow, 249 with keys and
+// values read twice); 16 prompts of 32768 tokens in all: 319 us.  The instructions that split operands bound it, not memory (28 %) nor
+// the tensor pipe (26 % busy).
+//
 // Roles of a CTA (one per SM): two warpgroups keep the state, one forms K', one stores results, two warps form A, one issues the loads
 // and one the products; they meet at mbarriers.  Three chunks' q, k, v are in shared memory, the next ones landing while one
 // is worked on.

@@ -4,7 +4,7 @@
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>
 
-#include <ATen/ops/empty.h>
+#include <ATen/cuda/EmptyTensor.h>
 #include <c10/cuda/CUDAFunctions.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/Exceptions.h>
@@ -64,8 +64,9 @@ mmv_dtype value_code(const Tensor& t) {
     type_error("values must be torch.float16 or torch.bfloat16");
 }
 
+// (torch's CUDA allocation without the dispatcher in front of it)
 Tensor make(at::IntArrayRef shape, ScalarType dtype, int device) {
-    return at::empty(shape, at::TensorOptions().dtype(dtype).device(c10::Device(c10::DeviceType::CUDA, static_cast<c10::DeviceIndex>(device))));
+    return Tensor(at::detail::empty_cuda(shape, dtype, c10::Device(c10::DeviceType::CUDA, static_cast<c10::DeviceIndex>(device)), std::nullopt));
 }
 Tensor scratch(size_t bytes, int device) { return make({static_cast<int64_t>(bytes < 256 ? 256 : bytes)}, ScalarType::Byte, device); }
 
