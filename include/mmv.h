@@ -381,7 +381,8 @@ mmv_status mmv_seg_scan_host(const void *x_host, const void *flags_host, int64_t
  * Values that are not finite make the results they enter not finite; they never
  * reach another request's or sequence's, nor results that a length or a window
  * keeps them from.  Metadata pointers need the alignment of their type.  Unlike the calls above,
- * these enqueue kernels only and can be captured in a CUDA graph like them.
+ * these enqueue kernels only (a call without requests, a memset) and can be captured
+ * in a CUDA graph like them.
  * Calls on different streams may overlap; a workspace each, as above.
  * ------------------------------------------------------------------------- */
 
