@@ -869,7 +869,8 @@ linear_chunks_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_con
                     tc_commit(&bars.empty[o1 % C::kStages]);
                     ++o1;
                 }
-                if (o2 < count && mbar_try_wait(&bars.a_full, o2 & 1) && (o2 == 0 || mbar_try_wait(&bars.o_empty, (o2 - 1) & 1))) {
+                // (behind the chunk's update: its keys' warps have zeroed the rows of V that are another sequence's, which A's zeros meet here too)
+                if (2 * o2 + 1 < kv && mbar_try_wait(&bars.a_full, o2 & 1) && (o2 == 0 || mbar_try_wait(&bars.o_empty, (o2 - 1) & 1))) {
                     tc_fence_after_sync();
                     const uint64_t dv = lin_desc_mn(sm + (o2 % C::kStages) * C::kStage + C::kV, LIN_BOX);
                     uint64_t da = lin_desc_mn(sm + C::kA, LIN_BOX);

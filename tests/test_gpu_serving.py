@@ -532,6 +532,31 @@ def test_linear_attention_neighbours_that_are_not_finite(mmv):
 
 
 @pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("tail", [1, 31, 32, 33, 63])
+def test_linear_attention_neighbours_that_are_not_finite_in_long_ranges(mmv, dim, tail):
+    """Ranges of many chunks, so that a sequence's short last chunk runs between others: its rows behind the end hold the next sequence's NaN and
+    infinities, or those of rows that no sequence has.  Every other sequence keeps its results bit by bit, however often it runs."""
+    heads, lens = 16, [64 * (1 + 3 * s % 6) + tail for s in range(200)]
+    q, k, v, off, g, state = linear_case(dim + tail, lens, heads, heads, dim, dim, first=37, behind=50)
+    offsets = ints(off)
+    want, last = mmv.linear_attention(q, k, v, offsets, g, scale=0.1, state=state)
+    clean = torch.zeros(q.size(0), dtype=torch.bool, device="cuda")
+    for s in range(0, 200, 2):
+        clean[off[s]:off[s + 1]] = True
+    bad = [x.clone() for x in (q, k, v)]
+    for i, value in enumerate((float("nan"), float("inf"), -float("inf"))):
+        mask = ~clean
+        mask[::3] &= i == 0
+        mask[1::3] &= i == 1
+        mask[2::3] &= i == 2
+        for x in bad:
+            x[mask] = value
+    for _ in range(5):
+        out, last2 = mmv.linear_attention(*bad, offsets, g, scale=0.1, state=state)
+        assert torch.equal(out[clean], want[clean]) and torch.equal(last2[::2], last[::2])
+
+
+@pytest.mark.parametrize("dim", [64, 128])
 @pytest.mark.parametrize("bad", [float("nan"), float("inf"), -float("inf")])
 def test_linear_attention_later_tokens_do_not_reach_earlier_ones(mmv, dim, bad):
     """A value of v, k or q that is not finite reaches no result in front of its token, and no other column, row or sequence: those stay
