@@ -452,7 +452,8 @@ mmv_status mmv_kv_append(const void *k, int64_t k_stride_token, int64_t k_stride
  * cache (mmv_kv_append) and counted in lens.  out: nreq x heads x dim, the
  * cache's type; lse: nreq x heads fp32, or NULL.  A request of length 0 gives out 0
  * and lse -infinity.  Scores, weights and sums are fp32 (weights enter the second
- * product as sums of two 16-bit values); results do not depend on timing.
+ * product as sums of two 16-bit values, which hold 2^-16 of a weight, in fp16 no less
+ * than 2^-40 of the largest one); results do not depend on timing.
  * Entries of the cache outside the stated tokens are never read, whatever they
  * hold.  Never dereferenced, and recorded as MMV_ERR_INVALID_ARG in the workspace
  * (outputs of that request are then unspecified): a table entry outside

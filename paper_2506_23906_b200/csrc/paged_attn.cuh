@@ -47,7 +47,7 @@ struct PagedParams {
     // workspace
     WorkspaceHeader* hdr;
     int32_t* desc;                                       // [grid][4]: joined (request, head part) or -1, last CTA of it, error code
-    float* part_ml;                                      // [grid][2][2][PA_ROWS]: maximum, sum
+    float* part_ml;                                      // [grid][2][2][PA_ROWS]: maximum (less the kernel's LIFT), sum
     float* part_o;                                       // [grid][2][rows][dim]
 };
 
@@ -172,6 +172,9 @@ __global__ void __launch_bounds__(PA_THREADS) paged_attention_kernel(const Paged
     __shared__ int s_start[2];
     __shared__ long long s_skip;
     __shared__ float s_m[PA_WARPS][PA_ROWS], s_l[PA_WARPS][PA_ROWS];
+    // The exponent that the largest weight gets.  fp16 holds nothing under 2^-24: a pair of values that starts at 2^15 reaches 2^-40 of the
+    // largest weight, one that starts at 1 would lose all under 2^-25 of it.  bfloat16 has the range of fp32.
+    constexpr float LIFT = BF16 ? 0.f : 15.f;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     griddep_launch_dependents();
 
@@ -280,7 +283,7 @@ __global__ void __launch_bounds__(PA_THREADS) paged_attention_kernel(const Paged
 
     uint32_t qf[DP / 16][4];
     float o[DP / 8][4];
-    float m[2], l[2];
+    float m[2], l[2];                                                 // maximum less LIFT; sum of weights 2^(s - m)
     int seg = 0, stage = 0;
     bool begins = true;
     // (The first PA_STAGES turns only fetch: with one place in the code that does, its loop fits the instruction cache.)
@@ -332,7 +335,7 @@ __global__ void __launch_bounds__(PA_THREADS) paged_attention_kernel(const Paged
                 float top = fmaxf(fmaxf(s[0][2 * h], s[0][2 * h + 1]), fmaxf(s[1][2 * h], s[1][2 * h + 1]));
                 top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
                 top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
-                const float now = fmaxf(m[h], top);
+                const float now = fmaxf(m[h], top - LIFT);
                 const float base = now == -INFINITY ? 0.f : now;      // (no token yet: every weight is 2^-inf = 0)
                 const float fall = paged_exp2(m[h] - base);
                 m[h] = now;
@@ -341,8 +344,8 @@ __global__ void __launch_bounds__(PA_THREADS) paged_attention_kernel(const Paged
                 for (int n = 0; n < 2; ++n) {
                     const float a = paged_exp2(s[n][2 * h] - base), b = paged_exp2(s[n][2 * h + 1] - base);
                     sum += a + b;
-                    // The weights enter the product as the sum of two 16-bit values: rounded to one, their error would be as
-                    // large as the result's own rounding.
+                    // The weights enter the product as the sum of two 16-bit values (2^-16 of themselves, in fp16 at least 2^-40 of the
+                    // largest): rounded to one, their error would be as large as the result's own rounding.
                     hi[n * 2 + h] = pack_pair<BF16>(a, b);
                     const float2 back = unpack_pair<BF16>(hi[n * 2 + h]);
                     (SMALL ? hi[n * 2 + 1] : lo[n * 2 + h]) = pack_pair<BF16>(a - back.x, b - back.y);

@@ -385,6 +385,26 @@ def test_paged_attention_large_scores(mmv):
     check_paged(mmv, (q * 0, kc, vc, table, lens), torch.float16, 2.0)
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("heads,kv", [(8, 2), (32, 2)])
+@pytest.mark.parametrize("gap", [10.0, 14.0, 16.0, 17.5, 20.0])
+def test_paged_attention_dominant_tokens_without_a_value(mmv, dtype, heads, kv, gap):
+    """Tokens that take almost all of the weight and whose value is zero (four in 256, one for each warp of a tile): the result is made of weights of
+    e^-gap.  All of them have the same score and positive values, so the bound is one on the result itself."""
+    q, kc, vc, table, lens = paged_case(int(gap), [6000] * 24 + [700, 65], heads, kv, 64, 16, dtype, garbage=0.0)
+    q[:] = 0.0
+    q[..., 0] = 1.0
+    vc.abs_()
+    kc[..., 0] = 0.0
+    for r, n in enumerate(lens.tolist()):
+        j = torch.arange(n, device="cuda")
+        j = j[(j % 256 < 64) & (j % 16 == 0)]
+        page = table[r, j // 16].long()
+        kc[page, j % 16, :, 0] = gap
+        vc[page, j % 16] = 0.0
+    check_paged(mmv, (q, kc, vc, table, lens), dtype, 1.0)
+
+
 def test_paged_attention_not_finite_inside(mmv):
     """A NaN among a request's own values stays in that request and head group; scores of -infinity weigh nothing."""
     q, kc, vc, table, lens = paged_case(5, [300, 200, 9000], 4, 2, 64, 16, torch.float16, garbage=0.0)
