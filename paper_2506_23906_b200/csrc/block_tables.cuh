@@ -78,7 +78,7 @@ __device__ __forceinline__ long long tables_scan(const TablesParams& p, int32_t*
             if (totals) p.total[r] = x.total;
             b = x.need - x.had;
             if (x.bad) code = code ? code : 4u;                                       // MMV_ERR_BAD_SEGMENTS
-            if (x.need > p.max_blocks && b > 0)
+            if (x.need > p.max_blocks && a > 0)                                       // (the last new token's block, new or held, is past the row)
                 code = code ? code : 7u;                                              // MMV_ERR_OUT_OF_BLOCKS
         }
         long long ia = a, ib = b;

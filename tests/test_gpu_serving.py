@@ -139,6 +139,19 @@ def test_block_tables_that_do_not_fit(mmv, short):
         assert g == list(w)
 
 
+@pytest.mark.parametrize("many", [0, 9000])
+@pytest.mark.parametrize("past,added,status", [(40, 3, 7), (33, 15, 7), (31, 2, 7), (30, 2, 0), (40, 0, 0)])
+def test_block_tables_held_block_past_the_row(mmv, past, added, status, many):
+    """New tokens in a block that the request holds and its row does not reach: no slot, and reported (with requests enough for two kernels too)."""
+    past, added = [5] * many + [past, 8], [0] * many + [added, 2]
+    table = [[10 * r, 10 * r + 1] for r in range(many + 2)]
+    want = tables_plain(past, added, [900, 901, 902], table, 20, 16)
+    got, code = run_tables(mmv, past, added, [900, 901, 902], table, 20, 16)
+    assert code == status
+    for g, w in zip(got, want):
+        assert g == list(w)
+
+
 def test_block_tables_bad_lengths_are_reported(mmv):
     table = [[7, 8], [9, 10]]
     got, status = run_tables(mmv, [-4, 3], [5, -1], [1, 2], table, 5, 16)
