@@ -408,6 +408,9 @@ mmv_status mmv_seg_scan_host(const void *x_host, const void *flags_host, int64_t
  * nslots are dropped, and the workspace records MMV_ERR_OUT_OF_BLOCKS; a negative
  * length counts as 0, a total (of a request, or of added) beyond int32 is cut, and
  * MMV_ERR_BAD_SEGMENTS is recorded.  All outputs are integers and deterministic.
+ * total may be past or added themselves (a server's lengths, advanced in place);
+ * any other overlap of offsets, total, used or slots with past, added or
+ * free_blocks answers MMV_ERR_INVALID_ARG.
  * nreq < 2^20.  Workspace: mmv_block_tables_workspace_bytes(nreq), 256-byte aligned.
  */
 size_t mmv_block_tables_workspace_bytes(int64_t nreq);

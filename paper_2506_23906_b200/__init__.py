@@ -415,7 +415,7 @@ def block_tables(past: torch.Tensor, added: torch.Tensor, free_blocks: torch.Ten
     """mmv_block_tables: token offsets, slots and new block-table entries of a packed batch from the requests' lengths.
 
     past, added: int32 [nreq]; free_blocks: int32; table: int32 [nreq, max_blocks] (rows may be strided), completed in
-    place; slots: int64, written whole (-1 behind the last token).  Returns (offsets int32 [nreq + 1], total int32 [nreq],
+    place; slots: int64, written whole (-1 behind the last token); total may be past itself (lengths advanced in place).  Returns (offsets int32 [nreq + 1], total int32 [nreq],
     used int32 [1]: how many of free_blocks were taken)."""
     args = (past, added, free_blocks, table, slots, block_size, offsets, total, used, workspace)
     if stream is not None:

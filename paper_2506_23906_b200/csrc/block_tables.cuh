@@ -10,7 +10,8 @@
 // serves its own tokens: one per thread as long as that fits the SMs (a thread's tokens wait for each other's table
 // entries: 256 requests of one token 3.7 against 6.8 us, 8192 of 18 tokens 13.5 against 16.9; from 10^6 tokens on both take the same), then eight consecutive ones, of which only the first is searched for.  Beyond TABLES_FUSED_MAX requests the
 // sums no longer fit shared memory and one CTA leaves them in global memory for a second kernel (for fewer the one launch is
-// always the faster: 6.9 against 9.8 us for 256 requests of one token each).
+// always the faster: 6.9 against 9.8 us for 256 requests of one token each).  Where the totals go over the past or the added lengths
+// and several kernels or CTAs read those, one more kernel writes them at the end.
 #pragma once
 #include <cstdint>
 #include "common.cuh"
@@ -22,7 +23,7 @@ constexpr int TABLES_FUSED_MAX = 8192;
 
 struct TablesParams {
     const int32_t *past, *added, *free_blocks;
-    int32_t *table, *offsets, *total, *used;
+    int32_t *table, *offsets, *total, *used;                         // total null: left to block_tables_total_kernel
     int64_t* slots;
     long long nfree, table_stride, nslots;
     int nreq, block_size;
@@ -217,7 +218,7 @@ __global__ void __launch_bounds__(TABLES_THREADS) block_tables_kernel(TablesPara
     int32_t* pasts = base + p.nreq;
     long long tokens;
     unsigned code = 0u;
-    const long long fresh = tables_scan(p, off, base, pasts, blockIdx.x == 0, tokens, code);
+    const long long fresh = tables_scan(p, off, base, pasts, blockIdx.x == 0 && p.total, tokens, code);
     __syncthreads();
     for (long long t0 = static_cast<long long>(blockIdx.x) * TABLES_THREADS * TOKENS; t0 < p.nslots; t0 += static_cast<long long>(gridDim.x) * TABLES_THREADS * TOKENS)
         tables_expand<TOKENS>(p, off, base, pasts, t0 + threadIdx.x * TOKENS);
@@ -232,7 +233,7 @@ __global__ void __launch_bounds__(TABLES_THREADS) block_tables_scan_kernel(Table
     griddep_launch_dependents();
     long long tokens;
     unsigned code = 0u;
-    const long long fresh = tables_scan(p, p.offsets, p.base, nullptr, true, tokens, code);
+    const long long fresh = tables_scan(p, p.offsets, p.base, nullptr, p.total != nullptr, tokens, code);
     tables_status(p, code, tokens, fresh);
 }
 // ... and the look-ups by all.
@@ -241,6 +242,11 @@ __global__ void __launch_bounds__(TABLES_THREADS) block_tables_expand_kernel(Tab
     griddep_wait();
     for (long long t0 = static_cast<long long>(blockIdx.x) * TABLES_THREADS * TOKENS; t0 < p.nslots; t0 += static_cast<long long>(gridDim.x) * TABLES_THREADS * TOKENS)
         tables_expand<TOKENS>(p, p.offsets, p.base, p.past, t0 + threadIdx.x * TOKENS);
+}
+// The totals, in place of the lengths that they are made of.
+__global__ void __launch_bounds__(TABLES_THREADS) block_tables_total_kernel(TablesParams p, int32_t* total) {
+    const int r = blockIdx.x * TABLES_THREADS + threadIdx.x;
+    if (r < p.nreq) total[r] = tables_len(p, r).total;
 }
 
 }  // namespace mmv

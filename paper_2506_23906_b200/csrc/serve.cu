@@ -68,6 +68,10 @@ ServeDevice* serve_device() {
 inline bool aligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
 // a stride of an axis that holds more than one entry keeps its rows on 16-byte words
 inline bool word_stride(int64_t stride, int64_t extent) { return extent <= 1 || stride % 8 == 0; }
+inline bool overlap(const void* a, size_t abytes, const void* b, size_t bbytes) {
+    const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+    return abytes && bbytes && x < y + bbytes && y < x + abytes;
+}
 inline size_t round_up(size_t v, size_t a) { return (v + a - 1) / a * a; }
 
 // `after`: the kernel may start while the one in front of it in the stream still runs (it waits before it reads).
@@ -233,6 +237,17 @@ mmv_status mmv_block_tables(const int32_t* past, const int32_t* added, int64_t n
     if (nreq && max_blocks && (!table || !aligned(table, 4) || (nreq > 1 && table_stride < max_blocks))) return MMV_ERR_INVALID_ARG;
     if ((nfree && (!free_blocks || !aligned(free_blocks, 4))) || (nslots && (!slots || !aligned(slots, 8)))) return MMV_ERR_INVALID_ARG;
     if (workspace_bytes < mmv_block_tables_workspace_bytes(nreq)) return MMV_ERR_WORKSPACE_TOO_SMALL;
+    const size_t lens = static_cast<size_t>(nreq) * sizeof(int32_t);
+    const bool in_place = nreq && (total == past || total == added);
+    const auto meets = [&](const void* out, size_t bytes) {           // an input that other CTAs may still read
+        return overlap(out, bytes, past, lens) || overlap(out, bytes, added, lens) ||
+               overlap(out, bytes, free_blocks, static_cast<size_t>(nfree) * sizeof(int32_t));
+    };
+    if (meets(offsets, lens + sizeof(int32_t)) || meets(used, sizeof(int32_t)) || meets(slots, static_cast<size_t>(nslots) * sizeof(int64_t)))
+        return MMV_ERR_INVALID_ARG;
+    if ((total != past && overlap(total, lens, past, lens)) || (total != added && overlap(total, lens, added, lens)) ||
+        overlap(total, lens, free_blocks, static_cast<size_t>(nfree) * sizeof(int32_t)))
+        return MMV_ERR_INVALID_ARG;
     ServeDevice* dev = serve_device();
     if (!dev) return MMV_ERR_CUDA;
     cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
@@ -260,15 +275,21 @@ mmv_status mmv_block_tables(const int32_t* past, const int32_t* added, int64_t n
     if (ctas > dev->sm_count) ctas = dev->sm_count;
     if (ctas < 1) ctas = 1;
     const dim3 grid(static_cast<unsigned>(ctas));
-    if (nreq <= TABLES_FUSED_MAX) {
+    const bool fused = nreq <= TABLES_FUSED_MAX, late = in_place && !(fused && ctas == 1);      // (one CTA has its own copy of the lengths)
+    if (late) p.total = nullptr;
+    mmv_status rc;
+    if (fused) {
         const size_t smem = (3 * nreq + 1) * sizeof(int32_t);
-        return single ? launch(block_tables_kernel<1>, grid, TABLES_THREADS, smem, st, false, p)
-                      : launch(block_tables_kernel<8>, grid, TABLES_THREADS, smem, st, false, p);
+        rc = single ? launch(block_tables_kernel<1>, grid, TABLES_THREADS, smem, st, false, p)
+                    : launch(block_tables_kernel<8>, grid, TABLES_THREADS, smem, st, false, p);
+    } else {
+        rc = launch(block_tables_scan_kernel, dim3(1), TABLES_THREADS, 0, st, false, p);
+        if (rc == MMV_OK && nslots)
+            rc = single ? launch(block_tables_expand_kernel<1>, grid, TABLES_THREADS, 0, st, true, p)
+                        : launch(block_tables_expand_kernel<8>, grid, TABLES_THREADS, 0, st, true, p);
     }
-    const mmv_status rc = launch(block_tables_scan_kernel, dim3(1), TABLES_THREADS, 0, st, false, p);
-    if (rc != MMV_OK || nslots == 0) return rc;
-    return single ? launch(block_tables_expand_kernel<1>, grid, TABLES_THREADS, 0, st, true, p)
-                  : launch(block_tables_expand_kernel<8>, grid, TABLES_THREADS, 0, st, true, p);
+    if (rc != MMV_OK || !late) return rc;
+    return launch(block_tables_total_kernel, dim3(static_cast<unsigned>((nreq + TABLES_THREADS - 1) / TABLES_THREADS)), TABLES_THREADS, 0, st, false, p, total);
 }
 
 mmv_status mmv_kv_append(const void* k, int64_t k_stride_token, int64_t k_stride_head, const void* v, int64_t v_stride_token,

@@ -152,6 +152,25 @@ def test_block_tables_held_block_past_the_row(mmv, past, added, status, many):
         assert g == list(w)
 
 
+@pytest.mark.parametrize("n,tokens", [(1, 3), (300, 2), (700, 40), (5000, 3), (8192, 150), (8193, 0), (20000, 2)])
+@pytest.mark.parametrize("over", ["past", "added"])
+def test_block_tables_totals_over_the_lengths(mmv, n, tokens, over):
+    """total handed in as past, or as added: every result is that of a buffer of its own (one CTA, several, two kernels; no slots at all)."""
+    gen = torch.Generator("cuda").manual_seed(n)
+    past, added = (torch.randint(0, top + 1, (n,), device="cuda", generator=gen, dtype=torch.int32) for top in (100, tokens))
+    table = torch.randint(0, 1 << 20, (n, 40), device="cuda", generator=gen, dtype=torch.int32)
+    free = torch.randperm(1 << 20, device="cuda", generator=gen).to(torch.int32)
+    slots = torch.empty(int(added.sum()), dtype=torch.int64, device="cuda")
+    want_table, want_slots = table.clone(), slots.clone()
+    want = mmv.block_tables(past, added, free, want_table, want_slots, 8)
+    for _ in range(3):
+        p, a, t = past.clone(), added.clone(), table.clone()
+        slots.fill_(-7)
+        got = mmv.block_tables(p, a, free, t, slots, 8, total=p if over == "past" else a)
+        assert all(torch.equal(x, y) for x, y in zip(got, want)) and torch.equal(t, want_table) and torch.equal(slots, want_slots)
+        assert got[1].data_ptr() == (p if over == "past" else a).data_ptr() and torch.equal(*((a, added) if over == "past" else (p, past)))
+
+
 def test_block_tables_bad_lengths_are_reported(mmv):
     table = [[7, 8], [9, 10]]
     got, status = run_tables(mmv, [-4, 3], [5, -1], [1, 2], table, 5, 16)

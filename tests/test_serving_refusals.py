@@ -77,6 +77,18 @@ def test_block_tables(lib):
     assert lib.mmv_block_tables_workspace_bytes(100000) >= 256 + 400000
 
 
+def test_block_tables_outputs_over_inputs(lib):
+    """1000 requests; the first bytes or the last ones of an output meet an input that the kernels still read."""
+    past, added, free, n = 1 << 20, 1 << 21, 1 << 22, 1000
+    good = dict(past=past, added=added, nreq=n, block=16, free=free, nfree=n, table=1 << 23, stride=8, columns=8, offsets=1 << 24, total=1 << 25,
+                slots=1 << 26, nslots=n, used=1 << 27, ws=1 << 28, bytes=1 << 20, stream=None)
+    for name, size in [("offsets", 4 * (n + 1)), ("total", 4 * n), ("used", 4), ("slots", 8 * n)]:
+        for at in (past, added, free):
+            for where in (at + 8, at - size + 8, at if name != "total" or at == free else at + 4 * n - 8):
+                if where % 8 == 0 or name != "slots":
+                    assert lib.mmv_block_tables(*dict(good, **{name: where}).values()) == INVALID, (name, where - at)
+
+
 @pytest.mark.parametrize("change", BAD_CACHES)
 def test_caches(lib, change):
     c = cache(**change)
