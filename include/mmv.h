@@ -506,7 +506,7 @@ mmv_status mmv_linear_attention_step(const mmv_linear_inputs *in, int64_t nreq, 
  * in front of its first token S is state[s] (state NULL: zero) and behind its last
  * one S is written to state_out[s] (if not NULL; an empty sequence's state is copied):
  * [nseq, heads, dim_k, dim_v] fp32, 16-byte aligned, two buffers that do not
- * overlap.  This is the segmented scan of Problem 2.1 with a decay between the
+ * overlap (MMV_ERR_INVALID_ARG if they do).  This is the segmented scan of Problem 2.1 with a decay between the
  * elements, which here are the matrices k_t v_t^T, read out by q_t.
  * Values are bfloat16 (MMV_BF16_TO_F32; another dtype answers MMV_ERR_INVALID_ARG): scores and
  * states, which have no bound, are operands of the tensor core, and fp16's range

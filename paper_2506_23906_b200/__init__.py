@@ -461,7 +461,8 @@ def linear_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, offsets:
 
     q [tokens, heads, dim_k], k, v [tokens, kv_heads, dim_k / dim_v], bfloat16 (views are fine); offsets int32
     [sequences + 1]; log_decay fp32 [heads]; state fp32 [sequences, heads, dim_k, dim_v] in front of the first tokens (None:
-    zero).  Returns (out [tokens, heads, dim_v], state_out: the states behind the last tokens)."""
+    zero).  Returns (out [tokens, heads, dim_v], state_out: the states behind the last tokens).  Unlike the single-token form's,
+    state_out must not overlap state."""
     args = (q, k, v, offsets, log_decay, scale, state, out, state_out, workspace)
     if stream is not None:
         return _on_stream(_serve.linear_attention, stream, (q, k, v, offsets, log_decay, state, out, state_out, workspace), args)

@@ -438,6 +438,8 @@ mmv_status mmv_linear_attention(const mmv_linear_inputs* in, const int32_t* offs
     if (ntok && (!in->q || !in->k || !in->v || !out || !aligned(out, 16))) return MMV_ERR_INVALID_ARG;
     if ((state && !aligned(state, 16)) || (state_out && !aligned(state_out, 16))) return MMV_ERR_INVALID_ARG;
     if (workspace_bytes < mmv_linear_attention_workspace_bytes(in, nseq, ntok)) return MMV_ERR_WORKSPACE_TOO_SMALL;
+    const size_t states = static_cast<size_t>(nseq) * in->heads * in->dim_k * in->dim_v * sizeof(float);
+    if (state && state_out && overlap(state, states, state_out, states)) return MMV_ERR_INVALID_ARG;      // (a cut sequence's state is read by several CTAs)
     cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
     if (nseq == 0) return cudaMemsetAsync(workspace, 0, sizeof(WorkspaceHeader), st) == cudaSuccess ? MMV_OK : MMV_ERR_CUDA;
     ServeDevice* dev = serve_device();

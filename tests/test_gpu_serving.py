@@ -673,6 +673,17 @@ def test_linear_attention_bad_offsets_are_reported(mmv):
     assert mmv.last_async_status(ws) == 0
 
 
+def test_linear_attention_states_that_overlap_are_refused(mmv):
+    q, k, v, off, g, state = linear_case(9, [70, 5], 2, 2, 64, 64)
+    both = torch.zeros(3, *state.shape[1:], device="cuda")
+    both[:2] = state
+    for to in (both[:2], both[1:]):
+        with pytest.raises(mmv.MmvError):
+            mmv.linear_attention(q, k, v, ints(off), g, state=both[:2], state_out=to)
+    _, last = mmv.linear_attention(q, k, v, ints(off), g, state=both[:1].expand(2, -1, -1, -1).contiguous(), state_out=both[1:])
+    assert last.data_ptr() == both[1:].data_ptr()
+
+
 def test_linear_attention_nothing(mmv):
     q, k, v, off, g, state = linear_case(8, [4], 2, 2, 64, 64)
     out, last = mmv.linear_attention(q[:0], k[:0], v[:0], ints([0, 0]), g, state=state)

@@ -149,6 +149,13 @@ def test_linear_attention(lib):
     assert lib.mmv_linear_attention_workspace_bytes(i, -1, 5) == 0 and lib.mmv_linear_attention_workspace_bytes(i, 1, 1 << 31) == 0
 
 
+def test_linear_attention_states_that_overlap(lib):
+    i, size = ctypes.byref(inputs()), 4 * 5 * 4 * 64 * 64
+    need = lib.mmv_linear_attention_workspace_bytes(i, 5, 70)
+    for gap in (0, 16, size - 16, 16 - size, -16):
+        assert lib.mmv_linear_attention(i, 1 << 23, 5, 70, 1 << 24, 1.0, 1 << 25, (1 << 25) + gap, 1 << 27, 1 << 28, need, None) == INVALID, gap
+
+
 def test_linear_attention_step(lib):
     i = ctypes.byref(inputs())
     good = [i, 3, 16, 1.0, 16, 16, 16, 9, 16, None]
