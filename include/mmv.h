@@ -489,7 +489,8 @@ typedef struct {
  *     out = scale * q^T S'                      (nreq x heads x dim_v, the inputs' type)
  * S is state[s], S' is written to state_out[s], with s = slots[r] (int32; slots NULL:
  * s = r); both are [num_slots, heads, dim_k, dim_v] fp32, 16-byte aligned, and
- * may be the same buffer (the state is then updated in place).  A request whose s
+ * may be the same buffer (the state is then updated in place), but must not overlap
+ * otherwise (MMV_ERR_INVALID_ARG).  A request whose s
  * is outside [0, num_slots) has no state: its out is zero and nothing is kept.
  * Two requests must not share a state.  log_decay: heads fp32 values, any <= 0,
  * -infinity included (the state is then this token's alone).  No workspace.

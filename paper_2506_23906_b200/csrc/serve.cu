@@ -402,6 +402,8 @@ mmv_status mmv_linear_attention_step(const mmv_linear_inputs* in, int64_t nreq, 
     if (num_slots && (!state || !state_out || !aligned(state, 16) || !aligned(state_out, 16))) return MMV_ERR_INVALID_ARG;
     if (slots ? !aligned(slots, 4) : num_slots < nreq) return MMV_ERR_INVALID_ARG;
     if (nreq > INT32_MAX / (static_cast<int64_t>(in->heads) * 16)) return MMV_ERR_INVALID_ARG;       // one CTA per state and column part
+    const size_t states = static_cast<size_t>(num_slots) * in->heads * in->dim_k * in->dim_v * sizeof(float);
+    if (state != state_out && overlap(state, states, state_out, states)) return MMV_ERR_INVALID_ARG;      // (in place, or apart)
     ServeDevice* dev = serve_device();
     if (!dev) return MMV_ERR_CUDA;
     LinParams p = linear_params(in, log_decay, scale, out);

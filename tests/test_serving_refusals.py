@@ -167,6 +167,12 @@ def test_linear_attention_step(lib):
     assert lib.mmv_linear_attention_step(i, 0, None, 1.0, None, None, None, 0, None, None) == OK           # nothing to do
 
 
+def test_linear_attention_step_states_that_overlap(lib):
+    i, size = ctypes.byref(inputs()), 4 * 5 * 4 * 64 * 64
+    for gap in (16, size - 16, 16 - size, -16):
+        assert lib.mmv_linear_attention_step(i, 3, 1 << 24, 1.0, 1 << 25, (1 << 25) + gap, None, 5, 1 << 27, None) == INVALID, gap
+
+
 def test_strides_of_axes_with_one_entry_do_not_matter(lib):
     c = cache(num_blocks=1, block_size=1, heads=1, stride_block=3, stride_token=5, stride_head=7)
     assert lib.mmv_paged_attention_workspace_bytes(4, ctypes.byref(c)) > 0
