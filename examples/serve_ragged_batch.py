@@ -5,7 +5,8 @@
 One layer keeps a decayed state (linear attention), the other a paged key-value cache (softmax attention).  A step of the server
 is always the same five calls: block_tables (offsets, slots, new table entries), then per layer its projection and
 linear_attention or linear_attention_step, kv_append and paged_attention.  Weights are random.  --check recomputes the last
-step's logits from the whole token sequences with dense fp32 attention.
+step's logits from the whole token sequences with dense fp32 attention, for that run and for one whose requests add none, one or two
+tokens in a step.
 """
 from __future__ import annotations
 
@@ -19,6 +20,7 @@ sys.path.insert(0, str(Path(__file__).resolve().parent.parent))
 import paper_2506_23906_b200 as mmv  # noqa: E402
 
 VOCAB, WIDTH, HEADS, KV_HEADS, DIM, BLOCK = 512, 512, 8, 2, 64, 16
+PIECES = [[40, 0, 17], [1, 1, 1], [2, 0, 1], [0, 3, 0], [0, 1, 2], [1, 2, 0], [1, 1, 1]]       # --check: tokens of each request in each step
 
 
 def norm(x: torch.Tensor) -> torch.Tensor:
@@ -43,13 +45,14 @@ class Server:
         self.past = torch.zeros(requests, dtype=torch.int32, device="cuda")
         self.state = torch.zeros(requests, HEADS, DIM, DIM, device="cuda")
 
-    def step(self, tokens: torch.Tensor, added: torch.Tensor) -> torch.Tensor:
-        """tokens: the batch's new tokens, packed; added: how many of each request.  Returns every token's logits."""
-        n, requests = tokens.numel(), added.numel()
+    def step(self, tokens: torch.Tensor, counts: list[int]) -> torch.Tensor:
+        """tokens: the batch's new tokens, packed; counts: how many of each request.  Returns every token's logits."""
+        n, requests = tokens.numel(), len(counts)
+        added = torch.tensor(counts, dtype=torch.int32, device="cuda")
         slots = torch.empty(n, dtype=torch.int64, device="cuda")
         offsets, total, used = mmv.block_tables(self.past, added, self.free, self.table, slots, BLOCK)
         x = self.embed[tokens]
-        single = n == requests                                          # a decoding step: one token of every request
+        single = all(c == 1 for c in counts)                            # a decoding step: one token of every request
 
         q, k, v = (norm(x) @ self.lin_in).view(n, 3, HEADS, DIM).unbind(1)
         if single:
@@ -99,13 +102,30 @@ def serve(requests: int, steps: int, seed: int = 0):
     lens = (torch.randint(1, 200, (requests,), generator=g)).tolist()
     texts = [torch.randint(0, VOCAB, (n,), generator=g).cuda() for n in lens]
     server = Server(requests, max(lens) + steps + 1, seed)
-    logits = server.step(torch.cat(texts), torch.tensor(lens, dtype=torch.int32, device="cuda"))
+    logits = server.step(torch.cat(texts), lens)
     last = logits[torch.tensor(lens).cumsum(0) - 1]
-    ones = torch.ones(requests, dtype=torch.int32, device="cuda")
     for _ in range(steps):
         token = last.argmax(-1)
         texts = [torch.cat([t, token[r:r + 1]]) for r, t in enumerate(texts)]
-        last = server.step(token, ones)
+        last = server.step(token, [1] * requests)
+    return server, texts, last
+
+
+def serve_in_pieces(schedule: list[list[int]], seed: int = 0):
+    """Random tokens, schedule[i][r] of them from request r in step i (none of some is fine).  Returns what serve() does, every request's
+    logits from the last step that it had a token in."""
+    g = torch.Generator().manual_seed(seed)
+    requests = len(schedule[0])
+    server = Server(requests, sum(map(max, schedule)) + 1, seed)
+    texts, last = [torch.empty(0, dtype=torch.int64, device="cuda")] * requests, torch.zeros(requests, VOCAB, device="cuda")
+    for counts in schedule:
+        new = [torch.randint(0, VOCAB, (c,), generator=g).cuda() for c in counts]
+        texts = [torch.cat(t) for t in zip(texts, new)]
+        logits = server.step(torch.cat(new), counts)
+        ends = torch.tensor(counts).cumsum(0) - 1
+        for r, c in enumerate(counts):
+            if c:
+                last[r] = logits[ends[r]]
     return server, texts, last
 
 
@@ -124,11 +144,13 @@ def main() -> int:
     server, texts, last = serve(a.requests, a.steps)
     for r, t in enumerate(texts):
         print(f"request {r}: {t.numel()} tokens, the last ones {t[-min(a.steps, 8):].tolist()}")
+    fine = True
     if a.check:
-        off, own = difference(server, texts, last)
-        print(f"last logits against the dense fp32 model: relative difference {off:.2e}; of the dense model with rounded activations: {own:.2e}")
-        return 0 if off < 2 * own else 1
-    return 0
+        for name, run in (("prompts and single tokens", (server, texts, last)), ("pieces", serve_in_pieces(PIECES))):
+            off, own = difference(*run)
+            print(f"{name}: last logits against the dense fp32 model: relative difference {off:.2e}; of the dense model with rounded activations: {own:.2e}")
+            fine &= off < 2 * own
+    return 0 if fine else 1
 
 
 if __name__ == "__main__":

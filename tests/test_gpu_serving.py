@@ -772,3 +772,17 @@ def test_example_serves_a_ragged_batch(mmv):
     spec.loader.exec_module(ex)
     off, own = ex.difference(*ex.serve(5, 6, seed=3))
     assert off < 2 * own
+
+
+@pytest.mark.parametrize("schedule", [[[2, 0]], [[5, 30], [2, 0]], [[3, 1, 2], [1, 0, 2]], None])
+def test_example_serves_pieces(mmv, schedule):
+    """Steps in which some requests add no token and others several, as many in all as there are requests among them; the bound as above."""
+    import importlib.util
+    from pathlib import Path
+    spec = importlib.util.spec_from_file_location("serve_ragged_batch", Path(__file__).resolve().parent.parent / "examples" / "serve_ragged_batch.py")
+    ex = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(ex)
+    server, texts, last = ex.serve_in_pieces(schedule or ex.PIECES, seed=5)
+    there = [r for r, t in enumerate(texts) if t.numel()]
+    off, own = ex.difference(server, [texts[r] for r in there], last[there])
+    assert off < 2 * own
