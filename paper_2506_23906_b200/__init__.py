@@ -4,7 +4,7 @@ segmented sum and CSR SpMV on B200 (sm_100a).
 The binding only marshals arguments (ctypes, and an extension for the serving
 operators): torch supplies device memory and the current CUDA stream, every step of the computation runs in the library's own
 kernels.  There is no CPU or PyTorch fallback: if the shared library is missing
-the import of this module fails.
+the import of this module fails, and without the extension the first serving call does.
 """
 from __future__ import annotations
 
@@ -16,6 +16,7 @@ import torch
 
 _PKG = Path(__file__).resolve().parent
 LIB_PATH = _PKG / "libmmv.so"
+SERVE_PATH = _PKG / "_serve.so"
 
 # enums of include/mmv.h
 MMV_OK = 0
@@ -386,17 +387,28 @@ def spmv_csr(rowptr: torch.Tensor, col: torch.Tensor, val: torch.Tensor, x: torc
 # small extension (csrc/torch_binding.cpp), which also allocates what is not handed in.
 # ---------------------------------------------------------------------------
 def _load_serve():
-    path = _PKG / "_serve.so"
-    if not path.exists():
-        raise ImportError(f"{path} is missing: build it with `python paper_2506_23906_b200/build.py`.  There is no fallback path.")
-    spec = importlib.util.spec_from_file_location(__name__ + "._serve", path)
+    if not SERVE_PATH.exists():
+        raise ImportError(f"{SERVE_PATH} is missing: build it with `python paper_2506_23906_b200/build.py`.  There is no fallback path.")
+    spec = importlib.util.spec_from_file_location(__name__ + "._serve", SERVE_PATH)
     mod = importlib.util.module_from_spec(spec)
     spec.loader.exec_module(mod)
     mod.set_error(MmvError)
     return mod
 
 
-_serve = _load_serve()
+class _Serve:
+    """The extension, loaded at the first serving call (it is tied to one version of torch, which the other operators are not);
+    its functions are then this object's own attributes."""
+
+    def __getattr__(self, name: str):
+        if name.startswith("__"):
+            raise AttributeError(name)
+        mod = _load_serve()
+        vars(self).update((f, getattr(mod, f)) for f in dir(mod) if not f.startswith("_"))
+        return getattr(mod, name)
+
+
+_serve = _Serve()
 
 
 def _on_stream(call, stream, inputs, args):
