@@ -1,9 +1,11 @@
 """Builds libmmv.so (the C-ABI CUDA library, nvcc for sm_100a) and _serve.so (its binding to torch tensors) in-tree."""
 from __future__ import annotations
 
+import importlib.util
 import os
 import subprocess
 import sys
+import sysconfig
 from pathlib import Path
 
 PKG = Path(__file__).resolve().parent
@@ -16,12 +18,36 @@ BINDING_SOURCE = CSRC / "torch_binding.cpp"
 NVCC = os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")
 
 
-def needs_build() -> bool:
-    if not LIB.exists() or not BINDING.exists() or BINDING_SOURCE.stat().st_mtime > BINDING.stat().st_mtime:
-        return True
-    t = LIB.stat().st_mtime
-    deps = list(CSRC.glob("*.cu")) + list(CSRC.glob("*.cuh")) + list(CSRC.glob("*.h")) + list((PKG.parent / "include").glob("*.h"))
+HEADERS = PKG.parent / "include"
+
+
+def newer(deps, than: Path) -> bool:
+    t = than.stat().st_mtime
     return any(d.stat().st_mtime > t for d in deps)
+
+
+def needs_library() -> bool:
+    return not LIB.exists() or newer([*CSRC.glob("*.cu"), *CSRC.glob("*.cuh"), *CSRC.glob("*.h"), *HEADERS.glob("*.h")], LIB)
+
+
+def torch_dir() -> Path:
+    return Path(importlib.util.find_spec("torch").origin).parent
+
+
+def binding_made_for() -> str:
+    """What the extension is compiled against, besides its sources."""
+    return f"{sys.implementation.cache_tag}\n{(torch_dir() / 'version.py').read_text()}"
+
+
+def needs_binding() -> bool:
+    made = OBJ / "binding"
+    if not BINDING.exists() or not made.exists() or newer([BINDING_SOURCE, *HEADERS.glob("*.h")], BINDING):
+        return True
+    return made.read_text() != binding_made_for()
+
+
+def needs_build() -> bool:
+    return needs_library() or needs_binding()
 
 
 def stale(obj: Path, deps: Path) -> bool:
@@ -34,8 +60,14 @@ def stale(obj: Path, deps: Path) -> bool:
 
 
 def build(force: bool = False, verbose: bool = False) -> Path:
-    if not force and not needs_build():
-        return LIB
+    if force or needs_library():
+        build_library(force, verbose)
+    if force or needs_binding():
+        build_binding()
+    return LIB
+
+
+def build_library(force: bool = False, verbose: bool = False) -> Path:
     flags = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17", "-Xcompiler", "-fPIC", "-DNDEBUG"]
     flags += os.environ.get("MMV_NVCC_FLAGS", "").split()
     if verbose:
@@ -54,16 +86,12 @@ def build(force: bool = False, verbose: bool = False) -> Path:
     tmp = LIB.with_suffix(f".{os.getpid()}.tmp")
     subprocess.run([NVCC, "-gencode", "arch=compute_100a,code=sm_100a", "-shared", "-o", str(tmp), *(str(o) for _, o, _ in objs)], check=True)
     os.replace(tmp, LIB)
-    build_binding()
     return LIB
 
 
 def build_binding() -> Path:
     """The extension is linked to libmmv.so beside it; torch's libraries are the ones that the process has loaded."""
-    import importlib.util
-    import sysconfig
-
-    torch = Path(importlib.util.find_spec("torch").origin).parent
+    torch = torch_dir()
     cuda = Path(NVCC).resolve().parent.parent
     include = [torch / "include", torch / "include/torch/csrc/api/include", sysconfig.get_paths()["include"], cuda / "include"]
     tmp = BINDING.with_suffix(f".{os.getpid()}.tmp")
@@ -71,6 +99,8 @@ def build_binding() -> Path:
                     str(BINDING_SOURCE), f"-L{torch / 'lib'}", f"-L{PKG}", "-l:libmmv.so", "-lc10", "-lc10_cuda", "-ltorch_cpu", "-ltorch_cuda", "-ltorch_python",
                     "-Wl,-rpath,$ORIGIN"], check=True)
     os.replace(tmp, BINDING)
+    OBJ.mkdir(exist_ok=True)
+    (OBJ / "binding").write_text(binding_made_for())
     return BINDING
 
 
