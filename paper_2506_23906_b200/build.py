@@ -50,9 +50,9 @@ def needs_build() -> bool:
     return needs_library() or needs_binding()
 
 
-def stale(obj: Path, deps: Path) -> bool:
-    """Whether an object is older than its source or a file that it included when it was last compiled."""
-    if not obj.exists() or not deps.exists():
+def stale(obj: Path, deps: Path, made: Path, command: str) -> bool:
+    """Whether an object is older than its source or a file that it included when it was last compiled, or was compiled otherwise."""
+    if not obj.exists() or not deps.exists() or not made.exists() or made.read_text() != command:
         return True
     names = deps.read_text().replace("\\\n", " ").partition(":")[2].split()
     t = obj.stat().st_mtime
@@ -70,21 +70,22 @@ def build(force: bool = False, verbose: bool = False) -> Path:
 def build_library(force: bool = False, verbose: bool = False) -> Path:
     flags = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17", "-Xcompiler", "-fPIC", "-DNDEBUG"]
     flags += os.environ.get("MMV_NVCC_FLAGS", "").split()
-    if verbose:
-        flags += ["-Xptxas", "-v"]
     # one object per source, so that an edit recompiles (side by side) only the sources that include the edited file
-    objs = [(s, OBJ / f"{s.stem}.o", OBJ / f"{s.stem}.d") for s in SOURCES]
+    command = " ".join([NVCC, *flags])
+    objs = [(s, *(OBJ / f"{s.stem}.{end}" for end in ("o", "d", "flags"))) for s in SOURCES]
     OBJ.mkdir(exist_ok=True)
     part = f".{os.getpid()}.tmp"
-    running = [(subprocess.Popen([NVCC, *flags, "-MD", "-MF", f"{d}{part}", "-c", "-o", f"{o}{part}", str(s)]), o, d)
-               for s, o, d in objs if force or stale(o, d)]
-    if any([p.wait() for p, _, _ in running]):
+    running = [(subprocess.Popen([NVCC, *flags, *(["-Xptxas", "-v"] if verbose else []), "-MD", "-MF", f"{d}{part}", "-c", "-o", f"{o}{part}", str(s)]), o, d, made)
+               for s, o, d, made in objs if force or stale(o, d, made, command)]
+    if any([p.wait() for p, *_ in running]):
         raise RuntimeError("nvcc failed")
-    for _, o, d in running:
+    for _, o, d, made in running:
+        made.unlink(missing_ok=True)
         os.replace(f"{o}{part}", o)
         os.replace(f"{d}{part}", d)
+        made.write_text(command)
     tmp = LIB.with_suffix(f".{os.getpid()}.tmp")
-    subprocess.run([NVCC, "-gencode", "arch=compute_100a,code=sm_100a", "-shared", "-o", str(tmp), *(str(o) for _, o, _ in objs)], check=True)
+    subprocess.run([NVCC, "-gencode", "arch=compute_100a,code=sm_100a", "-shared", "-o", str(tmp), *(str(o) for _, o, *_ in objs)], check=True)
     os.replace(tmp, LIB)
     return LIB
 

@@ -112,3 +112,14 @@ def test_a_failed_extension_is_made_again(tree):
     (tree.root / "cxx.log.fail").unlink()
     tree.ran()
     assert tree.build()[2] == 1
+
+
+def test_other_flags_compile_every_object(tree):
+    """A library that is built at all is built whole with the flags of that build."""
+    tree.build()
+    tree.monkeypatch.setenv("MMV_NVCC_FLAGS", "-DOTHER")
+    tree.touch("pkg/csrc/serve.cu")
+    sources, links, _, calls = tree.build()
+    assert sources == ["api.cu", "serve.cu"] and links == 1 and sum("-DOTHER" in c for c in calls) == 2
+    tree.touch("pkg/csrc/serve.cu")
+    assert tree.build()[0] == ["serve.cu"]
