@@ -30,8 +30,9 @@ def needs_library() -> bool:
     return not LIB.exists() or newer([*CSRC.glob("*.cu"), *CSRC.glob("*.cuh"), *CSRC.glob("*.h"), *HEADERS.glob("*.h")], LIB)
 
 
-def torch_dir() -> Path:
-    return Path(importlib.util.find_spec("torch").origin).parent
+def torch_dir() -> Path | None:
+    spec = importlib.util.find_spec("torch")
+    return Path(spec.origin).parent if spec else None
 
 
 def binding_made_for() -> str:
@@ -40,6 +41,8 @@ def binding_made_for() -> str:
 
 
 def needs_binding() -> bool:
+    if torch_dir() is None:                         # (nothing to bind to: the C library alone)
+        return False
     made = OBJ / "binding"
     if not BINDING.exists() or not made.exists() or newer([BINDING_SOURCE, *HEADERS.glob("*.h")], BINDING):
         return True
@@ -62,7 +65,7 @@ def stale(obj: Path, deps: Path, made: Path, command: str) -> bool:
 def build(force: bool = False, verbose: bool = False) -> Path:
     if force or needs_library():
         build_library(force, verbose)
-    if force or needs_binding():
+    if torch_dir() is not None and (force or needs_binding()):
         build_binding()
     return LIB
 

@@ -123,3 +123,9 @@ def test_other_flags_compile_every_object(tree):
     assert sources == ["api.cu", "serve.cu"] and links == 1 and sum("-DOTHER" in c for c in calls) == 2
     tree.touch("pkg/csrc/serve.cu")
     assert tree.build()[0] == ["serve.cu"]
+
+
+def test_the_library_needs_no_torch(tree):
+    tree.monkeypatch.setattr(importlib.util, "find_spec", lambda name, *a: None)
+    assert tree.build()[:3] == (["api.cu", "serve.cu"], 1, 0)
+    assert not tree.mod.needs_build() and tree.build(force=True)[:3] == (["api.cu", "serve.cu"], 1, 0)
