@@ -384,7 +384,8 @@ def spmv_csr(rowptr: torch.Tensor, col: torch.Tensor, val: torch.Tensor, x: torc
 # Serving a language model over a ragged batch
 #
 # These calls take a few microseconds on the GPU in a decoding step; their tensors' metadata is read and checked by a
-# small extension (csrc/torch_binding.cpp), which also allocates what is not handed in.
+# small extension (csrc/torch_binding.cpp), which also allocates what is not handed in.  They have no backward pass: in grad mode
+# a tensor that requires a gradient is refused (RuntimeError).
 # ---------------------------------------------------------------------------
 def _load_serve():
     if not SERVE_PATH.exists():

@@ -5,6 +5,7 @@
 #include <Python.h>
 
 #include <ATen/cuda/EmptyTensor.h>
+#include <c10/core/GradMode.h>
 #include <c10/cuda/CUDAFunctions.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/Exceptions.h>
@@ -43,6 +44,13 @@ Tensor optional(PyObject* o, const char* name) { return o == Py_None ? Tensor() 
 void on_device(int device, std::initializer_list<const Tensor*> all) {
     for (const Tensor* t : all)
         if (t->defined() && (!t->is_cuda() || t->get_device() != device)) value_error("tensors must be on the current CUDA device");
+}
+// The operators have no backward pass: results without a gradient where one is expected are refused.
+void no_gradient(std::initializer_list<const Tensor*> all) {
+    if (!c10::GradMode::is_enabled()) return;
+    for (const Tensor* t : all)
+        if (t->defined() && t->requires_grad())
+            throw Bad{PyExc_RuntimeError, "no backward pass: call this under torch.no_grad(), or on tensors that require no gradient"};
 }
 void contiguous_of(const Tensor& t, ScalarType dtype, const char* name) {
     if (t.defined() && (t.scalar_type() != dtype || !t.is_contiguous()))
@@ -201,6 +209,7 @@ PyObject* kv_append(PyObject* const* a) {
     const Tensor &k = tensor(a[0], "k"), &v = tensor(a[1], "v"), &slots = tensor(a[2], "slots"), &kc = tensor(a[3], "k_cache"), &vc = tensor(a[4], "v_cache");
     const int dev = c10::cuda::current_device();
     on_device(dev, {&k, &v, &slots, &kc, &vc});
+    no_gradient({&k, &v, &kc, &vc});
     rows(k, "k");
     rows(v, "v");
     contiguous_of(slots, ScalarType::Long, "slots");
@@ -221,6 +230,7 @@ PyObject* paged_attention(PyObject* const* a) {
     Tensor out = optional(a[7], "out"), lse = optional(a[8], "lse"), ws = optional(a[9], "workspace");
     const int dev = c10::cuda::current_device();
     on_device(dev, {&q, &kc, &vc, &table, &lens, &out, &lse, &ws});
+    no_gradient({&q, &kc, &vc, &out, &lse});
     rows(q, "q");
     const int64_t n = q.size(0), heads = q.size(1), dim = q.size(2);
     const mmv_kv_cache cache = cache_of(kc, vc);
@@ -252,6 +262,7 @@ PyObject* linear_attention(PyObject* const* a) {
     Tensor state = optional(a[6], "state"), out = optional(a[7], "out"), last = optional(a[8], "state_out"), ws = optional(a[9], "workspace");
     const int dev = c10::cuda::current_device();
     on_device(dev, {&q, &k, &v, &offsets, &decay, &state, &out, &last, &ws});
+    no_gradient({&q, &k, &v, &decay, &state, &out, &last});
     const mmv_linear_inputs in = linear_of(q, k, v);
     const int64_t tokens = q.size(0), heads = q.size(1), dk = q.size(2), dv = v.size(2), nseq = offsets.numel() - 1;
     if (nseq < 0) value_error("offsets holds one entry more than there are sequences");
@@ -282,6 +293,7 @@ PyObject* linear_attention_step(PyObject* const* a) {
     if (!to.defined()) to = state;
     const int dev = c10::cuda::current_device();
     on_device(dev, {&q, &k, &v, &decay, &state, &slots, &to, &out});
+    no_gradient({&q, &k, &v, &decay, &state, &to, &out});
     const mmv_linear_inputs in = linear_of(q, k, v);
     const int64_t n = q.size(0), heads = q.size(1), dk = q.size(2), dv = v.size(2);
     contiguous_of(decay, ScalarType::Float, "log_decay");

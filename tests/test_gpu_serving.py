@@ -724,6 +724,28 @@ def test_binding_refusals(mmv):
         mmv.block_tables(ints([1]), ints([1]), ints([0]), torch.zeros(1, 4, dtype=torch.int32, device="cuda"), torch.zeros(4, dtype=torch.int64, device="cuda"), 0)
 
 
+def test_tensors_that_require_a_gradient(mmv):
+    """Refused in grad mode, each of them; the same call under no_grad gives the results of plain tensors."""
+    q, kc, vc, table, lens = paged_case(2, [5, 40], 4, 2, 64, 16, torch.bfloat16, garbage=0.0)
+    lq, lk, lv, off, g, state = linear_case(3, [3, 70], 4, 2, 64, 64)
+    slots = torch.arange(3, device="cuda")
+    calls = [(mmv.paged_attention, dict(q=q, k_cache=kc, v_cache=vc, table=table, lens=lens), ("q", "k_cache", "v_cache")),
+             (mmv.kv_append, dict(k=lk[:3], v=lv[:3], slots=slots, k_cache=kc.clone(), v_cache=vc.clone()), ("k", "v", "k_cache", "v_cache")),
+             (mmv.linear_attention, dict(q=lq, k=lk, v=lv, offsets=ints(off), log_decay=g, state=state), ("q", "k", "v", "log_decay", "state")),
+             (mmv.linear_attention_step, dict(q=lq[:2], k=lk[:2], v=lv[:2], log_decay=g, state=state, state_out=torch.empty_like(state)),
+              ("q", "k", "v", "log_decay", "state"))]
+    first = lambda r: r[0] if isinstance(r, tuple) else r                                                  # noqa: E731
+    for call, args, names in calls:
+        want = first(call(**args))
+        for name in names:
+            wanting = dict(args, **{name: args[name].detach().requires_grad_()})
+            with pytest.raises(RuntimeError, match="no_grad"):
+                call(**wanting)
+            with torch.no_grad():
+                got = first(call(**wanting))
+            assert got is None and want is None or torch.equal(got, want)
+
+
 def test_calls_on_another_stream_and_in_a_graph(mmv):
     """The same results on a side stream, and from a captured step replayed with new contents."""
     q, kc, vc, table, lens = paged_case(21, [300, 77, 4000], 8, 2, 64, 16, torch.bfloat16, garbage=0.0)
