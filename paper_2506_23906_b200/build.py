@@ -53,13 +53,13 @@ def needs_build() -> bool:
     return needs_library() or needs_binding()
 
 
-def stale(obj: Path, deps: Path, made: Path, command: str) -> bool:
-    """Whether an object is older than its source or a file that it included when it was last compiled, or was compiled otherwise."""
+def stale(source: Path, obj: Path, deps: Path, made: Path, command: str) -> bool:
+    """Whether an object is older than its source or a file that it included when it was last compiled, or was compiled otherwise or elsewhere."""
     if not obj.exists() or not deps.exists() or not made.exists() or made.read_text() != command:
         return True
     names = deps.read_text().replace("\\\n", " ").partition(":")[2].split()
     t = obj.stat().st_mtime
-    return not names or any(not Path(n).exists() or Path(n).stat().st_mtime > t for n in names if not n.startswith("/usr/"))
+    return str(source) not in names or any(not Path(n).exists() or Path(n).stat().st_mtime > t for n in names if not n.startswith("/usr/"))
 
 
 def build(force: bool = False, verbose: bool = False) -> Path:
@@ -79,7 +79,7 @@ def build_library(force: bool = False, verbose: bool = False) -> Path:
     OBJ.mkdir(exist_ok=True)
     part = f".{os.getpid()}.tmp"
     running = [(subprocess.Popen([NVCC, *flags, *(["-Xptxas", "-v"] if verbose else []), "-MD", "-MF", f"{d}{part}", "-c", "-o", f"{o}{part}", str(s)]), o, d, made)
-               for s, o, d, made in objs if force or stale(o, d, made, command)]
+               for s, o, d, made in objs if force or stale(s, o, d, made, command)]
     if any([p.wait() for p, *_ in running]):
         raise RuntimeError("nvcc failed")
     for _, o, d, made in running:

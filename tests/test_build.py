@@ -1,6 +1,7 @@
 """What build.py makes, and when: with compilers that only note what they were asked for."""
 import importlib.util
 import os
+import shutil
 from pathlib import Path
 
 import pytest
@@ -129,3 +130,18 @@ def test_the_library_needs_no_torch(tree):
     tree.monkeypatch.setattr(importlib.util, "find_spec", lambda name, *a: None)
     assert tree.build()[:3] == (["api.cu", "serve.cu"], 1, 0)
     assert not tree.mod.needs_build() and tree.build(force=True)[:3] == (["api.cu", "serve.cu"], 1, 0)
+
+
+def test_a_copied_tree_compiles_its_own_sources(tree, tmp_path):
+    """Objects that were copied with the tree say nothing of the copy's sources."""
+    tree.build()
+    copy = tmp_path / "copy"
+    shutil.copytree(tree.root / "pkg", copy / "pkg")
+    shutil.copytree(tree.root / "include", copy / "include")
+    spec = importlib.util.spec_from_file_location("_build_of_the_copy", copy / "pkg" / "build.py")
+    mod = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(mod)
+    assert not mod.needs_library()
+    (copy / "pkg" / "csrc" / "serve.cu").write_text("// changed")
+    mod.build()
+    assert "serve.cu" in tree.ran()[0]
