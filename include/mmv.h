@@ -493,7 +493,8 @@ typedef struct {
  * otherwise (MMV_ERR_INVALID_ARG).  A request whose s
  * is outside [0, num_slots) has no state: its out is zero and nothing is kept.
  * Two requests must not share a state.  log_decay: heads fp32 values, any <= 0,
- * -infinity included (the state is then this token's alone).  No workspace.
+ * -infinity included (the state is then this token's alone, if S was finite: a
+ * decay of 0 does not hide what is not).  No workspace.
  */
 mmv_status mmv_linear_attention_step(const mmv_linear_inputs *in, int64_t nreq, const float *log_decay, float scale,
                                      const float *state, float *state_out, const int32_t *slots, int64_t num_slots,

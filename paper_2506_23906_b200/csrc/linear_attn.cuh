@@ -148,9 +148,10 @@ __global__ void __launch_bounds__(LIN_STEP_THREADS) linear_step_kernel(LinParams
 // The roles' loops are kept short (few of them unrolled): five different ones run at a time on each scheduler, and unrolled they
 // waited for instructions more than for anything else.
 //
-// Measured: one prompt of 65536 tokens, 16 heads of 128: 578 us (1.9 TB/s; 166 us is what the copy rate would allow, 249 with keys and
-// values read twice); 16 prompts of 32768 tokens in all: 319 us.  The instructions that split operands bound it, not memory (28 %) nor
-// the tensor pipe (26 % busy).
+// Measured: one prompt of 65536 tokens, 16 heads of 128: 565 to 588 us (1.9 TB/s; 166 us is what the copy rate would allow, 249 with keys and
+// values read twice); 16 prompts of 32768 tokens in all: 307 to 327 us.  Neither memory (28 %) nor the tensor pipe (26 % busy) bounds it:
+// without the splits of the keys the first kernel takes 120 instead of 170 us and the second 285 instead of 331; the rest is roles that
+// wait for one another.
 //
 // Roles of a CTA (one per SM): two warpgroups keep the state, one forms K', one stores results, two warps form A, one issues the loads
 // and one the products; they meet at mbarriers.  Three chunks' q, k, v are in shared memory, the next ones landing while one
@@ -159,7 +160,8 @@ __global__ void __launch_bounds__(LIN_STEP_THREADS) linear_step_kernel(LinParams
 // Split: the list of (sequence, head, chunk) is cut into equal contiguous ranges, one per CTA.  A range that ends inside a
 // (sequence, head) hands its state on; a first, short kernel (CARRY: the same code with keys and values only) computes what the
 // part behind its last start adds to a state, and a range that starts inside one sums the decayed contributions of the
-// ranges in front of it.  Batches of many sequences are hardly cut; one long prompt reads its keys and values twice.  A range is no
+// ranges in front of it.  One long prompt reads its keys and values twice; of a batch, the part of a cut (sequence, head) that lies in front of
+// a range's end is, and the first kernel lasts as long as the longest such part.  A range is no
 // shorter than half the root of the longest sequence's number of chunks: a sequence of n chunks cut into m ranges takes n / m
 // chunks' time and up to m contributions', and of these two a chunk takes about twice as long.
 // ---------------------------------------------------------------------------------------------------------------------

@@ -161,8 +161,8 @@ __device__ __forceinline__ bool paged_next(const PagedParams& p, PagedIter& it) 
 }
 
 // SMALL: up to 8 query heads per key head.  Their rows fill half of the product; the other half takes what rounding the
-// weights to 16 bits left of them, so that one product does for both (4 requests of 131072 tokens, 32/8 heads of 128: 419 -> 341 us; 64 requests
-// of up to 4096: 123 -> 100 us).
+// weights to 16 bits left of them, so that one product does for both (4 requests of 131072 tokens, 32/8 heads of 128: 386 -> 340 us; 64 requests
+// of up to 4096: 119 -> 98 us; both sides on one GPU, others take up to a tenth more).
 template <bool BF16, int DP, bool SMALL>
 __global__ void __launch_bounds__(PA_THREADS) paged_attention_kernel(const PagedParams p) {
     using C = PagedCfg<DP>;
