@@ -471,6 +471,84 @@ mmv_status mmv_paged_attention(const void *q, int64_t q_stride_request, int64_t 
                                void *out, float *lse, void *workspace, size_t workspace_bytes, void *cuda_stream);
 
 /*
+ * A paged key-value cache in 8 bits, with a scale for each block of tokens and
+ * head: the code at k[b * stride_block + i * stride_token + h * stride_head + c]
+ * (bytes) stands for code * k_scale[b * scale_stride_block + h * scale_stride_head],
+ * and the same of the values.  code: MMV_CODE_INT8 (-127 to 127) or
+ * MMV_CODE_E4M3 (finite up to 448).  Any order of the axes; dim is a multiple of
+ * 16 up to 256, the codes' strides are multiples of 16 and k, v 16-byte aligned;
+ * the scales are fp32, >= 0, any strides.
+ */
+typedef enum { MMV_CODE_INT8 = 0, MMV_CODE_E4M3 = 1 } mmv_code;
+typedef struct {
+    void *k, *v;
+    float *k_scale, *v_scale;
+    int64_t num_blocks;
+    int64_t stride_block, stride_token, stride_head;
+    int64_t scale_stride_block, scale_stride_head;
+    int32_t block_size, heads, dim, code;
+} mmv_kv_cache_q8;
+
+/*
+ * Quantises the keys and values of a packed batch into the cache.  Request r's
+ * new tokens are the rows [offsets[r], offsets[r + 1]) of k and v; they are its
+ * LAST tokens: it holds total[r] of them with these, and its token p is in block
+ * table[r, p / block_size] (offsets, total and table as mmv_block_tables leaves
+ * them).  With amax the largest magnitude of the new keys (values) of one block
+ * and head, top = 127 or 448, and old the scale of a block that the call
+ * CONTINUES (its place 0 is not among the new tokens; 0 for one that it begins):
+ *     amax <= old * top:  the scale stays old
+ *     otherwise           int8: amax / top, rounded up to 11 significant bits
+ *                         e4m3: the smallest power of two >= amax / top
+ *                         and the codes at the places in front of the new ones
+ *                         become code * old / scale, rounded like new ones
+ *     new codes           x / scale; int8: to the nearest whole number, halves away
+ *                         from zero; e4m3: to the nearest, halves to even
+ * so that everything but a converted code is rounded once.  Magnitudes below 2^-100 count as 0
+ * (scale 0, codes 0).  A new value that is not finite, or an old scale that is
+ * not >= 0 and finite, makes the scale of its block and head (of the keys or of the
+ * values) NaN: they read as NaN until the block is begun anew.  Results are
+ * deterministic.  k, v: ntok rows of heads x dim, fp16 or bfloat16 (dtype), token
+ * and head strides of their own; they must not overlap the cache.  Rows behind
+ * offsets[nreq] (a padded batch) are ignored, and so are tokens without a
+ * place: a table entry outside [0, num_blocks), a block past max_blocks, a total
+ * smaller than what is added, offsets that leave [0, ntok].  The last block of a request must
+ * not be another's too.  ntok < 2^31, nreq < 2^20.  No workspace.
+ */
+mmv_status mmv_kv_append_q8(const void *k, int64_t k_stride_token, int64_t k_stride_head, const void *v, int64_t v_stride_token,
+                            int64_t v_stride_head, mmv_dtype dtype, int64_t ntok, const int32_t *offsets, const int32_t *total,
+                            int64_t nreq, const int32_t *table, int64_t table_stride, int64_t max_blocks,
+                            const mmv_kv_cache_q8 *cache, void *cuda_stream);
+
+/*
+ * Reads the first tokens of every request back in 16 bits, packed: row
+ * offsets[r] + p of k_out and v_out (ntok x heads x dim, contiguous, fp16 or
+ * bfloat16) is request r's token p, for p < offsets[r + 1] - offsets[r]: code *
+ * scale, rounded once.  Rows in front of offsets[0] and behind offsets[nreq] are
+ * not written; a token without a page (see above) reads as zero.
+ * ntok < 2^31, nreq < 2^20.  No workspace.
+ */
+mmv_status mmv_kv_read_q8(const mmv_kv_cache_q8 *cache, const int32_t *table, int64_t table_stride, int64_t max_blocks,
+                          const int32_t *offsets, int64_t nreq, int64_t ntok, mmv_dtype dtype, void *k_out, void *v_out,
+                          void *cuda_stream);
+
+/*
+ * mmv_paged_attention over a cache in 8 bits: the same arguments, results and
+ * reports, with keys and values code * scale.  dtype: q's and out's type.  Codes
+ * enter the products exactly; a value's scale enters with its weight, and a
+ * weight with its scale is a sum of two fp16 values (2^-22 of it, no less than
+ * 2^-40 of the request's and head's largest such product).  A bfloat16 query's columns below 2^-29
+ * of its head's largest one lose accuracy, and below 2^-39 count as 0.  Scales that are NaN or negative make the
+ * results that read their block NaN.
+ */
+size_t mmv_paged_attention_q8_workspace_bytes(int32_t heads, const mmv_kv_cache_q8 *cache);
+mmv_status mmv_paged_attention_q8(const void *q, int64_t q_stride_request, int64_t q_stride_head, int32_t heads,
+                                  mmv_dtype dtype, const mmv_kv_cache_q8 *cache, const int32_t *table,
+                                  int64_t table_stride, int64_t max_blocks, const int32_t *lens, int64_t nreq,
+                                  float scale, int64_t window, void *out, float *lse, void *workspace,
+                                  size_t workspace_bytes, void *cuda_stream);
+
+/*
  * Inputs of linear attention: q [.., heads, dim_k], k [.., kv_heads, dim_k],
  * v [.., kv_heads, dim_v] with a token (or request) in front, token and head
  * strides of their own.  heads is a multiple of kv_heads: query head h uses key /

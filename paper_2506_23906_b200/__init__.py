@@ -34,6 +34,7 @@ EXPORTS = (
     "mmv_block_tables_workspace_bytes", "mmv_block_tables", "mmv_kv_append", "mmv_linear_attention_step",
     "mmv_paged_attention_workspace_bytes", "mmv_paged_attention",
     "mmv_linear_attention_workspace_bytes", "mmv_linear_attention",
+    "mmv_kv_append_q8", "mmv_kv_read_q8", "mmv_paged_attention_q8_workspace_bytes", "mmv_paged_attention_q8",
 )
 SHARD_SUMMARY_BYTES = 16
 STATIC_SCAN_MAX_N = 1 << 28
@@ -460,6 +461,49 @@ def paged_attention(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tenso
     if stream is not None:
         return _on_stream(_serve.paged_attention, stream, (q, k_cache, v_cache, table, lens, out, lse, workspace), args)
     return _serve.paged_attention(*args, None)
+
+
+def kv_append_q8(k: torch.Tensor, v: torch.Tensor, offsets: torch.Tensor, total: torch.Tensor, table: torch.Tensor, k_cache: torch.Tensor,
+                 v_cache: torch.Tensor, k_scale: torch.Tensor, v_scale: torch.Tensor, stream=None) -> None:
+    """mmv_kv_append_q8: quantises the keys and values k, v [tokens, heads, dim] of a packed batch (views are fine) into the paged
+    caches [blocks, block_size, heads, dim] (int8 or float8_e4m3fn; any order in memory, rows contiguous), a code standing for
+    code * scale with k_scale, v_scale fp32 [blocks, heads].
+
+    offsets int32 [requests + 1], total int32 [requests] and table int32 [requests, max_blocks] as block_tables gives them: request
+    r's rows are its last tokens, of total[r].  A block that a request goes on in keeps its scale where the new tokens fit; else the
+    scale grows and the codes in front of them are converted."""
+    args = (k, v, offsets, total, table, k_cache, v_cache, k_scale, v_scale)
+    if stream is not None:
+        return _on_stream(_serve.kv_append_q8, stream, args, args)
+    return _serve.kv_append_q8(*args, None)
+
+
+def kv_read_q8(k_cache: torch.Tensor, v_cache: torch.Tensor, k_scale: torch.Tensor, v_scale: torch.Tensor, table: torch.Tensor, offsets: torch.Tensor,
+               tokens: int, dtype: torch.dtype = torch.bfloat16, k: torch.Tensor | None = None, v: torch.Tensor | None = None, stream=None):
+    """mmv_kv_read_q8: the first offsets[r + 1] - offsets[r] tokens of every request r, read back from caches in 8 bits.
+
+    table int32 [requests, max_blocks], offsets int32 [requests + 1].  Returns (k, v) [tokens, heads, dim] of `dtype` (float16 or bfloat16),
+    request r's from row offsets[r] on; rows outside [offsets[0], offsets[requests]) are not written."""
+    args = (k_cache, v_cache, k_scale, v_scale, table, offsets, tokens, dtype, k, v)
+    if stream is not None:
+        return _on_stream(_serve.kv_read_q8, stream, (k_cache, v_cache, k_scale, v_scale, table, offsets, k, v), args)
+    return _serve.kv_read_q8(*args, None)
+
+
+def paged_attention_q8_workspace_bytes(heads: int, k_cache: torch.Tensor, v_cache: torch.Tensor, k_scale: torch.Tensor, v_scale: torch.Tensor) -> int:
+    """mmv_paged_attention_q8_workspace_bytes of a call with `heads` query heads over these caches."""
+    return _serve.paged_attention_q8_workspace_bytes(heads, k_cache, v_cache, k_scale, v_scale)
+
+
+def paged_attention_q8(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor, k_scale: torch.Tensor, v_scale: torch.Tensor, table: torch.Tensor,
+                       lens: torch.Tensor, scale: float | None = None, window: int = 0, out: torch.Tensor | None = None,
+                       lse: torch.Tensor | None = None, workspace: torch.Tensor | None = None, stream=None):
+    """mmv_paged_attention_q8: paged_attention over caches in 8 bits (int8 or float8_e4m3fn [blocks, block_size, kv_heads, dim], scales
+    fp32 [blocks, kv_heads]); q float16 or bfloat16.  Returns (out, lse) as paged_attention does."""
+    args = (q, k_cache, v_cache, k_scale, v_scale, table, lens, scale, window, out, lse, workspace)
+    if stream is not None:
+        return _on_stream(_serve.paged_attention_q8, stream, (q, k_cache, v_cache, k_scale, v_scale, table, lens, out, lse, workspace), args)
+    return _serve.paged_attention_q8(*args, None)
 
 
 def linear_attention_workspace_bytes(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, sequences: int) -> int:

@@ -12,7 +12,7 @@ PKG = Path(__file__).resolve().parent
 CSRC = PKG / "csrc"
 LIB = PKG / "libmmv.so"
 OBJ = PKG / "build"
-SOURCES = [CSRC / "api.cu", CSRC / "serve.cu"]
+SOURCES = sorted(CSRC.glob("*.cu"))
 BINDING = PKG / "_serve.so"
 BINDING_SOURCE = CSRC / "torch_binding.cpp"
 NVCC = os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")

@@ -1,0 +1,343 @@
+// A paged key-value cache in 8 bits with a scale for each block of tokens and head: the quantising write and the read in 16 bits.
+//
+// A code stands for code * scale.  With top = 127 (int8) or 448 (e4m3) and amax the largest magnitude of a (block, head):
+//     int8   scale = amax / top rounded up to 11 significant bits;  code = x / scale to the nearest whole number, halves away from zero
+//     e4m3   scale = the smallest power of two >= amax / top;       code = x / scale to the nearest e4m3 value, halves to even
+// Both are reproducible bit by bit from products alone.  e4m3: x / scale is exact.  int8: x and scale have at most 11 significant bits, so that
+// x / scale = X / S (integers) differs from n + 1/2 = N / 2 by |2X - NS| / 2S, which is 0 or at least 2^-19 of it (2X < 2^12 or, for a
+// held code being converted, 2 code S < 2^19).  x times the rounded reciprocal times 1 + 2^-21 is off by 2^-21 +- 2^-23: every half goes
+// away from zero and nothing else changes its side.  The product is rounded once, by the fused sum that puts it in a float's low bits.
+#pragma once
+#include <cstdint>
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <cuda_fp8.h>
+#include "common.cuh"
+
+namespace mmv {
+
+struct CacheQ8 {
+    uint8_t* code[2];                                        // keys, values
+    float* scale[2];
+    long long block, tok, head;                              // strides of the codes
+    long long s_block, s_head;                               // and of the scales
+    long long num_blocks;
+    int block_size, heads, dim;
+};
+
+constexpr float Q8_TINY = 7.888609052210118e-31f;            // 2^-100: magnitudes below it are held as zero (1 / scale stays finite)
+constexpr float Q8_MAGIC = 12582912.f;                       // 1.5 * 2^23: a sum's low bits are the addend as an integer
+
+template <bool E4M3>
+__device__ __forceinline__ float q8_scale_of(float amax) {
+    if (amax < Q8_TINY) return 0.f;
+    if constexpr (E4M3) {                                    // amax / 448 = m 2^e with 1 <= m < 2: 2^e if m is 1, else 2^(e + 1)
+        const uint32_t b = __float_as_uint(__fdiv_rn(amax, 448.f));
+        return __uint_as_float((b + 0x7fffffu) & 0x7f800000u);
+    } else {
+        const uint32_t b = __float_as_uint(__fdiv_rn(amax, 127.f));
+        return __uint_as_float((b + 0x1fffu) & ~0x1fffu);    // (up at the 13th bit from below: 11 bits are left)
+    }
+}
+// what a value is multiplied with in front of q8_code
+template <bool E4M3>
+__device__ __forceinline__ float q8_inverse(float scale) {
+    if (!(scale > 0.f)) return 0.f;
+    const float r = __frcp_rn(scale);
+    return E4M3 ? r : r * (1.f + 4.76837158203125e-7f);      // 1 + 2^-21
+}
+// four codes in a word
+template <bool E4M3>
+__device__ __forceinline__ uint32_t q8_pack(float a, float b, float c, float d, float inv) {
+    if constexpr (E4M3) {
+        const uint32_t lo = __nv_cvt_float2_to_fp8x2(make_float2(a * inv, b * inv), __NV_SATFINITE, __NV_E4M3);
+        const uint32_t hi = __nv_cvt_float2_to_fp8x2(make_float2(c * inv, d * inv), __NV_SATFINITE, __NV_E4M3);
+        return lo | (hi << 16);
+    } else {
+        const uint32_t ab = __byte_perm(__float_as_uint(fmaf(a, inv, Q8_MAGIC)), __float_as_uint(fmaf(b, inv, Q8_MAGIC)), 0x0040);
+        const uint32_t cd = __byte_perm(__float_as_uint(fmaf(c, inv, Q8_MAGIC)), __float_as_uint(fmaf(d, inv, Q8_MAGIC)), 0x0040);
+        return __byte_perm(ab, cd, 0x5410);
+    }
+}
+// the numbers that four codes are (without their scale)
+template <bool E4M3>
+__device__ __forceinline__ float4 q8_unpack(uint32_t w) {
+    if constexpr (E4M3) {
+        const float2 a = __half22float2(__half2(__nv_cvt_fp8x2_to_halfraw2(static_cast<__nv_fp8x2_storage_t>(w & 0xffffu), __NV_E4M3)));
+        const float2 b = __half22float2(__half2(__nv_cvt_fp8x2_to_halfraw2(static_cast<__nv_fp8x2_storage_t>(w >> 16), __NV_E4M3)));
+        return make_float4(a.x, a.y, b.x, b.y);
+    } else {                                                 // 2^23 + 128 + code, less that
+        const uint32_t u = w ^ 0x80808080u;
+        constexpr float off = 8388608.f + 128.f;
+        return make_float4(__uint_as_float(__byte_perm(u, 0x4b000000u, 0x7440)) - off, __uint_as_float(__byte_perm(u, 0x4b000000u, 0x7441)) - off,
+                           __uint_as_float(__byte_perm(u, 0x4b000000u, 0x7442)) - off, __uint_as_float(__byte_perm(u, 0x4b000000u, 0x7443)) - off);
+    }
+}
+template <bool BF16>
+__device__ __forceinline__ float2 q8_widen(uint32_t w) {
+    if constexpr (BF16) return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u));
+    else return __half22float2(*reinterpret_cast<const __half2*>(&w));
+}
+template <bool BF16>
+__device__ __forceinline__ uint32_t q8_narrow(float a, float b) {
+    if constexpr (BF16) {
+        const __nv_bfloat162 x = __floats2bfloat162_rn(a, b);
+        return *reinterpret_cast<const uint32_t*>(&x);
+    } else {
+        const __half2 x = __floats2half2_rn(a, b);
+        return *reinterpret_cast<const uint32_t*>(&x);
+    }
+}
+
+// How many of offsets[1 .. n] are <= t: the sequence that token t belongs to (n: none).  32 samples per trip to memory; any values in
+// offsets give a result in [0, n].
+__device__ __forceinline__ int q8_sequence_of(const int32_t* offsets, int n, int t) {
+    const int lane = threadIdx.x & 31;
+    int lo = 0, len = n;
+    while (len > 0) {
+        const int step = (len + 31) >> 5, i = (lane + 1) * step - 1;
+        const int c = __popc(__ballot_sync(0xffffffffu, i < len && offsets[lo + i + 1] <= t));
+        lo += c * step;
+        len = min(step - 1, len - c * step);
+    }
+    return lo;
+}
+
+// ---------------------------------------------------------------------------------------------------------------------
+// The write.  3 bytes of traffic per value: bound by HBM for prompts, by the launch and a chain of dependent trips (offsets, page,
+// old scale, store) for a decoding step.
+//
+// Split: a unit is (window of tokens, head, keys or values), taken by a group of threads (a warp where a run is short, else the CTA); a
+// group takes the RUNS that begin in its window.  A run is a request's tokens that lie in one block: all that a scale depends on
+// besides the old one, so that no unit meets another's and nothing has to be joined.  The run's values are loaded once and stay in
+// registers (Q8_KEEP elements of 16 per thread; what is longer is read a second time, from the L2) between the maximum and the codes.
+// ---------------------------------------------------------------------------------------------------------------------
+constexpr int Q8_THREADS = 128;
+constexpr int Q8_KEEP = 4;
+
+struct AppendQ8Params {
+    CacheQ8 c;
+    const uint16_t* x[2];
+    long long x_tok[2], x_head[2];
+    const int32_t *offsets, *total, *table;
+    long long table_stride, max_blocks;
+    int nreq, ntok, window;
+    long long units;
+};
+
+template <bool BF16, bool E4M3, bool WARP>
+__global__ void __launch_bounds__(Q8_THREADS) kv_append_q8_kernel(const AppendQ8Params p) {
+    constexpr int G = WARP ? 32 : Q8_THREADS;
+    constexpr float top = E4M3 ? 448.f : 127.f;
+    __shared__ uint32_t s_max[2][Q8_THREADS / 32];
+    const int me = threadIdx.x % G, per = p.c.dim / 16;      // elements of 16 values per row
+    const long long unit = static_cast<long long>(blockIdx.x) * (Q8_THREADS / G) + threadIdx.x / G;
+    if (unit >= p.units) return;
+    const int head = static_cast<int>(unit % p.c.heads), kv = static_cast<int>(unit / p.c.heads % 2);
+    const int t0 = static_cast<int>(unit / (2 * p.c.heads)) * p.window, t1 = min(p.ntok, t0 + p.window);       // (below 2^31: window divides it up)
+    const uint16_t* x = p.x[kv] + head * p.x_head[kv];
+    uint8_t* codes = p.c.code[kv] + head * p.c.head;
+    float* scales = p.c.scale[kv] + head * p.c.s_head;
+    int turn = 0;
+    for (int t = t0; t < t1;) {
+        const int r = q8_sequence_of(p.offsets, p.nreq, t);
+        if (r >= p.nreq) return;
+        const int lo = p.offsets[r], hi = p.offsets[r + 1];
+        if (lo < 0 || hi > p.ntok || hi <= t) return;        // (not offsets: nothing is written)
+        if (lo > t) {                                        // tokens in front of the first request
+            t = lo;
+            continue;
+        }
+        const long long past = static_cast<long long>(p.total[r]) - (hi - lo), at = past + (t - lo);
+        if (past < 0) {
+            t = hi;
+            continue;
+        }
+        const int b = static_cast<int>(static_cast<uint32_t>(at) / static_cast<uint32_t>(p.c.block_size)), place = static_cast<int>(at - static_cast<long long>(b) * p.c.block_size);
+        const int len = min(p.c.block_size - place, hi - t);
+        const int first = t;
+        t += len;
+        if (place > 0 && first > lo) continue;               // the run began in an earlier window
+        if (b >= p.max_blocks) continue;
+        const long long page = p.table[r * p.table_stride + b];
+        if (page < 0 || page >= p.c.num_blocks) continue;
+        float* scale = scales + page * p.c.s_block;
+        const float old = place > 0 ? *scale : 0.f;
+
+        // the run's values and their largest magnitude (as bits: a NaN is above infinity)
+        const int n = len * per;
+        uint4 w[Q8_KEEP][2];
+        uint32_t most = 0u;
+        const auto load = [&](int i, uint4 (&v)[2]) {
+            const int row = i / per, col = i - row * per;
+            const uint4* src = reinterpret_cast<const uint4*>(x + (first + row) * p.x_tok[kv] + col * 16);
+            v[0] = src[0];
+            v[1] = src[1];
+        };
+        const auto widest = [&](const uint4 (&v)[2]) {
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                most = __vmaxu2(most, v[j].x & 0x7fff7fffu);
+                most = __vmaxu2(most, v[j].y & 0x7fff7fffu);
+                most = __vmaxu2(most, v[j].z & 0x7fff7fffu);
+                most = __vmaxu2(most, v[j].w & 0x7fff7fffu);
+            }
+        };
+#pragma unroll
+        for (int i = 0; i < Q8_KEEP; ++i)
+            if (me + i * G < n) load(me + i * G, w[i]);
+#pragma unroll
+        for (int i = 0; i < Q8_KEEP; ++i)
+            if (me + i * G < n) widest(w[i]);
+        for (int i = me + Q8_KEEP * G; i < n; i += G) {
+            uint4 v[2];
+            load(i, v);
+            widest(v);
+        }
+        most = __reduce_max_sync(0xffffffffu, max(most & 0xffffu, most >> 16));
+        if constexpr (!WARP) {
+            if ((threadIdx.x & 31) == 0) s_max[turn][threadIdx.x / 32] = most;
+            __syncthreads();
+#pragma unroll
+            for (int i = 0; i < Q8_THREADS / 32; ++i) most = max(most, s_max[turn][i]);
+            turn ^= 1;                                       // (the next run's maxima go elsewhere: one barrier per run is enough)
+        }
+        const bool wild = most >= (BF16 ? 0x7f80u : 0x7c00u) || !(old >= 0.f && old < INFINITY);
+        const float amax = q8_widen<BF16>(most).x;
+        const float now = wild ? __uint_as_float(0x7fc00000u) : amax <= old * top ? old : q8_scale_of<E4M3>(amax);
+        const float inv = q8_inverse<E4M3>(now);             // (0 for a scale that is 0 or NaN: the codes are 0)
+        uint8_t* dst = codes + page * p.c.block;
+        if (place > 0 && now > old) {                        // the scale grows: the codes in front of the run are converted
+            for (int i = me; i < place * per; i += G) {
+                const int row = i / per, col = i - row * per;
+                uint4* q = reinterpret_cast<uint4*>(dst + row * p.c.tok + col * 16);
+                uint4 v = *q;
+                uint32_t* word = reinterpret_cast<uint32_t*>(&v);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const float4 y = q8_unpack<E4M3>(word[j]);
+                    word[j] = q8_pack<E4M3>(y.x * old, y.y * old, y.z * old, y.w * old, inv);
+                }
+                *q = v;
+            }
+        }
+        const auto store = [&](int i, const uint4 (&v)[2]) {
+            const int row = i / per, col = i - row * per;
+            uint32_t out[4];
+            const uint32_t in[8] = {v[0].x, v[0].y, v[0].z, v[0].w, v[1].x, v[1].y, v[1].z, v[1].w};
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const float2 a = q8_widen<BF16>(in[2 * j]), c = q8_widen<BF16>(in[2 * j + 1]);
+                out[j] = wild ? 0u : q8_pack<E4M3>(a.x, a.y, c.x, c.y, inv);
+            }
+            *reinterpret_cast<uint4*>(dst + (place + row) * p.c.tok + col * 16) = make_uint4(out[0], out[1], out[2], out[3]);
+        };
+#pragma unroll
+        for (int i = 0; i < Q8_KEEP; ++i)
+            if (me + i * G < n) store(me + i * G, w[i]);
+        for (int i = me + Q8_KEEP * G; i < n; i += G) {
+            uint4 v[2];
+            load(i, v);
+            store(i, v);
+        }
+        if constexpr (WARP) __syncwarp();                    // (every lane has read the old scale)
+        if (me == 0 && !(now == old && place > 0)) *scale = now;
+    }
+}
+
+// ---------------------------------------------------------------------------------------------------------------------
+// The read: 1 byte in, 2 out per value, HBM.  A warp takes `tile` (up to 32) tokens of the packed result; lane i finds where token i lies,
+// then the warp moves the rows' words of 16 values, keys and values side by side.
+// ---------------------------------------------------------------------------------------------------------------------
+constexpr int READ_Q8_THREADS = 256;
+constexpr int READ_Q8_UNROLL = 2;
+
+struct ReadQ8Params {
+    CacheQ8 c;
+    uint16_t* out[2];                                        // [token, heads, dim]
+    const int32_t *offsets, *table;
+    long long table_stride, max_blocks;
+    int nreq, ntok, tile;
+    int words;                                               // of a token: heads * dim / 16
+    uint32_t by_words, by_head;                              // ceil(2^32 / words), ceil(2^32 / (dim / 16)); 0 for a divisor of 1
+};
+// n / d for n * d < 2^32, by the reciprocal above
+__device__ __forceinline__ int q8_quotient(int n, uint32_t by) { return by ? static_cast<int>(__umulhi(static_cast<uint32_t>(n), by)) : n; }
+
+template <bool BF16, bool E4M3>
+__global__ void __launch_bounds__(READ_Q8_THREADS) kv_read_q8_kernel(const ReadQ8Params p) {
+    const int lane = threadIdx.x & 31;
+    const long long warps = static_cast<long long>(gridDim.x) * (READ_Q8_THREADS / 32);
+    const long long tiles = (static_cast<long long>(p.ntok) + p.tile - 1) / p.tile;
+    for (long long i = static_cast<long long>(blockIdx.x) * (READ_Q8_THREADS / 32) + threadIdx.x / 32; i < tiles; i += warps) {
+        const int t0 = static_cast<int>(i * p.tile), held = min(p.tile, p.ntok - t0), t = t0 + lane;
+        int r = q8_sequence_of(p.offsets, p.nreq, t0);
+        if (r >= p.nreq) return;                             // behind the last sequence
+        // where token t lies: -2 behind the sequences or in front of them (not written), -1 without a page (zero)
+        long long codes = -2, scales = 0;
+        if (lane < held) {
+            int hi = p.nreq;                                 // the first sequence from r on that ends behind t
+            if (p.offsets[r + 1] > t) hi = r;
+            while (r < hi) {
+                const int mid = (r + hi) >> 1;
+                if (p.offsets[mid + 1] > t) hi = mid;
+                else r = mid + 1;
+            }
+            if (r < p.nreq && p.offsets[r] <= t && p.offsets[r] >= 0) {
+                const uint32_t at = static_cast<uint32_t>(t - p.offsets[r]), b = at / static_cast<uint32_t>(p.c.block_size);
+                const long long page = b < p.max_blocks ? p.table[r * p.table_stride + b] : -1;
+                codes = -1;
+                if (page >= 0 && page < p.c.num_blocks) {
+                    codes = page * p.c.block + (at - b * static_cast<uint32_t>(p.c.block_size)) * p.c.tok;
+                    scales = page * p.c.s_block;
+                }
+            }
+        }
+        const int n = held * p.words, per = p.c.dim / 16;
+#pragma unroll 1
+        for (int j0 = 0; j0 < n; j0 += 32 * READ_Q8_UNROLL) {
+            uint4 w[READ_Q8_UNROLL][2];
+            float s[READ_Q8_UNROLL][2];
+            long long dst[READ_Q8_UNROLL];
+#pragma unroll
+            for (int u = 0; u < READ_Q8_UNROLL; ++u) {
+                const int j = j0 + u * 32 + lane, row = q8_quotient(j, p.by_words);
+                const long long at = __shfl_sync(0xffffffffu, codes, row & 31), sc = __shfl_sync(0xffffffffu, scales, row & 31);
+                dst[u] = -1;
+                if (j < n && at >= -1) {
+                    const int c = j - row * p.words, head = q8_quotient(c, p.by_head), col = c - head * per;
+                    dst[u] = (static_cast<long long>(t0) * p.words + j) * 16;
+#pragma unroll
+                    for (int kv = 0; kv < 2; ++kv) {
+                        w[u][kv] = make_uint4(0u, 0u, 0u, 0u);
+                        s[u][kv] = 0.f;
+                        if (at >= 0) {
+                            w[u][kv] = *reinterpret_cast<const uint4*>(p.c.code[kv] + at + head * p.c.head + col * 16);
+                            s[u][kv] = p.c.scale[kv][sc + head * p.c.s_head];
+                        }
+                    }
+                }
+            }
+#pragma unroll
+            for (int u = 0; u < READ_Q8_UNROLL; ++u) {
+                if (dst[u] < 0) continue;
+#pragma unroll
+                for (int kv = 0; kv < 2; ++kv) {
+                    const uint32_t in[4] = {w[u][kv].x, w[u][kv].y, w[u][kv].z, w[u][kv].w};
+                    uint32_t out[8];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const float4 y = q8_unpack<E4M3>(in[e]);
+                        out[2 * e] = q8_narrow<BF16>(y.x * s[u][kv], y.y * s[u][kv]);
+                        out[2 * e + 1] = q8_narrow<BF16>(y.z * s[u][kv], y.w * s[u][kv]);
+                    }
+                    uint4* to = reinterpret_cast<uint4*>(p.out[kv] + dst[u]);
+                    to[0] = make_uint4(out[0], out[1], out[2], out[3]);
+                    to[1] = make_uint4(out[4], out[5], out[6], out[7]);
+                }
+            }
+        }
+    }
+}
+
+}  // namespace mmv

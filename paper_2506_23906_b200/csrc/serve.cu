@@ -1,9 +1,7 @@
 // Host side of the serving operators of include/mmv.h: argument checks, workspace carve-up and launches.
-#include <atomic>
 #include <cstdint>
 #include <cuda.h>
 #include <cuda_runtime.h>
-#include <mutex>
 
 #include "../../include/mmv.h"
 #include "common.cuh"
@@ -12,24 +10,12 @@
 #include "kv_cache.cuh"
 #include "linear_attn.cuh"
 #include "paged_attn.cuh"
+#include "serve_host.h"
 
 namespace mmv {
 namespace {
 
-constexpr int kMaxDevices = 64;
-constexpr int kMaxHeads = 1024;
-
-struct ServeDevice {
-    std::mutex lock;
-    std::atomic<bool> ok{false};
-    int sm_count = 0;
-};
 ServeDevice g_serve[kMaxDevices];
-
-template <typename K>
-bool allow_smem(K kernel, int bytes) {
-    return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes) == cudaSuccess;
-}
 
 template <int DP>
 bool allow_paged() {
@@ -40,61 +26,18 @@ bool allow_paged() {
 
 constexpr int kTablesSmemMax = (3 * TABLES_FUSED_MAX + 1) * static_cast<int>(sizeof(int32_t));
 
-// One-time set-up of the current device (only success is remembered).
+// One-time set-up of the current device.
 ServeDevice* serve_device() {
-    int dev = 0;
-    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= kMaxDevices) return nullptr;
-    ServeDevice* d = &g_serve[dev];
-    if (d->ok.load(std::memory_order_acquire)) return d;
-    std::lock_guard<std::mutex> guard(d->lock);
-    if (d->ok.load(std::memory_order_relaxed)) return d;
-    int sm = 0;
-    if (cudaDeviceGetAttribute(&sm, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) return nullptr;
-    d->sm_count = sm;
-    bool ok = allow_smem(block_tables_kernel<1>, kTablesSmemMax) && allow_smem(block_tables_kernel<8>, kTablesSmemMax);
-    ok &= allow_paged<64>() && allow_paged<128>() && allow_paged<256>();
-    ok &= allow_smem(linear_chunks_kernel<64, true>, LinCfg<64, true>::kSmemBytes);
-    ok &= allow_smem(linear_chunks_kernel<64, false>, LinCfg<64, false>::kSmemBytes);
-    ok &= allow_smem(linear_chunks_kernel<128, true>, LinCfg<128, true>::kSmemBytes);
-    ok &= allow_smem(linear_chunks_kernel<128, false>, LinCfg<128, false>::kSmemBytes);
-    if (!ok) {
-        cudaGetLastError();
-        return nullptr;
-    }
-    d->ok.store(true, std::memory_order_release);
-    return d;
+    return device_once(g_serve, [] {
+        bool ok = allow_smem(block_tables_kernel<1>, kTablesSmemMax) && allow_smem(block_tables_kernel<8>, kTablesSmemMax);
+        ok &= allow_paged<64>() && allow_paged<128>() && allow_paged<256>();
+        ok &= allow_smem(linear_chunks_kernel<64, true>, LinCfg<64, true>::kSmemBytes);
+        ok &= allow_smem(linear_chunks_kernel<64, false>, LinCfg<64, false>::kSmemBytes);
+        ok &= allow_smem(linear_chunks_kernel<128, true>, LinCfg<128, true>::kSmemBytes);
+        ok &= allow_smem(linear_chunks_kernel<128, false>, LinCfg<128, false>::kSmemBytes);
+        return ok;
+    });
 }
-
-inline bool aligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
-// a stride of an axis that holds more than one entry keeps its rows on 16-byte words
-inline bool word_stride(int64_t stride, int64_t extent) { return extent <= 1 || stride % 8 == 0; }
-inline bool overlap(const void* a, size_t abytes, const void* b, size_t bbytes) {
-    const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
-    return abytes && bbytes && x < y + bbytes && y < x + abytes;
-}
-inline size_t round_up(size_t v, size_t a) { return (v + a - 1) / a * a; }
-
-// `after`: the kernel may start while the one in front of it in the stream still runs (it waits before it reads).
-template <typename... KP, typename... A>
-mmv_status launch(void (*kernel)(KP...), dim3 grid, int threads, size_t smem, cudaStream_t st, bool after, const A&... args) {
-    cudaLaunchConfig_t cfg{};
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[0].val.programmaticStreamSerializationAllowed = 1;
-    cfg.gridDim = grid;
-    cfg.blockDim = dim3(static_cast<unsigned>(threads));
-    cfg.dynamicSmemBytes = smem;
-    cfg.stream = st;
-    cfg.attrs = attr;
-    cfg.numAttrs = after ? 1 : 0;
-    const cudaError_t err = cudaLaunchKernelEx(&cfg, kernel, args...);
-    ++g_launches;
-    if (err == cudaSuccess) return MMV_OK;
-    cudaGetLastError();
-    return MMV_ERR_CUDA;
-}
-
-inline bool value_type(int dt) { return dt == MMV_F16_TO_F32 || dt == MMV_BF16_TO_F32; }
 
 mmv_status check_cache(const mmv_kv_cache* c) {
     if (!c || !value_type(c->dtype)) return MMV_ERR_INVALID_ARG;
@@ -138,21 +81,8 @@ LinParams linear_params(const mmv_linear_inputs* in, const float* log_decay, flo
     return p;
 }
 
-// Query heads of one key head in parts of up to PA_ROWS, of nearly equal size.
-struct PagedHeads {
-    int group, parts, rows;
-};
-PagedHeads paged_heads(int heads, int kv_heads) {
-    PagedHeads h;
-    h.group = heads / kv_heads;
-    h.parts = (h.group + PA_ROWS - 1) / PA_ROWS;
-    h.rows = (h.group + h.parts - 1) / h.parts;
-    return h;
-}
-int paged_padded(int dim) { return dim <= 64 ? 64 : dim <= 128 ? 128 : 256; }
 // Resident CTAs per SM: what the shared memory of PA_ROWS rows allows (111, 57 and 220 KB of 227).
 int paged_per_sm(int padded) { return padded == 64 ? 3 : padded == 128 ? 2 : 1; }
-constexpr int kPagedMaxSms = 160;
 
 struct PagedPlan {
     size_t desc_off, ml_off, o_off, total;
@@ -329,7 +259,7 @@ mmv_status mmv_kv_append(const void* k, int64_t k_stride_token, int64_t k_stride
 
 size_t mmv_paged_attention_workspace_bytes(int32_t heads, const mmv_kv_cache* cache) {
     if (check_cache(cache) != MMV_OK || heads < 1 || heads > kMaxHeads || heads % cache->heads) return 0;
-    return paged_plan(paged_heads(heads, cache->heads), cache->dim).total;
+    return paged_plan(paged_heads(heads, cache->heads, PA_ROWS), cache->dim).total;
 }
 
 mmv_status mmv_paged_attention(const void* q, int64_t q_stride_request, int64_t q_stride_head, int32_t heads, const mmv_kv_cache* cache,
@@ -343,7 +273,7 @@ mmv_status mmv_paged_attention(const void* q, int64_t q_stride_request, int64_t 
     if (nreq && (!q || !aligned(q, 16) || !lens || !aligned(lens, 4) || !out || !aligned(out, 16) || (lse && !aligned(lse, 4))))
         return MMV_ERR_INVALID_ARG;
     if (nreq && max_blocks && (!table || !aligned(table, 4) || (nreq > 1 && table_stride < max_blocks))) return MMV_ERR_INVALID_ARG;
-    const PagedHeads h = paged_heads(heads, cache->heads);
+    const PagedHeads h = paged_heads(heads, cache->heads, PA_ROWS);
     const PagedPlan plan = paged_plan(h, cache->dim);
     if (workspace_bytes < plan.total) return MMV_ERR_WORKSPACE_TOO_SMALL;
     cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);

@@ -8,6 +8,7 @@
 #include <c10/core/GradMode.h>
 #include <c10/cuda/CUDAFunctions.h>
 #include <c10/cuda/CUDAStream.h>
+#include <torch/csrc/Dtype.h>
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
 
@@ -146,6 +147,33 @@ mmv_kv_cache cache_of(const Tensor& k, const Tensor& v) {
     return c;
 }
 
+mmv_kv_cache_q8 cache_q8_of(const Tensor& k, const Tensor& v, const Tensor& ks, const Tensor& vs) {
+    if (k.dim() != 4 || k.sizes() != v.sizes() || k.strides() != v.strides() || k.scalar_type() != v.scalar_type())
+        value_error("k_cache and v_cache must be alike: [blocks, block_size, heads, dim]");
+    if (k.scalar_type() != ScalarType::Char && k.scalar_type() != ScalarType::Float8_e4m3fn) type_error("the caches must be torch.int8 or torch.float8_e4m3fn");
+    if (k.size(3) > 1 && k.stride(3) != 1) value_error("the caches' last axis must be contiguous");
+    if (k.size(1) > INT32_MAX || k.size(2) > INT32_MAX || k.size(3) > INT32_MAX) value_error("the caches' axes do not fit 32 bits");
+    if (ks.scalar_type() != ScalarType::Float || vs.scalar_type() != ScalarType::Float) type_error("k_scale and v_scale must be torch.float32");
+    if (ks.dim() != 2 || ks.size(0) != k.size(0) || ks.size(1) != k.size(2) || ks.sizes() != vs.sizes() || ks.strides() != vs.strides())
+        value_error("k_scale and v_scale must be alike: [blocks, heads]");
+    mmv_kv_cache_q8 c;
+    c.k = k.data_ptr();
+    c.v = v.data_ptr();
+    c.k_scale = ks.data_ptr<float>();
+    c.v_scale = vs.data_ptr<float>();
+    c.num_blocks = k.size(0);
+    c.stride_block = k.stride(0);
+    c.stride_token = k.stride(1);
+    c.stride_head = k.stride(2);
+    c.scale_stride_block = ks.stride(0);
+    c.scale_stride_head = ks.stride(1);
+    c.block_size = static_cast<int32_t>(k.size(1));
+    c.heads = static_cast<int32_t>(k.size(2));
+    c.dim = static_cast<int32_t>(k.size(3));
+    c.code = k.scalar_type() == ScalarType::Char ? MMV_CODE_INT8 : MMV_CODE_E4M3;
+    return c;
+}
+
 mmv_linear_inputs linear_of(const Tensor& q, const Tensor& k, const Tensor& v) {
     rows(q, "q");
     rows(k, "k");
@@ -256,6 +284,92 @@ PyObject* paged_attention(PyObject* const* a) {
     return wrap({out, lse});
 }
 
+// k, v, offsets, total, table, k_cache, v_cache, k_scale, v_scale, stream
+PyObject* kv_append_q8(PyObject* const* a) {
+    const Tensor &k = tensor(a[0], "k"), &v = tensor(a[1], "v"), &offsets = tensor(a[2], "offsets"), &total = tensor(a[3], "total"), &table = tensor(a[4], "table"),
+                 &kc = tensor(a[5], "k_cache"), &vc = tensor(a[6], "v_cache"), &ks = tensor(a[7], "k_scale"), &vs = tensor(a[8], "v_scale");
+    const int dev = c10::cuda::current_device();
+    on_device(dev, {&k, &v, &offsets, &total, &table, &kc, &vc, &ks, &vs});
+    no_gradient({&k, &v, &kc, &vc, &ks, &vs});
+    rows(k, "k");
+    rows(v, "v");
+    const mmv_kv_cache_q8 cache = cache_q8_of(kc, vc, ks, vs);
+    contiguous_of(offsets, ScalarType::Int, "offsets");
+    contiguous_of(total, ScalarType::Int, "total");
+    const int64_t n = total.numel();
+    table_of(table, n);
+    if (offsets.numel() != n + 1) value_error("offsets holds one entry more than total");
+    if (k.scalar_type() != v.scalar_type()) type_error("keys and values must have one type");
+    if (k.sizes() != v.sizes() || k.size(1) != kc.size(2) || k.size(2) != kc.size(3)) value_error("k, v must be [tokens, heads, dim] like the caches");
+    check(mmv_kv_append_q8(k.data_ptr(), k.stride(0), k.stride(1), v.data_ptr(), v.stride(0), v.stride(1), value_code(k), k.size(0),
+                           offsets.data_ptr<int32_t>(), total.data_ptr<int32_t>(), n, table.data_ptr<int32_t>(), table.stride(0), table.size(1), &cache,
+                           stream_of(a[9], dev)),
+          "mmv_kv_append_q8");
+    Py_RETURN_NONE;
+}
+
+// k_cache, v_cache, k_scale, v_scale, table, offsets, tokens, dtype, k, v, stream
+PyObject* kv_read_q8(PyObject* const* a) {
+    const Tensor &kc = tensor(a[0], "k_cache"), &vc = tensor(a[1], "v_cache"), &ks = tensor(a[2], "k_scale"), &vs = tensor(a[3], "v_scale"),
+                 &table = tensor(a[4], "table"), &offsets = tensor(a[5], "offsets");
+    Tensor k = optional(a[8], "k"), v = optional(a[9], "v");
+    const int dev = c10::cuda::current_device();
+    on_device(dev, {&kc, &vc, &ks, &vs, &table, &offsets, &k, &v});
+    no_gradient({&kc, &vc, &ks, &vs, &k, &v});
+    const mmv_kv_cache_q8 cache = cache_q8_of(kc, vc, ks, vs);
+    contiguous_of(offsets, ScalarType::Int, "offsets");
+    const int64_t n = offsets.numel() - 1, tokens = integer(a[6]);
+    if (n < 0) value_error("offsets holds one entry more than there are requests");
+    if (tokens < 0) value_error("tokens must not be negative");
+    table_of(table, n);
+    if (!THPDtype_Check(a[7])) type_error("dtype must be a torch.dtype");
+    const ScalarType type = reinterpret_cast<THPDtype*>(a[7])->scalar_type;
+    if (type != ScalarType::Half && type != ScalarType::BFloat16) type_error("dtype must be torch.float16 or torch.bfloat16");
+    contiguous_of(k, type, "k");
+    contiguous_of(v, type, "v");
+    shaped(k, {tokens, kc.size(2), kc.size(3)}, "k");
+    shaped(v, {tokens, kc.size(2), kc.size(3)}, "v");
+    if (!k.defined()) k = make({tokens, kc.size(2), kc.size(3)}, type, dev);
+    if (!v.defined()) v = make({tokens, kc.size(2), kc.size(3)}, type, dev);
+    check(mmv_kv_read_q8(&cache, table.data_ptr<int32_t>(), table.stride(0), table.size(1), offsets.data_ptr<int32_t>(), n, tokens, value_code(k),
+                         k.data_ptr(), v.data_ptr(), stream_of(a[10], dev)),
+          "mmv_kv_read_q8");
+    return wrap({k, v});
+}
+
+// q, k_cache, v_cache, k_scale, v_scale, table, lens, scale, window, out, lse, workspace, stream
+PyObject* paged_attention_q8(PyObject* const* a) {
+    const Tensor &q = tensor(a[0], "q"), &kc = tensor(a[1], "k_cache"), &vc = tensor(a[2], "v_cache"), &ks = tensor(a[3], "k_scale"), &vs = tensor(a[4], "v_scale"),
+                 &table = tensor(a[5], "table"), &lens = tensor(a[6], "lens");
+    Tensor out = optional(a[9], "out"), lse = optional(a[10], "lse"), ws = optional(a[11], "workspace");
+    const int dev = c10::cuda::current_device();
+    on_device(dev, {&q, &kc, &vc, &ks, &vs, &table, &lens, &out, &lse, &ws});
+    no_gradient({&q, &kc, &vc, &ks, &vs, &out, &lse});
+    rows(q, "q");
+    const int64_t n = q.size(0), heads = q.size(1), dim = q.size(2);
+    const mmv_kv_cache_q8 cache = cache_q8_of(kc, vc, ks, vs);
+    contiguous_of(lens, ScalarType::Int, "lens");
+    contiguous_of(out, q.scalar_type(), "out");
+    contiguous_of(lse, ScalarType::Float, "lse");
+    contiguous_of(ws, ScalarType::Byte, "workspace");
+    shaped(lens, {n}, "lens");
+    shaped(out, q.sizes(), "out");
+    shaped(lse, {n, heads}, "lse");
+    table_of(table, n);
+    if (dim != kc.size(3) || kc.size(2) == 0 || heads % kc.size(2) || heads > INT32_MAX)
+        value_error("q must be [requests, heads, dim] with the caches' dim and a multiple of their heads");
+    const mmv_dtype type = value_code(q);
+    if (!out.defined()) out = make({n, heads, dim}, q.scalar_type(), dev);
+    if (!lse.defined()) lse = make({n, heads}, ScalarType::Float, dev);
+    if (!ws.defined()) ws = scratch(mmv_paged_attention_q8_workspace_bytes(static_cast<int32_t>(heads), &cache), dev);
+    const double scale = a[7] == Py_None ? 1.0 / std::sqrt(static_cast<double>(dim)) : number(a[7]);
+    check(mmv_paged_attention_q8(q.data_ptr(), q.stride(0), q.stride(1), static_cast<int32_t>(heads), type, &cache, table.data_ptr<int32_t>(), table.stride(0),
+                                 table.size(1), lens.data_ptr<int32_t>(), n, static_cast<float>(scale), integer(a[8]), out.data_ptr(), lse.data_ptr<float>(),
+                                 ws.data_ptr(), static_cast<size_t>(ws.numel()), stream_of(a[12], dev)),
+          "mmv_paged_attention_q8");
+    return wrap({out, lse});
+}
+
 // q, k, v, offsets, log_decay, scale, state, out, state_out, workspace, stream
 PyObject* linear_attention(PyObject* const* a) {
     const Tensor &q = tensor(a[0], "q"), &k = tensor(a[1], "k"), &v = tensor(a[2], "v"), &offsets = tensor(a[3], "offsets"), &decay = tensor(a[4], "log_decay");
@@ -328,6 +442,12 @@ PyObject* paged_workspace(PyObject* const* a) {
     return PyLong_FromSize_t(mmv_paged_attention_workspace_bytes(int32_of(a[0], "heads"), &c));
 }
 
+// heads, k_cache, v_cache, k_scale, v_scale
+PyObject* paged_q8_workspace(PyObject* const* a) {
+    const mmv_kv_cache_q8 c = cache_q8_of(tensor(a[1], "k_cache"), tensor(a[2], "v_cache"), tensor(a[3], "k_scale"), tensor(a[4], "v_scale"));
+    return PyLong_FromSize_t(mmv_paged_attention_q8_workspace_bytes(int32_of(a[0], "heads"), &c));
+}
+
 PyObject* set_error(PyObject* const* a) {
     Py_INCREF(a[0]);
     Py_XDECREF(g_error);
@@ -366,6 +486,10 @@ PyMethodDef g_methods[] = {method<block_tables, 11>("block_tables"),
                            method<linear_attention_step, 10>("linear_attention_step"),
                            method<linear_workspace, 4>("linear_attention_workspace_bytes"),
                            method<paged_workspace, 3>("paged_attention_workspace_bytes"),
+                           method<kv_append_q8, 10>("kv_append_q8"),
+                           method<kv_read_q8, 11>("kv_read_q8"),
+                           method<paged_attention_q8, 13>("paged_attention_q8"),
+                           method<paged_q8_workspace, 5>("paged_attention_q8_workspace_bytes"),
                            method<set_error, 1>("set_error"),
                            {nullptr, nullptr, 0, nullptr}};
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_serve", nullptr, -1, g_methods, nullptr, nullptr, nullptr, nullptr};
