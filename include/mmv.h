@@ -604,6 +604,56 @@ mmv_status mmv_linear_attention(const mmv_linear_inputs *in, const int32_t *offs
                                 void *workspace, size_t workspace_bytes, void *cuda_stream);
 
 /*
+ * Inputs of the gated delta rule: q, k [.., key_heads, dim_k], v [.., heads,
+ * dim_v] with a token (or request) in front, token and head strides of their own;
+ * log_decay and beta [.., heads] fp32, heads contiguous, any token stride.  heads is a
+ * multiple of key_heads: value head h uses query and key head
+ * h / (heads / key_heads) and has a decay, a beta and a state of its own.  dim_k and dim_v
+ * are multiples of 8 up to 128.
+ */
+typedef struct {
+    const void *q, *k, *v;
+    const float *log_decay, *beta;
+    int64_t q_stride_token, q_stride_head, k_stride_token, k_stride_head, v_stride_token, v_stride_head;
+    int64_t log_decay_stride_token, beta_stride_token;
+    int32_t heads, key_heads, dim_k, dim_v, dtype;
+} mmv_delta_inputs;
+
+/*
+ * The gated delta rule, ONE token for each of nreq requests (token r of the
+ * inputs):
+ *     u   = beta (v - exp(log_decay) S^T k)
+ *     S'  = exp(log_decay) S + k u^T          (fp32, dim_k x dim_v, row-major)
+ *     out = scale * S'^T q                    (nreq x heads x dim_v, the inputs' type)
+ * S is state[s], S' is written to state_out[s], with s = slots[r] (int32; slots NULL:
+ * s = r): as in mmv_linear_attention_step, to the same conditions.  No workspace.
+ */
+mmv_status mmv_gated_delta_step(const mmv_delta_inputs *in, int64_t nreq, float scale, const float *state,
+                                float *state_out, const int32_t *slots, int64_t num_slots, void *out,
+                                void *cuda_stream);
+
+/*
+ * The gated delta rule over packed prompts: sequence s is the tokens
+ * [offsets[s], offsets[s + 1]) (empty sequences allowed), each token as above.  In front of its
+ * first token S is state[s] (state NULL: zero), behind its last one S is written to
+ * state_out[s] (required; an empty sequence's state is copied): [nseq, heads, dim_k, dim_v]
+ * fp32, 16-byte aligned; state_out may be state itself, and must not overlap it otherwise
+ * (MMV_ERR_INVALID_ARG).  Values are bfloat16 (another dtype answers MMV_ERR_INVALID_ARG: states
+ * are operands of the tensor core, and fp16's range does not hold them).  out: ntok x heads x dim_v; rows of
+ * tokens outside [offsets[0], offsets[nseq]) are not written.  log_decay: any <= 0, -infinity
+ * included (the state in front of the token is then forgotten, if it was finite).
+ * The rule does not grow where beta |k|^2 <= 2, so keys are expected normalised; operands
+ * are held to 2^-17 of themselves, states in fp32.  Offsets that decrease or leave [0, ntok] are reported as
+ * MMV_ERR_BAD_SEGMENTS in the workspace; nothing outside the buffers is touched.
+ * ntok < 2^31, nseq < 2^20.  Workspace: mmv_gated_delta_workspace_bytes(in, nseq, ntok), 256-byte
+ * aligned: 21 KB per chunk of 64 tokens and head, 174 MB at most (longer batches are taken in parts).
+ */
+size_t mmv_gated_delta_workspace_bytes(const mmv_delta_inputs *in, int64_t nseq, int64_t ntok);
+mmv_status mmv_gated_delta(const mmv_delta_inputs *in, const int32_t *offsets, int64_t nseq, int64_t ntok, float scale,
+                           const float *state, float *state_out, void *out, void *workspace, size_t workspace_bytes,
+                           void *cuda_stream);
+
+/*
  * Test hook.  wait_budget_ns: time after which a device-side wait gives up
  * (<= 0 restores the default of 4 s).  skip_publish_span: index of one
  * 4096-element span of the scan that never publishes its carry, so that its

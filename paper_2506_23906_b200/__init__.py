@@ -35,6 +35,7 @@ EXPORTS = (
     "mmv_paged_attention_workspace_bytes", "mmv_paged_attention",
     "mmv_linear_attention_workspace_bytes", "mmv_linear_attention",
     "mmv_kv_append_q8", "mmv_kv_read_q8", "mmv_paged_attention_q8_workspace_bytes", "mmv_paged_attention_q8",
+    "mmv_gated_delta_step", "mmv_gated_delta_workspace_bytes", "mmv_gated_delta",
 )
 SHARD_SUMMARY_BYTES = 16
 STATIC_SCAN_MAX_N = 1 << 28
@@ -538,3 +539,37 @@ def linear_attention_step(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, log
     if stream is not None:
         return _on_stream(_serve.linear_attention_step, stream, (q, k, v, log_decay, state, slots, state_out, out), args)
     return _serve.linear_attention_step(*args, None)
+
+
+def gated_delta_workspace_bytes(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, log_decay: torch.Tensor, beta: torch.Tensor, sequences: int) -> int:
+    """mmv_gated_delta_workspace_bytes of a call with these inputs."""
+    return _serve.gated_delta_workspace_bytes(q, k, v, log_decay, beta, sequences)
+
+
+def gated_delta(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, offsets: torch.Tensor, log_decay: torch.Tensor, beta: torch.Tensor,
+                scale: float = 1.0, state: torch.Tensor | None = None, out: torch.Tensor | None = None,
+                state_out: torch.Tensor | None = None, workspace: torch.Tensor | None = None, stream=None):
+    """mmv_gated_delta: the gated delta rule over packed sequences, S_t = a_t S_{t-1} + k_t u_t^T with
+    u_t = beta_t (v_t - a_t S_{t-1}^T k_t), a_t = exp(log_decay_t), out_t = scale S_t^T q_t.
+
+    q, k [tokens, key_heads, dim_k], v [tokens, heads, dim_v], bfloat16 (views are fine), keys normalised; log_decay, beta fp32
+    [tokens, heads]; offsets int32 [sequences + 1]; state fp32 [sequences, heads, dim_k, dim_v] in front of the first tokens (None:
+    zero).  Returns (out [tokens, heads, dim_v], state_out: the states behind the last tokens; it may be state itself)."""
+    args = (q, k, v, offsets, log_decay, beta, scale, state, out, state_out, workspace)
+    if stream is not None:
+        return _on_stream(_serve.gated_delta, stream, (q, k, v, offsets, log_decay, beta, state, out, state_out, workspace), args)
+    return _serve.gated_delta(*args, None)
+
+
+def gated_delta_step(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, log_decay: torch.Tensor, beta: torch.Tensor, state: torch.Tensor,
+                     scale: float = 1.0, slots: torch.Tensor | None = None, state_out: torch.Tensor | None = None,
+                     out: torch.Tensor | None = None, stream=None) -> torch.Tensor:
+    """mmv_gated_delta_step: one token of the gated delta rule for every request.
+
+    q, k [requests, key_heads, dim_k], v [requests, heads, dim_v]; log_decay, beta fp32 [requests, heads]; state fp32
+    [states, heads, dim_k, dim_v], request r's at slots[r] (int32; None: at r), updated in place unless state_out is given.
+    Returns out [requests, heads, dim_v]."""
+    args = (q, k, v, log_decay, beta, state, scale, slots, state_out, out)
+    if stream is not None:
+        return _on_stream(_serve.gated_delta_step, stream, (q, k, v, log_decay, beta, state, slots, state_out, out), args)
+    return _serve.gated_delta_step(*args, None)

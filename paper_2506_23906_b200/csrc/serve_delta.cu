@@ -1,0 +1,155 @@
+// Host side of the gated delta rule of include/mmv.h: argument checks, workspace carve-up and launches.
+#include <cstdint>
+#include <cuda_runtime.h>
+
+#include "../../include/mmv.h"
+#include "common.cuh"
+#include "gated_delta.cuh"
+#include "host_state.h"
+#include "serve_host.h"
+
+namespace mmv {
+namespace {
+
+ServeDevice g_devices[kMaxDevices];
+
+template <int DK>
+bool allow_dim() {
+    return allow_smem(delta_prep_kernel<DK>, DeltaPrepCfg<DK>::kSmemBytes) && allow_smem(delta_chunks_kernel<DK, 16>, DeltaCfg<DK, 16>::kSmemBytes) &&
+           allow_smem(delta_chunks_kernel<DK, 32>, DeltaCfg<DK, 32>::kSmemBytes);
+}
+ServeDevice* device() {
+    return device_once(g_devices, [] { return allow_dim<64>() && allow_dim<128>(); });
+}
+
+mmv_status check_inputs(const mmv_delta_inputs* in, int64_t tokens) {
+    if (!in || !value_type(in->dtype)) return MMV_ERR_INVALID_ARG;
+    if (in->heads < 1 || in->heads > kMaxHeads || in->key_heads < 1 || in->heads % in->key_heads) return MMV_ERR_INVALID_ARG;
+    if (in->dim_k < 8 || in->dim_k > 128 || in->dim_k % 8 || in->dim_v < 8 || in->dim_v > 128 || in->dim_v % 8) return MMV_ERR_INVALID_ARG;
+    if (!word_stride(in->q_stride_token, tokens) || !word_stride(in->q_stride_head, in->key_heads) || !word_stride(in->k_stride_token, tokens) ||
+        !word_stride(in->k_stride_head, in->key_heads) || !word_stride(in->v_stride_token, tokens) || !word_stride(in->v_stride_head, in->heads))
+        return MMV_ERR_INVALID_ARG;
+    if (!aligned(in->q, 16) || !aligned(in->k, 16) || !aligned(in->v, 16) || !aligned(in->log_decay, 4) || !aligned(in->beta, 4)) return MMV_ERR_INVALID_ARG;
+    return MMV_OK;
+}
+bool missing(const mmv_delta_inputs* in) { return !in->q || !in->k || !in->v || !in->log_decay || !in->beta; }
+
+DeltaParams params_of(const mmv_delta_inputs* in, float scale, void* out) {
+    DeltaParams p{};
+    p.q = static_cast<const uint16_t*>(in->q);
+    p.k = static_cast<const uint16_t*>(in->k);
+    p.v = static_cast<const uint16_t*>(in->v);
+    p.q_tok = in->q_stride_token;
+    p.q_head = in->q_stride_head;
+    p.k_tok = in->k_stride_token;
+    p.k_head = in->k_stride_head;
+    p.v_tok = in->v_stride_token;
+    p.v_head = in->v_stride_head;
+    p.decay = in->log_decay;
+    p.beta = in->beta;
+    p.decay_tok = in->log_decay_stride_token;
+    p.beta_tok = in->beta_stride_token;
+    p.heads = in->heads;
+    p.group = in->heads / in->key_heads;
+    p.dk = in->dim_k;
+    p.dv = in->dim_v;
+    p.scale = scale;
+    p.out = static_cast<uint16_t*>(out);
+    return p;
+}
+
+// Places of chunks (delta_slot): all of them, and those that one pair of launches takes, whose operands the workspace holds.
+int64_t all_places(int64_t nseq, int64_t ntok) { return ntok / DELTA_C + nseq; }
+constexpr int64_t kPlaces = 8192;                            // (chunk, head)s: 174 MB
+int64_t places_at_once(const mmv_delta_inputs* in, int64_t nseq, int64_t ntok) {
+    const int64_t most = kPlaces / in->heads, all = all_places(nseq, ntok);
+    return all < most ? all : most;
+}
+
+template <int DK>
+mmv_status launch_delta(const DeltaParams& p, int64_t places, int nv, cudaStream_t st) {
+    const unsigned prep = static_cast<unsigned>(places * (p.heads / p.group)), ctas = static_cast<unsigned>(static_cast<int64_t>(p.nseq) * p.heads * p.slices);
+    const mmv_status rc = launch(delta_prep_kernel<DK>, dim3(prep), DELTA_PREP_THREADS, DeltaPrepCfg<DK>::kSmemBytes, st, false, p);
+    if (rc != MMV_OK) return rc;
+    return nv == 16 ? launch(delta_chunks_kernel<DK, 16>, dim3(ctas), DELTA_THREADS, DeltaCfg<DK, 16>::kSmemBytes, st, true, p)
+                    : launch(delta_chunks_kernel<DK, 32>, dim3(ctas), DELTA_THREADS, DeltaCfg<DK, 32>::kSmemBytes, st, true, p);
+}
+
+}  // namespace
+}  // namespace mmv
+
+using namespace mmv;
+
+extern "C" {
+
+mmv_status mmv_gated_delta_step(const mmv_delta_inputs* in, int64_t nreq, float scale, const float* state, float* state_out, const int32_t* slots,
+                                int64_t num_slots, void* out, void* cuda_stream) {
+    if (nreq < 0 || num_slots < 0 || check_inputs(in, nreq) != MMV_OK) return MMV_ERR_INVALID_ARG;
+    if (nreq == 0) return MMV_OK;
+    if (missing(in) || !out || !aligned(out, 16)) return MMV_ERR_INVALID_ARG;
+    if (num_slots && (!state || !state_out || !aligned(state, 16) || !aligned(state_out, 16))) return MMV_ERR_INVALID_ARG;
+    if (slots ? !aligned(slots, 4) : num_slots < nreq) return MMV_ERR_INVALID_ARG;
+    if (nreq > INT32_MAX / (static_cast<int64_t>(in->heads) * 16)) return MMV_ERR_INVALID_ARG;       // one CTA per state and column part
+    const size_t states = static_cast<size_t>(num_slots) * in->heads * in->dim_k * in->dim_v * sizeof(float);
+    if (state != state_out && overlap(state, states, state_out, states)) return MMV_ERR_INVALID_ARG;      // (in place, or apart)
+    ServeDevice* dev = device();
+    if (!dev) return MMV_ERR_CUDA;
+    DeltaParams p = params_of(in, scale, out);
+    p.state = state;
+    p.state_out = state_out;
+    p.slots = slots;
+    p.nreq = nreq;
+    p.num_slots = num_slots;
+    const bool wide = p.dv > 64 && nreq * p.heads >= dev->sm_count;
+    p.parts = wide ? 1 : (p.dv + 31) / 32;
+    const dim3 grid(static_cast<unsigned>(nreq * p.heads * p.parts));
+    cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+    if (in->dtype == MMV_BF16_TO_F32)
+        return wide ? launch(delta_step_kernel<true, 128>, grid, LIN_STEP_THREADS, 0, st, false, p)
+                    : launch(delta_step_kernel<true, 32>, grid, LIN_STEP_THREADS, 0, st, false, p);
+    return wide ? launch(delta_step_kernel<false, 128>, grid, LIN_STEP_THREADS, 0, st, false, p)
+                : launch(delta_step_kernel<false, 32>, grid, LIN_STEP_THREADS, 0, st, false, p);
+}
+
+size_t mmv_gated_delta_workspace_bytes(const mmv_delta_inputs* in, int64_t nseq, int64_t ntok) {
+    if (nseq < 0 || nseq >= (1ll << 20) || ntok < 0 || ntok > INT32_MAX || check_inputs(in, ntok) != MMV_OK) return 0;
+    return round_up(sizeof(WorkspaceHeader) + static_cast<size_t>(places_at_once(in, nseq, ntok)) * in->heads * sizeof(DeltaChunk), 256);
+}
+
+mmv_status mmv_gated_delta(const mmv_delta_inputs* in, const int32_t* offsets, int64_t nseq, int64_t ntok, float scale, const float* state,
+                           float* state_out, void* out, void* workspace, size_t workspace_bytes, void* cuda_stream) {
+    if (nseq < 0 || nseq >= (1ll << 20) || ntok < 0 || ntok > INT32_MAX || check_inputs(in, ntok) != MMV_OK || in->dtype != MMV_BF16_TO_F32)
+        return MMV_ERR_INVALID_ARG;
+    if (!workspace || !aligned(workspace, 256)) return MMV_ERR_INVALID_ARG;
+    if (nseq && (!offsets || !aligned(offsets, 4) || !state_out || !aligned(state_out, 16) || (state && !aligned(state, 16)))) return MMV_ERR_INVALID_ARG;
+    if (ntok && (missing(in) || !out || !aligned(out, 16))) return MMV_ERR_INVALID_ARG;
+    if (workspace_bytes < mmv_gated_delta_workspace_bytes(in, nseq, ntok)) return MMV_ERR_WORKSPACE_TOO_SMALL;
+    const size_t states = static_cast<size_t>(nseq) * in->heads * in->dim_k * in->dim_v * sizeof(float);
+    if (state && state != state_out && overlap(state, states, state_out, states)) return MMV_ERR_INVALID_ARG;      // (in place, or apart)
+    cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+    if (nseq == 0) return cudaMemsetAsync(workspace, 0, sizeof(WorkspaceHeader), st) == cudaSuccess ? MMV_OK : MMV_ERR_CUDA;
+    ServeDevice* dev = device();
+    if (!dev) return MMV_ERR_CUDA;
+    DeltaParams p = params_of(in, scale, out);
+    p.state = state;
+    p.state_out = state_out;
+    p.offsets = offsets;
+    p.nseq = static_cast<int>(nseq);
+    p.ntok = static_cast<int>(ntok);
+    p.hdr = static_cast<WorkspaceHeader*>(workspace);
+    p.chunks = static_cast<uint8_t*>(workspace) + sizeof(WorkspaceHeader);
+    const int nv = 32;
+    p.slices = (p.dv + nv - 1) / nv;
+    if (nseq * p.heads > INT32_MAX / p.slices) return MMV_ERR_INVALID_ARG;       // one CTA per (sequence, head) and slice
+    const int64_t all = all_places(nseq, ntok), step = places_at_once(in, nseq, ntok);
+    for (int64_t at = 0; at < all; at += step) {
+        p.first_slot = at;
+        p.last_slot = at + step < all ? at + step : all;
+        const int64_t places = p.last_slot - at;
+        const mmv_status rc = in->dim_k <= 64 ? launch_delta<64>(p, places, nv, st) : launch_delta<128>(p, places, nv, st);
+        if (rc != MMV_OK) return rc;
+    }
+    return MMV_OK;
+}
+
+}  // extern "C"

@@ -201,6 +201,42 @@ mmv_linear_inputs linear_of(const Tensor& q, const Tensor& k, const Tensor& v) {
     return in;
 }
 
+mmv_delta_inputs delta_of(const Tensor& q, const Tensor& k, const Tensor& v, const Tensor& decay, const Tensor& beta) {
+    rows(q, "q");
+    rows(k, "k");
+    rows(v, "v");
+    if (q.scalar_type() != k.scalar_type() || q.scalar_type() != v.scalar_type()) type_error("q, k and v must have one type");
+    if (q.sizes() != k.sizes() || k.size(0) != v.size(0) || k.size(1) == 0 || v.size(1) == 0 || v.size(1) % k.size(1) != 0)
+        value_error("q, k [tokens, key_heads, dim_k], v [tokens, heads, dim_v] expected, heads a multiple of key_heads");
+    if (v.size(1) > INT32_MAX || q.size(2) > INT32_MAX || v.size(2) > INT32_MAX) value_error("heads and dims do not fit 32 bits");
+    for (const Tensor* t : {&decay, &beta}) {
+        const char* name = t == &decay ? "log_decay" : "beta";
+        if (t->scalar_type() != ScalarType::Float) type_error(std::string(name) + " must be torch.float32");
+        if (t->dim() != 2 || t->size(0) != v.size(0) || t->size(1) != v.size(1)) value_error(std::string(name) + " must be [tokens, heads]");
+        if (t->size(1) > 1 && t->stride(1) != 1) value_error(std::string(name) + "'s last axis must be contiguous");
+    }
+    mmv_delta_inputs in;
+    in.q = q.data_ptr();
+    in.k = k.data_ptr();
+    in.v = v.data_ptr();
+    in.log_decay = decay.data_ptr<float>();
+    in.beta = beta.data_ptr<float>();
+    in.q_stride_token = q.stride(0);
+    in.q_stride_head = q.stride(1);
+    in.k_stride_token = k.stride(0);
+    in.k_stride_head = k.stride(1);
+    in.v_stride_token = v.stride(0);
+    in.v_stride_head = v.stride(1);
+    in.log_decay_stride_token = decay.stride(0);
+    in.beta_stride_token = beta.stride(0);
+    in.heads = static_cast<int32_t>(v.size(1));
+    in.key_heads = static_cast<int32_t>(k.size(1));
+    in.dim_k = static_cast<int32_t>(q.size(2));
+    in.dim_v = static_cast<int32_t>(v.size(2));
+    in.dtype = value_code(q);
+    return in;
+}
+
 // past, added, free_blocks, table, slots, block_size, offsets, total, used, workspace, stream
 PyObject* block_tables(PyObject* const* a) {
     const Tensor &past = tensor(a[0], "past"), &added = tensor(a[1], "added"), &fresh = tensor(a[2], "free_blocks"), &table = tensor(a[3], "table"),
@@ -428,6 +464,68 @@ PyObject* linear_attention_step(PyObject* const* a) {
     return THPVariable_Wrap(out);
 }
 
+// q, k, v, offsets, log_decay, beta, scale, state, out, state_out, workspace, stream
+PyObject* gated_delta(PyObject* const* a) {
+    const Tensor &q = tensor(a[0], "q"), &k = tensor(a[1], "k"), &v = tensor(a[2], "v"), &offsets = tensor(a[3], "offsets"), &decay = tensor(a[4], "log_decay"),
+                 &beta = tensor(a[5], "beta");
+    Tensor state = optional(a[7], "state"), out = optional(a[8], "out"), last = optional(a[9], "state_out"), ws = optional(a[10], "workspace");
+    const int dev = c10::cuda::current_device();
+    on_device(dev, {&q, &k, &v, &offsets, &decay, &beta, &state, &out, &last, &ws});
+    no_gradient({&q, &k, &v, &decay, &beta, &state, &out, &last});
+    const mmv_delta_inputs in = delta_of(q, k, v, decay, beta);
+    const int64_t tokens = v.size(0), heads = v.size(1), dk = q.size(2), dv = v.size(2), nseq = offsets.numel() - 1;
+    if (nseq < 0) value_error("offsets holds one entry more than there are sequences");
+    contiguous_of(offsets, ScalarType::Int, "offsets");
+    contiguous_of(state, ScalarType::Float, "state");
+    contiguous_of(last, ScalarType::Float, "state_out");
+    contiguous_of(out, q.scalar_type(), "out");
+    contiguous_of(ws, ScalarType::Byte, "workspace");
+    shaped(state, {nseq, heads, dk, dv}, "state");
+    shaped(last, {nseq, heads, dk, dv}, "state_out");
+    shaped(out, {tokens, heads, dv}, "out");
+    if (!out.defined()) out = make({tokens, heads, dv}, q.scalar_type(), dev);
+    if (!last.defined()) last = make({nseq, heads, dk, dv}, ScalarType::Float, dev);
+    if (!ws.defined()) ws = scratch(mmv_gated_delta_workspace_bytes(&in, nseq, tokens), dev);
+    check(mmv_gated_delta(&in, offsets.data_ptr<int32_t>(), nseq, tokens, static_cast<float>(number(a[6])), state.defined() ? state.data_ptr<float>() : nullptr,
+                          last.data_ptr<float>(), out.data_ptr(), ws.data_ptr(), static_cast<size_t>(ws.numel()), stream_of(a[11], dev)),
+          "mmv_gated_delta");
+    return wrap({out, last});
+}
+
+// q, k, v, log_decay, beta, state, scale, slots, state_out, out, stream
+PyObject* gated_delta_step(PyObject* const* a) {
+    const Tensor &q = tensor(a[0], "q"), &k = tensor(a[1], "k"), &v = tensor(a[2], "v"), &decay = tensor(a[3], "log_decay"), &beta = tensor(a[4], "beta"),
+                 &state = tensor(a[5], "state");
+    Tensor slots = optional(a[7], "slots"), to = optional(a[8], "state_out"), out = optional(a[9], "out");
+    if (!to.defined()) to = state;
+    const int dev = c10::cuda::current_device();
+    on_device(dev, {&q, &k, &v, &decay, &beta, &state, &slots, &to, &out});
+    no_gradient({&q, &k, &v, &decay, &beta, &state, &to, &out});
+    const mmv_delta_inputs in = delta_of(q, k, v, decay, beta);
+    const int64_t n = v.size(0), heads = v.size(1), dk = q.size(2), dv = v.size(2);
+    contiguous_of(state, ScalarType::Float, "state");
+    contiguous_of(to, ScalarType::Float, "state_out");
+    contiguous_of(slots, ScalarType::Int, "slots");
+    contiguous_of(out, q.scalar_type(), "out");
+    if (state.dim() != 4) value_error("state has the wrong shape");
+    shaped(state, {state.size(0), heads, dk, dv}, "state");
+    shaped(to, state.sizes(), "state_out");
+    shaped(slots, {n}, "slots");
+    shaped(out, {n, heads, dv}, "out");
+    if (!out.defined()) out = make({n, heads, dv}, q.scalar_type(), dev);
+    check(mmv_gated_delta_step(&in, n, static_cast<float>(number(a[6])), state.data_ptr<float>(), to.data_ptr<float>(),
+                               slots.defined() ? slots.data_ptr<int32_t>() : nullptr, state.size(0), out.data_ptr(), stream_of(a[10], dev)),
+          "mmv_gated_delta_step");
+    return THPVariable_Wrap(out);
+}
+
+// q, k, v, log_decay, beta, sequences
+PyObject* delta_workspace(PyObject* const* a) {
+    const Tensor& v = tensor(a[2], "v");
+    const mmv_delta_inputs in = delta_of(tensor(a[0], "q"), tensor(a[1], "k"), v, tensor(a[3], "log_decay"), tensor(a[4], "beta"));
+    return PyLong_FromSize_t(mmv_gated_delta_workspace_bytes(&in, integer(a[5]), v.size(0)));
+}
+
 // q, k, v, sequences
 PyObject* linear_workspace(PyObject* const* a) {
     const Tensor &q = tensor(a[0], "q"), &k = tensor(a[1], "k"), &v = tensor(a[2], "v");
@@ -490,6 +588,9 @@ PyMethodDef g_methods[] = {method<block_tables, 11>("block_tables"),
                            method<kv_read_q8, 11>("kv_read_q8"),
                            method<paged_attention_q8, 13>("paged_attention_q8"),
                            method<paged_q8_workspace, 5>("paged_attention_q8_workspace_bytes"),
+                           method<gated_delta, 12>("gated_delta"),
+                           method<gated_delta_step, 11>("gated_delta_step"),
+                           method<delta_workspace, 6>("gated_delta_workspace_bytes"),
                            method<set_error, 1>("set_error"),
                            {nullptr, nullptr, 0, nullptr}};
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_serve", nullptr, -1, g_methods, nullptr, nullptr, nullptr, nullptr};
