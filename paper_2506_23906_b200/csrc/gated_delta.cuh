@@ -34,6 +34,7 @@ struct DeltaParams {
     int slices;                                              // column parts of a (sequence, head)
     WorkspaceHeader* hdr;
     uint8_t* chunks;                                         // [last_slot - first_slot][heads] DeltaChunk
+    uint64_t budget_ns;                                      // bound of every wait
 };
 
 // ---------------------------------------------------------------------------------------------------------------------
@@ -147,14 +148,15 @@ __global__ void __launch_bounds__(LIN_STEP_THREADS) delta_step_kernel(const Delt
 // Packed prompts, chunks of 64 tokens on the tensor cores.  With G the running sum of g in a chunk of n tokens, S the state in front of it and
 // D_ij = exp(G_i - G_j):
 //     L_ij = b_i D_ij k_i . k_j  (j < i),  T = (1 + L)^-1,  A_ij = D_ij q_i . k_j  (j <= i)
-//     U  = T diag(b) (V - exp(G) K S)          (row i is u_i)
+//     R  = diag(b) (V - exp(G) K S),  U = T R            (row i is u_i)
 //     O  = scale (exp(G) Q S + A U)
 //     S' = exp(G_n) S + K^T diag(exp(G_n - G)) U
 // T and A do not depend on the state: a first kernel forms them for all chunks side by side; the second one walks along a sequence's chunks, one
 // CTA per (sequence, head, slice of columns), whose columns never meet others'.
 //
-// Every operand that is formed here enters its product as the sum of two bfloat16 values (2^-17 of it), so that the fp32 state stays exact to
-// about 2^-16 of what is added to it; products of two such leave out the two low parts' (2^-18).
+// Operands that are formed here enter their products as sums of bfloat16 values, of two (2^-17 of the value; products of two such leave
+// out the two low parts', 2^-18) or, where the fp32 state would lose by it, of three: its own copy in K S and the update's exp(G_n - G) U.
+// U is R + (T - 1) R, the first term in fp32.  With two parts everywhere and T R as a product the state was off by 4.0e-6 of itself.
 //
 // A chunk that holds a value that is not finite (or whose products are not) is taken token by token: zeros of the triangles would carry it to
 // tokens in front of it.
@@ -164,15 +166,18 @@ constexpr int DELTA_TILES = 10;                              // 16 x 16 blocks o
 __host__ __device__ constexpr int delta_tile(int i, int j) { return i * (i + 1) / 2 + j; }
 
 // What the first kernel leaves of a chunk and head.  A block's 32 x 16 bytes are the lanes' registers of a product's first operand.
-struct DeltaChunk {
-    uint4 t[2][DELTA_TILES][32];                             // T: high parts, low parts
-    uint4 a[2][DELTA_TILES][32];                             // A
+struct DeltaScalars {
     float beta[DELTA_C], past[DELTA_C], left[DELTA_C];       // b, exp(G), exp(G_n - G)
     float whole_hi, whole_lo;                                // exp(G_n)
     int wild;                                                // to be taken token by token
     int pad;
 };
-static_assert(sizeof(DeltaChunk) % 16 == 0, "copied in 16-byte words");
+struct DeltaChunk {
+    uint4 t[2][DELTA_TILES][32];                             // T - 1: high parts, low parts
+    uint4 a[2][DELTA_TILES][32];                             // A
+    DeltaScalars x;
+};
+static_assert(sizeof(DeltaScalars) % 16 == 0 && sizeof(DeltaChunk) % 16 == 0, "copied in 16-byte words");
 
 // Sequence s: its first token and length; its chunk c lies at place tok / 64 + s + c (no two at the same, in any offsets that grow).
 __device__ __forceinline__ long long delta_slot(int tok, int seq) { return static_cast<long long>(tok / DELTA_C) + seq; }
@@ -189,13 +194,15 @@ __device__ __forceinline__ int delta_sequence_of(const int32_t* offsets, int n, 
     return lo;
 }
 
-// 128-byte columns of 64 values; word c of a row at c ^ (row modulo 8)
-template <int DK>
-__device__ __forceinline__ uint32_t delta_at(int row, int c) { return row * (DK * 2) + ((c ^ (row & 7)) << 4); }
 __device__ __forceinline__ void delta_split(float a, float b, uint32_t& hi, uint32_t& lo) {
     hi = pack_pair<true>(a, b);
     const float2 x = unpack_pair<true>(hi);
     lo = pack_pair<true>(a - x.x, b - x.y);
+}
+__device__ __forceinline__ void delta_split3(float a, float b, uint32_t (&r)[3]) {
+    r[0] = pack_pair<true>(a, b);
+    const float2 x = unpack_pair<true>(r[0]);
+    delta_split(a - x.x, b - x.y, r[1], r[2]);
 }
 // d += (ahi + alo)(bhi + blo) less alo blo
 __device__ __forceinline__ void delta_mma3(float (&d)[4], const uint32_t (&ahi)[4], const uint32_t (&alo)[4], uint32_t bh0, uint32_t bh1, uint32_t bl0, uint32_t bl1) {
@@ -204,34 +211,58 @@ __device__ __forceinline__ void delta_mma3(float (&d)[4], const uint32_t (&ahi)[
     mma_16816<true>(d, ahi, bl0, bl1);
 }
 __device__ __forceinline__ bool delta_finite(float x) { return (__float_as_uint(x) & 0x7f800000u) != 0x7f800000u; }
-
-// A tile of 64 tokens x DK columns into shared memory; what lies behind the chunk or the row reads as zero.
-template <int DK, int THREADS>
-__device__ __forceinline__ void delta_fetch(uint32_t dst, const uint16_t* src, long long tok, int n, int words, const void* any) {
-    for (int i = threadIdx.x; i < DELTA_C * (DK / 8); i += THREADS) {
-        const int row = i / (DK / 8), c = i - row * (DK / 8);
-        const bool on = row < n && c < words;
-        cp_async_16_or_zero(dst + delta_at<DK>(row, c), on ? static_cast<const void*>(src + row * tok + c * 8) : any, on);
-    }
+__device__ __forceinline__ bool delta_finite2(uint32_t pair) { return (pair & 0x7f80u) != 0x7f80u && (pair & 0x7f800000u) != 0x7f800000u; }
+__device__ __forceinline__ void ldsm_x2_t(uint32_t& a, uint32_t& b, uint32_t addr) {
+    asm volatile("ldmatrix.sync.aligned.m8n8.x2.trans.shared.b16 {%0, %1}, [%2];" : "=r"(a), "=r"(b) : "r"(addr) : "memory");
+}
+// an 8 x 8 matrix of 16-bit values, as a product leaves its results, transposed
+__device__ __forceinline__ uint32_t delta_transpose(uint32_t x) {
+    uint32_t r;
+    asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(x));
+    return r;
 }
 
-constexpr int DELTA_PREP_THREADS = 128;
-constexpr int DELTA_PITCH = 144;                             // bytes of a row of 64 bfloat16: nine words of 16, so that 8 rows' meet all banks
+constexpr int DELTA_BOX = DELTA_C * 128;                     // bytes of 64 tokens x 64 columns, as the loads leave them
+// Word c of a token's row in a tile of 64 tokens x DK columns: boxes of 64 columns, 128-byte swizzle.
+__device__ __forceinline__ uint32_t delta_word(int row, int c) { return (c >> 3) * DELTA_BOX + row * 128 + (((c & 7) ^ (row & 7)) << 4); }
+
+// ---------------------------------------------------------------------------------------------------------------------
+// T and A of one chunk, for the value heads of one key head.  Warps 0 to 3 form K K^T and from it T, 16 rows (then 16 columns) each, warps 4 to 7
+// Q K^T and A.  T's diagonal blocks of 16 x 16 are found by substitution in fp32; warp J then goes down block column J, transposed:
+//     T_IJ^T = -(sum_K T_KJ^T L_IK^T) T_II^T,  K = J .. I - 1
+// where the results of one product are the first operand of the next as they lie in registers (all operands of three parts).
+// ---------------------------------------------------------------------------------------------------------------------
+constexpr int DELTA_PREP_THREADS = 256;
+constexpr int DELTA_BLOCK = 16 * 48;                         // bytes of a 16 x 16 block of bfloat16: rows of three 16-byte words, so that eight meet all banks
 
 template <int DK>
 struct DeltaPrepCfg {
     static constexpr int kTile = DELTA_C * DK * 2;
-    static constexpr int kMat = DELTA_C * DELTA_PITCH;
-    static constexpr int kDiag = 4 * 16 * 17 * 4;
-    static constexpr int kLoads = 2 * kTile, kWork = 4 * kMat + kDiag;
-    static constexpr int kSmemBytes = kLoads + kWork;
+    static constexpr int kL = 0;                             // (over the tiles, when those have been read) L's six blocks under the diagonal, three parts
+    static constexpr int kT = kL + 3 * 6 * DELTA_BLOCK;      // T's four on the diagonal
+    static constexpr int kDiag = kT + 3 * 4 * DELTA_BLOCK;   // L's, fp32
+    static constexpr int kWork = kDiag + 4 * 16 * 17 * 4;
+    static constexpr int kSmemBytes = 2 * kTile > kWork ? 2 * kTile : kWork;
 };
+__device__ __forceinline__ int delta_under(int i, int j) { return i * (i - 1) / 2 + j; }       // j < i
 
-// T and A of one chunk, for the value heads of one key head.
+// d += a b of three parts each, without what is below 2^-24
+__device__ __forceinline__ void delta_mma6(float (&d)[4], const uint32_t (&a)[3][4], const uint32_t (&b)[3][2]) {
+    mma_16816<true>(d, a[2], b[0][0], b[0][1]);
+    mma_16816<true>(d, a[0], b[2][0], b[2][1]);
+    mma_16816<true>(d, a[1], b[1][0], b[1][1]);
+    mma_16816<true>(d, a[1], b[0][0], b[0][1]);
+    mma_16816<true>(d, a[0], b[1][0], b[1][1]);
+    mma_16816<true>(d, a[0], b[0][0], b[0][1]);
+}
+
 template <int DK>
-__global__ void __launch_bounds__(DELTA_PREP_THREADS) delta_prep_kernel(const DeltaParams p) {
+__global__ void __launch_bounds__(DELTA_PREP_THREADS, 2)
+delta_prep_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k, const DeltaParams p) {
     using C = DeltaPrepCfg<DK>;
-    extern __shared__ __align__(128) uint8_t smem[];
+    extern __shared__ __align__(1024) uint8_t lin_smem[];    // (the loads' swizzle goes by the address)
+    uint8_t* smem = lin_smem;
+    __shared__ uint64_t s_full;
     __shared__ double s_g[DELTA_C];
     __shared__ float s_beta[DELTA_C];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, c = lane & 3;
@@ -248,51 +279,62 @@ __global__ void __launch_bounds__(DELTA_PREP_THREADS) delta_prep_kernel(const De
     if (!lin_sequence(p.offsets, p.ntok, seq, tok, len)) return;
     const long long nth = slot - delta_slot(tok, seq);
     if (nth < 0 || nth * DELTA_C >= len) return;
+    if (smem_u32(smem) & 1023u) {                            // (never: the declaration asks for it)
+        if (tid == 0) report_error(p.hdr, 6u);               // MMV_ERR_CUDA
+        return;
+    }
     const int first = tok + static_cast<int>(nth) * DELTA_C, n = min(DELTA_C, len - static_cast<int>(nth) * DELTA_C);
-
-    const uint32_t sm = smem_u32(smem), sm_k = sm, sm_q = sm + C::kTile;
-    delta_fetch<DK, DELTA_PREP_THREADS>(sm_k, p.k + first * p.k_tok + hk * p.k_head, p.k_tok, n, p.dk / 8, p.offsets);
-    delta_fetch<DK, DELTA_PREP_THREADS>(sm_q, p.q + first * p.q_tok + hk * p.q_head, p.q_tok, n, p.dk / 8, p.offsets);
-    cp_async_commit();
-    cp_async_wait<0>();
+    if (tid == 0) {
+        mbar_init(&s_full, 1);
+        mbar_fence_init();
+        mbar_arrive_expect_tx(&s_full, 2 * C::kTile);
+#pragma unroll
+        for (int b = 0; b < DK / 64; ++b) {
+            tma_load_3d(smem + b * DELTA_BOX, &map_k, &s_full, b * 64, hk, first);
+            tma_load_3d(smem + C::kTile + b * DELTA_BOX, &map_q, &s_full, b * 64, hk, first);
+        }
+    }
     __syncthreads();
+    const bool late = !mbar_wait(&s_full, 0, p.budget_ns);
+    if (__syncthreads_or(late)) {
+        if (tid == 0) {
+            report_error(p.hdr, 5u);                         // MMV_ERR_TIMEOUT
+            mbar_wait(&s_full, 0, 1000000);                  // (the loads in flight land before the CTA leaves)
+        }
+        return;
+    }
 
-    // ---- K K^T and Q K^T: a warp's 16 rows, columns up to the diagonal's ---------------------------------------------------------
-    float kk[8][4], qk[8][4];
+    // ---- K K^T or Q K^T: a warp's 16 rows, columns up to the diagonal's ------------------------------------------------------------
+    const bool scores = warp >= 4;
+    const int block = warp & 3;
+    const uint32_t sm = smem_u32(smem);
+    float x[8][4];
 #pragma unroll
     for (int j = 0; j < 8; ++j)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) kk[j][e] = qk[j][e] = 0.f;
+        for (int e = 0; e < 4; ++e) x[j][e] = 0.f;
 #pragma unroll
     for (int d = 0; d < DK / 16; ++d) {
-        uint32_t ak[4], aq[4];
-        const int arow = warp * 16 + (lane & 15);
-        ldsm_x4(ak, sm_k + delta_at<DK>(arow, 2 * d + (lane >> 4)));
-        ldsm_x4(aq, sm_q + delta_at<DK>(arow, 2 * d + (lane >> 4)));
+        uint32_t a[4];
+        ldsm_x4(a, sm + (scores ? C::kTile : 0) + delta_word(block * 16 + (lane & 15), 2 * d + (lane >> 4)));
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-            if (j > warp) break;
+            if (j > block) break;
             uint32_t b[4];
-            ldsm_x4(b, sm_k + delta_at<DK>(j * 16 + (lane & 7) + ((lane >> 4) << 3), 2 * d + ((lane >> 3) & 1)));
-            mma_16816<true>(kk[2 * j], ak, b[0], b[1]);
-            mma_16816<true>(kk[2 * j + 1], ak, b[2], b[3]);
-            mma_16816<true>(qk[2 * j], aq, b[0], b[1]);
-            mma_16816<true>(qk[2 * j + 1], aq, b[2], b[3]);
+            ldsm_x4(b, sm + delta_word(j * 16 + (lane & 7) + ((lane >> 4) << 3), 2 * d + ((lane >> 3) & 1)));
+            mma_16816<true>(x[2 * j], a, b[0], b[1]);
+            mma_16816<true>(x[2 * j + 1], a, b[2], b[3]);
         }
     }
 
-    uint8_t* l_mat = smem + C::kLoads;                       // L, then T: high parts, low parts, [i][j]
-    uint8_t* t_mat = l_mat + 2 * C::kMat;
-    float* diag = reinterpret_cast<float*>(t_mat + 2 * C::kMat);
-    const uint32_t sm_l = smem_u32(l_mat), sm_t = smem_u32(t_mat);
-
+    float* diag = reinterpret_cast<float*>(smem + C::kDiag) + block * 16 * 17;
     for (int rep = 0; rep < p.group; ++rep) {
         const int h = hk * p.group + rep;
         DeltaChunk* to = reinterpret_cast<DeltaChunk*>(p.chunks) + (slot - p.first_slot) * p.heads + h;
         bool fine = true;
-        __syncthreads();                                     // (the last head's numbers have been used)
-        if (warp == 0) {                                     // G, in 64 bits: its differences count.  exp(-200) is 0, whatever is in front of it
-            double x[2];
+        if (rep) __syncthreads();                            // (the last head's numbers have been used)
+        if (warp == 7) {                                     // G, in 64 bits: its differences count.  exp(-200) is 0, whatever is in front of it
+            double y[2];
             float b[2];
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
@@ -304,165 +346,203 @@ __global__ void __launch_bounds__(DELTA_PREP_THREADS) delta_prep_kernel(const De
                     b[e] = p.beta[(first + i) * p.beta_tok + h];
                 }
                 fine &= delta_finite(b[e]) && gi < INFINITY;
-                x[e] = gi < -200.f ? -200.0 : static_cast<double>(gi);
+                y[e] = gi < -200.f ? -200.0 : static_cast<double>(gi);
                 s_beta[i] = b[e];
             }
-            double sum = x[0] + x[1];
+            double sum = y[0] + y[1];
 #pragma unroll
             for (int o = 1; o < 32; o <<= 1) {
-                const double y = __shfl_up_sync(0xffffffffu, sum, o);
-                if (lane >= o) sum += y;
+                const double z = __shfl_up_sync(0xffffffffu, sum, o);
+                if (lane >= o) sum += z;
             }
             const double last = __shfl_sync(0xffffffffu, sum, 31);
-            s_g[2 * lane] = sum - x[1];
+            s_g[2 * lane] = sum - y[1];
             s_g[2 * lane + 1] = sum;
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
-                const double at = e ? sum : sum - x[1];
-                to->beta[2 * lane + e] = b[e];
-                to->past[2 * lane + e] = expf(static_cast<float>(at));
-                to->left[2 * lane + e] = expf(static_cast<float>(last - at));
+                const double at = e ? sum : sum - y[1];
+                to->x.beta[2 * lane + e] = b[e];
+                to->x.past[2 * lane + e] = expf(static_cast<float>(at));
+                to->x.left[2 * lane + e] = expf(static_cast<float>(last - at));
             }
             if (lane == 0) {
                 const double w = exp(last);
-                to->whole_hi = static_cast<float>(w);
-                to->whole_lo = static_cast<float>(w - static_cast<double>(static_cast<float>(w)));
+                to->x.whole_hi = static_cast<float>(w);
+                to->x.whole_lo = static_cast<float>(w - static_cast<double>(static_cast<float>(w)));
             }
         }
-        __syncthreads();
-        // ---- L into shared memory, A as the second kernel's operand -----------------------------------------------------------------
-        const double gr[2] = {s_g[warp * 16 + g], s_g[warp * 16 + g + 8]};
-        const float br[2] = {s_beta[warp * 16 + g], s_beta[warp * 16 + g + 8]};
+        __syncthreads();                                     // (and the tiles have been read: L and T go over them)
+        const double gr[2] = {s_g[block * 16 + g], s_g[block * 16 + g + 8]};
+        const float br[2] = {s_beta[block * 16 + g], s_beta[block * 16 + g + 8]};
 #pragma unroll
         for (int t = 0; t < 4; ++t) {                        // blocks of 16 columns
-            if (t > warp) break;
+            if (t > block) break;
             uint32_t ahi[4], alo[4];
 #pragma unroll
             for (int half = 0; half < 2; ++half) {           // 8 columns
                 const int j0 = t * 16 + half * 8 + 2 * c;
                 const double gc[2] = {s_g[j0], s_g[j0 + 1]};
-                float l[4], a[4];
+                float y[4];
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    const int i = warp * 16 + g + 8 * (e >> 1), j = j0 + (e & 1);
-                    const float d = j <= i ? expf(static_cast<float>(gr[e >> 1] - gc[e & 1])) : 0.f;
-                    a[e] = j <= i ? d * qk[2 * t + half][e] : 0.f;
-                    l[e] = j < i ? br[e >> 1] * d * kk[2 * t + half][e] : 0.f;
-                    fine &= delta_finite(a[e]) && delta_finite(l[e]) && (j != i || delta_finite(kk[2 * t + half][e]));
-                    if (t == warp) diag[warp * 16 * 17 + (g + 8 * (e >> 1)) * 17 + half * 8 + 2 * c + (e & 1)] = l[e];
+                    const int i = block * 16 + g + 8 * (e >> 1), j = j0 + (e & 1);
+                    const bool on = (scores ? j <= i : j < i) && i < n;
+                    const float d = expf(static_cast<float>(gr[e >> 1] - gc[e & 1]));
+                    y[e] = on ? (scores ? d : br[e >> 1] * d) * x[2 * t + half][e] : 0.f;
+                    fine &= delta_finite(y[e]) && (j != i || i >= n || delta_finite(x[2 * t + half][e]));
                 }
+                if (scores) {
 #pragma unroll
-                for (int e = 0; e < 2; ++e) {                // rows g, g + 8
-                    uint32_t hi, lo;
-                    delta_split(l[2 * e], l[2 * e + 1], hi, lo);
-                    uint8_t* at = l_mat + (warp * 16 + g + 8 * e) * DELTA_PITCH + j0 * 2;
-                    *reinterpret_cast<uint32_t*>(at) = hi;
-                    *reinterpret_cast<uint32_t*>(at + C::kMat) = lo;
-                    delta_split(a[2 * e], a[2 * e + 1], ahi[2 * half + e], alo[2 * half + e]);
+                    for (int e = 0; e < 2; ++e) delta_split(y[2 * e], y[2 * e + 1], ahi[2 * half + e], alo[2 * half + e]);
+                } else if (t == block) {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) diag[(g + 8 * (e >> 1)) * 17 + half * 8 + 2 * c + (e & 1)] = y[e];
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {            // rows g, g + 8
+                        uint32_t r[3];
+                        delta_split3(y[2 * e], y[2 * e + 1], r);
+                        uint8_t* at = smem + C::kL + delta_under(block, t) * DELTA_BLOCK + (g + 8 * e) * 48 + half * 16 + c * 4;
+#pragma unroll
+                        for (int part = 0; part < 3; ++part) *reinterpret_cast<uint32_t*>(at + part * 6 * DELTA_BLOCK) = r[part];
+                    }
                 }
             }
-            to->a[0][delta_tile(warp, t)][lane] = make_uint4(ahi[0], ahi[1], ahi[2], ahi[3]);
-            to->a[1][delta_tile(warp, t)][lane] = make_uint4(alo[0], alo[1], alo[2], alo[3]);
+            if (scores) {
+                to->a[0][delta_tile(block, t)][lane] = make_uint4(ahi[0], ahi[1], ahi[2], ahi[3]);
+                to->a[1][delta_tile(block, t)][lane] = make_uint4(alo[0], alo[1], alo[2], alo[3]);
+            }
         }
-        __syncwarp();
-        // ---- T's diagonal blocks, by substitution: lane j has column j ----------------------------------------------------------------
-        {
-            const float* l = diag + warp * 16 * 17;
+        if (!scores) {
+            // ---- T's diagonal blocks: lane j (and j + 16) has column j -------------------------------------------------------------------
+            __syncwarp();
             const int j = lane & 15;
-            float x[16];
+            float y[16];
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
-                float y = i == j ? 1.f : 0.f;
+                float z = i == j ? 1.f : 0.f;
 #pragma unroll
-                for (int k = 0; k < i; ++k) y = fmaf(-l[i * 17 + k], x[k], y);
-                x[i] = y;
-                const __nv_bfloat16 hi = __float2bfloat16_rn(y);
-                uint8_t* at = t_mat + (warp * 16 + i) * DELTA_PITCH + (warp * 16 + j) * 2;
-                if (lane < 16) *reinterpret_cast<__nv_bfloat16*>(at) = hi;
-                else *reinterpret_cast<__nv_bfloat16*>(at + C::kMat) = __float2bfloat16_rn(y - __bfloat162float(hi));
+                for (int k = 0; k < i; ++k) z = fmaf(-diag[i * 17 + k], y[k], z);
+                y[i] = z;
+                const __nv_bfloat16 hi = __float2bfloat16_rn(z);
+                const float rest = z - __bfloat162float(hi);
+                const __nv_bfloat16 mid = __float2bfloat16_rn(rest);
+                uint8_t* at = smem + C::kT + block * DELTA_BLOCK + i * 48 + j * 2;
+                if (lane < 16) {
+                    *reinterpret_cast<__nv_bfloat16*>(at) = hi;
+                } else {
+                    *reinterpret_cast<__nv_bfloat16*>(at + 4 * DELTA_BLOCK) = mid;
+                    *reinterpret_cast<__nv_bfloat16*>(at + 8 * DELTA_BLOCK) = __float2bfloat16_rn(rest - __bfloat162float(mid));
+                }
             }
-        }
-        __syncthreads();
-        // ---- the blocks under them: warp J has block column J, transposed:  T_IJ^T = -(sum_K T_KJ^T L_IK^T) T_II^T,  K = J .. I - 1 ----------
-        {
-            const int trow = ((lane >> 4) << 3) + (lane & 7), tcol = (lane >> 3) & 1;       // operand by rows of k (transposed load)
-            const int nrow = (lane & 7) + ((lane >> 4) << 3), ncol = (lane >> 3) & 1;
-            uint32_t xh[4][4], xl[4][4];                     // T_KJ^T, K = J + index
+            asm volatile("bar.sync 1, 128;" ::: "memory");   // (warps 0 to 3)
+            // T - 1 on the diagonal: its ones left out
             {
-                const uint32_t at = sm_t + (warp * 16 + trow) * DELTA_PITCH + warp * 32 + tcol * 16;
-                ldsm_x4_t(xh[0], at);
-                ldsm_x4_t(xl[0], at + C::kMat);
+                uint32_t r[2][4];
+#pragma unroll
+                for (int part = 0; part < 2; ++part) {
+                    ldsm_x4(r[part], sm + C::kT + part * 4 * DELTA_BLOCK + block * DELTA_BLOCK + (lane & 15) * 48 + (lane >> 4) * 16);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) fine &= delta_finite2(r[part][e]);
+                }
+                if (g == 2 * c) r[0][0] &= 0xffff0000u, r[0][3] &= 0xffff0000u;
+                if (g == 2 * c + 1) r[0][0] &= 0xffffu, r[0][3] &= 0xffffu;
+#pragma unroll
+                for (int part = 0; part < 2; ++part) to->t[part][delta_tile(block, block)][lane] = make_uint4(r[part][0], r[part][1], r[part][2], r[part][3]);
             }
+            // ---- the blocks under it ------------------------------------------------------------------------------------------------------
+            const int nrow = (lane & 7) + ((lane >> 4) << 3), ncol = (lane >> 3) & 1;
+            uint32_t xt[3][3][4];                            // T_KJ^T, K = J + index: three parts
+#pragma unroll
+            for (int part = 0; part < 3; ++part)
+                ldsm_x4_t(xt[0][part], sm + C::kT + (part * 4 + block) * DELTA_BLOCK + (((lane >> 4) << 3) + (lane & 7)) * 48 + ((lane >> 3) & 1) * 16);
 #pragma unroll
             for (int s = 1; s < 4; ++s) {                    // I = J + s
-                if (warp + s > 3) break;
-                const int I = warp + s;
-                float y[2][4] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}}, z[2][4] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+                if (block + s > 3) break;
+                const int I = block + s;
+                float y2[2][4] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}}, z2[2][4] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
 #pragma unroll
                 for (int k = 0; k < s; ++k) {
-                    uint32_t bh[4], bl[4];
-                    const uint32_t at = sm_l + (I * 16 + nrow) * DELTA_PITCH + (warp + k) * 32 + ncol * 16;
-                    ldsm_x4(bh, at);
-                    ldsm_x4(bl, at + C::kMat);
-                    delta_mma3(y[0], xh[k], xl[k], bh[0], bh[1], bl[0], bl[1]);
-                    delta_mma3(y[1], xh[k], xl[k], bh[2], bh[3], bl[2], bl[3]);
-                }
-                uint32_t yh[4], yl[4], bh[4], bl[4];
+                    uint32_t b[2][3][2];
 #pragma unroll
-                for (int e = 0; e < 4; ++e) delta_split(-y[e >> 1][2 * (e & 1)], -y[e >> 1][2 * (e & 1) + 1], yh[e], yl[e]);
-                const uint32_t at = sm_t + (I * 16 + nrow) * DELTA_PITCH + I * 32 + ncol * 16;
-                ldsm_x4(bh, at);
-                ldsm_x4(bl, at + C::kMat);
-                delta_mma3(z[0], yh, yl, bh[0], bh[1], bl[0], bl[1]);
-                delta_mma3(z[1], yh, yl, bh[2], bh[3], bl[2], bl[3]);
+                    for (int part = 0; part < 3; ++part) {
+                        uint32_t r[4];
+                        ldsm_x4(r, sm + C::kL + (part * 6 + delta_under(I, block + k)) * DELTA_BLOCK + nrow * 48 + ncol * 16);
+                        b[0][part][0] = r[0], b[0][part][1] = r[1], b[1][part][0] = r[2], b[1][part][1] = r[3];
+                    }
+                    delta_mma6(y2[0], xt[k], b[0]);
+                    delta_mma6(y2[1], xt[k], b[1]);
+                }
+                uint32_t ya[3][4], b[2][3][2];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    uint32_t r[3];
+                    delta_split3(-y2[e >> 1][2 * (e & 1)], -y2[e >> 1][2 * (e & 1) + 1], r);
+                    ya[0][e] = r[0], ya[1][e] = r[1], ya[2][e] = r[2];
+                }
+#pragma unroll
+                for (int part = 0; part < 3; ++part) {
+                    uint32_t r[4];
+                    ldsm_x4(r, sm + C::kT + (part * 4 + I) * DELTA_BLOCK + nrow * 48 + ncol * 16);
+                    b[0][part][0] = r[0], b[0][part][1] = r[1], b[1][part][0] = r[2], b[1][part][1] = r[3];
+                }
+                delta_mma6(z2[0], ya, b[0]);
+                delta_mma6(z2[1], ya, b[1]);
+                uint32_t out[2][4];
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {                // rows j = g + 8 (e & 1), columns i = 8 (e >> 1) + 2 c, + 1
-                    delta_split(z[e >> 1][2 * (e & 1)], z[e >> 1][2 * (e & 1) + 1], xh[s][e], xl[s][e]);
-                    uint8_t* to_t = t_mat + (I * 16 + 8 * (e >> 1) + 2 * c) * DELTA_PITCH + (warp * 16 + g + 8 * (e & 1)) * 2;
-                    *reinterpret_cast<uint16_t*>(to_t) = static_cast<uint16_t>(xh[s][e]);
-                    *reinterpret_cast<uint16_t*>(to_t + DELTA_PITCH) = static_cast<uint16_t>(xh[s][e] >> 16);
-                    *reinterpret_cast<uint16_t*>(to_t + C::kMat) = static_cast<uint16_t>(xl[s][e]);
-                    *reinterpret_cast<uint16_t*>(to_t + C::kMat + DELTA_PITCH) = static_cast<uint16_t>(xl[s][e] >> 16);
+                    uint32_t r[3];
+                    delta_split3(z2[e >> 1][2 * (e & 1)], z2[e >> 1][2 * (e & 1) + 1], r);
+                    if (s < 3) xt[s < 3 ? s : 0][0][e] = r[0], xt[s < 3 ? s : 0][1][e] = r[1], xt[s < 3 ? s : 0][2][e] = r[2];
+                    fine &= delta_finite2(r[0]);
+                    // the block itself: rows i = 8 (e >> 1) + g, columns j = 8 (e & 1) + 2 c, + 1
+#pragma unroll
+                    for (int part = 0; part < 2; ++part) out[part][(e >> 1) + 2 * (e & 1)] = delta_transpose(r[part]);
                 }
+#pragma unroll
+                for (int part = 0; part < 2; ++part) to->t[part][delta_tile(I, block)][lane] = make_uint4(out[part][0], out[part][1], out[part][2], out[part][3]);
             }
         }
-        __syncthreads();
-        for (int x = warp; x < 2 * DELTA_TILES; x += DELTA_PREP_THREADS / 32) {
-            const int part = x / DELTA_TILES, tile = x - part * DELTA_TILES;
-            const int i = tile >= 6 ? 3 : tile >= 3 ? 2 : tile >= 1 ? 1 : 0, j = tile - delta_tile(i, 0);
-            uint32_t r[4];
-            ldsm_x4(r, sm_t + part * C::kMat + (i * 16 + (lane & 15)) * DELTA_PITCH + j * 32 + (lane >> 4) * 16);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) fine &= (r[e] & 0x7f80u) != 0x7f80u && (r[e] & 0x7f800000u) != 0x7f800000u;
-            to->t[part][tile][lane] = make_uint4(r[0], r[1], r[2], r[3]);
-        }
         const bool wild = __syncthreads_or(!fine);
-        if (tid == 0) to->wild = wild ? 1 : 0;
+        if (tid == 0) to->x.wild = wild ? 1 : 0;
     }
 }
 
+// ---------------------------------------------------------------------------------------------------------------------
+// The walk along the chunks.  Eight warps share a chunk's products and meet three times a chunk: when the state's copy, R and U are in shared
+// memory.  Slices of 32 columns leave room for two CTAs per SM: K and the scalars are two chunks deep, Q's place is filled again behind the
+// chunk's first products, T and A take turns in one.  Slices of 16 (where there are few CTAs) have all of the next chunk's operands on their way.
 // ---------------------------------------------------------------------------------------------------------------------
 constexpr int DELTA_THREADS = 256;
 
 template <int DK, int NV>
 struct DeltaCfg {
-    static constexpr int kTile = DELTA_C * DK * 2;
-    static constexpr int kPitch = NV * 2 + 16;               // bytes of a row of NV bfloat16: an odd number of 16-byte words
-    static constexpr int kK = 0, kQ = kTile, kV = 2 * kTile, kChunk = kV + DELTA_C * kPitch;
-    static constexpr int kStage = kChunk + static_cast<int>(sizeof(DeltaChunk));
-    static constexpr int kStages = 2;
-    static constexpr int kS = kStages * kStage, kSPart = DK * kPitch;            // the state, high parts and low parts
-    static constexpr int kR = kS + 2 * kSPart, kRPart = DELTA_C * kPitch;
-    static constexpr int kU = kR + 2 * kRPart;                                   // U, then exp(G_n - G) U
-    static constexpr int kSum = kU + 4 * kRPart;                                 // token by token: a row of sums per warp
-    static constexpr int kSmemBytes = kSum + 8 * NV * 4;
+    static constexpr bool kDeep = NV == 16;                  // two of everything
+    static constexpr int kTile = DELTA_C * DK * 2, kBlocks = DELTA_TILES * 2 * 512;
+    static constexpr int kPitch = NV * 2;                    // bytes of a row of NV bfloat16
+    static constexpr int kK = 0, kQ = 2 * kTile, kT = kQ + (kDeep ? 2 : 1) * kTile;          // T, A or both in turn
+    static constexpr int kX = kT + (kDeep ? 4 : 1) * kBlocks, kXPitch = 1024;    // the scalars
+    static constexpr int kS = kX + 2 * kXPitch, kSPart = DK * kPitch;            // the state, three parts
+    static constexpr int kR = kS + 3 * kSPart, kRPart = DELTA_C * kPitch;        // two
+    static constexpr int kU = kR + 2 * kRPart;                                   // two
+    static constexpr int kW = kU + 2 * kRPart;                                   // exp(G_n - G) U, three
+    static constexpr int kSmemBytes = kW + 3 * kRPart;
+    static_assert(4 * NV * 4 <= 2 * kRPart, "token by token: sums in R's place");
 };
+// Where word w of a row lies: eight rows' words of one column in different banks.
+template <int NV>
+__device__ __forceinline__ int delta_place(int row, int w) { return row * (NV * 2) + ((NV == 32 ? w ^ ((row >> 1) & 3) : w ^ ((row >> 2) & 1)) << 4); }
 
 template <int DK, int NV>
-__global__ void __launch_bounds__(DELTA_THREADS, 1) delta_chunks_kernel(const DeltaParams p) {
+__global__ void __launch_bounds__(DELTA_THREADS, DeltaCfg<DK, NV>::kDeep ? 1 : 2)
+delta_chunks_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k, const DeltaParams p) {
     using C = DeltaCfg<DK, NV>;
-    constexpr int N = NV / 8;                                // products' column tiles
-    extern __shared__ __align__(128) uint8_t smem[];
+    constexpr int N = NV / 16;                               // product tiles of 8 columns of a warp: half of the slice
+    constexpr int M = DK / 64;                               // and of 16 rows of the state
+    extern __shared__ __align__(1024) uint8_t lin_smem[];    // (the loads' swizzle goes by the address)
+    uint8_t* smem = lin_smem;
+    __shared__ uint64_t s_k[2], s_q, s_t;                    // loads that have landed
+    __shared__ int s_late;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, c = lane & 3;
     const int slice = static_cast<int>(blockIdx.x % p.slices), h = static_cast<int>(blockIdx.x / p.slices % p.heads);
     const int seq = static_cast<int>(blockIdx.x / p.slices / p.heads), hk = h / p.group, col0 = slice * NV;
@@ -473,272 +553,391 @@ __global__ void __launch_bounds__(DELTA_THREADS, 1) delta_chunks_kernel(const De
     // the chunks that this launch has the operands of
     const int begin = static_cast<int>(max(0ll, min(static_cast<long long>(chunks), p.first_slot - slot0)));
     const int end = static_cast<int>(max(0ll, min(static_cast<long long>(chunks), p.last_slot - slot0)));
+    if (tid == 0) {
+        s_late = 0;
+        mbar_init(&s_k[0], 1);
+        mbar_init(&s_k[1], 1);
+        mbar_init(&s_q, 1);
+        mbar_init(&s_t, 1);
+        mbar_fence_init();
+    }
     griddep_wait();
-    if (!good && slice == 0 && h == 0 && tid == 0) p.hdr->error = 4u;            // MMV_ERR_BAD_SEGMENTS
+    if (!good && slice == 0 && h == 0 && tid == 0) report_error(p.hdr, 4u);      // MMV_ERR_BAD_SEGMENTS
+    if (smem_u32(smem) & 1023u) {                            // (never: the declaration asks for it)
+        if (tid == 0) report_error(p.hdr, 6u);               // MMV_ERR_CUDA
+        return;
+    }
     if (begin >= end && !(chunks == 0 && p.first_slot == 0)) return;
+    __syncthreads();
 
     const uint32_t sm = smem_u32(smem);
-    const auto fetch = [&](int chunk) {
-        const uint32_t dst = sm + (chunk & 1) * C::kStage;
-        const long long first = tok + static_cast<long long>(chunk) * DELTA_C;
-        const int n = min(DELTA_C, len - chunk * DELTA_C);
-        delta_fetch<DK, DELTA_THREADS>(dst + C::kK, p.k + first * p.k_tok + hk * p.k_head, p.k_tok, n, p.dk / 8, p.offsets);
-        delta_fetch<DK, DELTA_THREADS>(dst + C::kQ, p.q + first * p.q_tok + hk * p.q_head, p.q_tok, n, p.dk / 8, p.offsets);
-        const uint16_t* v = p.v + first * p.v_tok + h * p.v_head + col0;
-        for (int i = tid; i < DELTA_C * N; i += DELTA_THREADS) {
-            const int row = i / N, w = i - row * N;
-            const bool on = row < n && col0 + w * 8 < p.dv;
-            cp_async_16_or_zero(dst + C::kV + row * C::kPitch + w * 16, on ? static_cast<const void*>(v + row * p.v_tok + w * 8) : p.offsets, on);
+    const DeltaChunk* made = reinterpret_cast<const DeltaChunk*>(p.chunks) + (slot0 - p.first_slot) * p.heads + h;       // of chunk i: made[i * heads]
+    // ---- loads, each by one thread of another warp ---------------------------------------------------------------------------------
+    const auto load_keys = [&](int chunk) {                  // (kDeep: and all the rest)
+        const int i = (chunk - begin) & 1;
+        const DeltaChunk* from = made + static_cast<long long>(chunk) * p.heads;
+        mbar_arrive_expect_tx(&s_k[i], (C::kDeep ? 2 * C::kTile + 2 * C::kBlocks : C::kTile) + sizeof(DeltaScalars));
+#pragma unroll
+        for (int b = 0; b < DK / 64; ++b) {
+            tma_load_3d(smem + C::kK + i * C::kTile + b * DELTA_BOX, &map_k, &s_k[i], b * 64, hk, tok + chunk * DELTA_C);
+            if (C::kDeep) tma_load_3d(smem + C::kQ + i * C::kTile + b * DELTA_BOX, &map_q, &s_k[i], b * 64, hk, tok + chunk * DELTA_C);
         }
-        const uint8_t* src = p.chunks + ((slot0 + chunk - p.first_slot) * p.heads + h) * sizeof(DeltaChunk);
-        for (int i = tid; i < static_cast<int>(sizeof(DeltaChunk) / 16); i += DELTA_THREADS) cp_async_16_or_zero(dst + C::kChunk + i * 16, src + i * 16, true);
+        tma_load_1d(smem + C::kX + i * C::kXPitch, &from->x, sizeof(DeltaScalars), &s_k[i]);
+        if (C::kDeep) tma_load_1d(smem + C::kT + i * 2 * C::kBlocks, from->t, 2 * C::kBlocks, &s_k[i]);
     };
-    if (begin < end) fetch(begin);
-    cp_async_commit();
+    const auto load_queries = [&](int chunk) {
+        mbar_arrive_expect_tx(&s_q, C::kTile);
+#pragma unroll
+        for (int b = 0; b < DK / 64; ++b) tma_load_3d(smem + C::kQ + b * DELTA_BOX, &map_q, &s_q, b * 64, hk, tok + chunk * DELTA_C);
+    };
+    const auto load_blocks = [&](const void* from) {
+        mbar_arrive_expect_tx(&s_t, C::kBlocks);
+        tma_load_1d(smem + C::kT, from, C::kBlocks, &s_t);
+    };
+    if (begin < end && tid == 0) {
+        load_keys(begin);
+        if (!C::kDeep) {
+            load_queries(begin);
+            load_blocks(made[static_cast<long long>(begin) * p.heads].t);
+        }
+    }
+    // A load did not land in time: those in flight do before the CTA leaves.
+    const auto given_up = [&](int chunk) {
+        if (tid != 0) return;
+        report_error(p.hdr, 5u);                             // MMV_ERR_TIMEOUT
+        for (int i = 0; i < 2; ++i)
+            for (int parity = 0; parity < 2; ++parity) {
+                mbar_wait(&s_k[i], parity, 1000000);
+                mbar_wait(i ? &s_q : &s_t, parity, 1000000);
+            }
+    };
 
-    // ---- the state: rows 16 warp + g and + 8, columns 8 j + 2 c and + 1 of the slice ------------------------------------------------
-    float s[N][4];
-    const bool keeps = warp * 16 < DK;
+    // Of the tokens a warp has 16 (two warps of a scheduler together five of the triangles' blocks), of the state 16 M rows; of both, half of the
+    // slice's columns.
+    const int block = warp < 4 ? warp >> 1 : 3 - ((warp - 4) >> 1), half = warp & 1, row0 = (warp >> 1) * 16 * M;
+    const int mine = col0 + half * (NV / 2);                 // this warp's first column
+    // values of this lane's tokens, one chunk ahead
+    uint32_t v[N][2];
+    const auto values = [&](int chunk) {
+#pragma unroll
+        for (int j = 0; j < N; ++j)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                const int t = chunk * DELTA_C + block * 16 + g + 8 * e;
+                v[j][e] = 0u;
+                if (t < len && mine + j * 8 < p.dv)
+                    v[j][e] = *reinterpret_cast<const uint32_t*>(p.v + (static_cast<long long>(tok) + t) * p.v_tok + h * p.v_head + mine + j * 8 + 2 * c);
+            }
+    };
+    if (begin < end) values(begin);
+
+    // ---- the state: rows row0 + 16 m + g and + 8, columns 8 j + 2 c and + 1 of the warp's -----------------------------------------
+    float s[M][N][4];
     const float* from = begin > 0 ? p.state_out : p.state;
     const long long base = (static_cast<long long>(seq) * p.heads + h) * p.dk * p.dv;
-    const auto state_at = [&](int j, int e) { return base + static_cast<long long>(warp * 16 + g + 8 * e) * p.dv + col0 + j * 8 + 2 * c; };
-    const auto held = [&](int j, int e) { return keeps && warp * 16 + g + 8 * e < p.dk && col0 + j * 8 < p.dv; };
+    const auto state_at = [&](int m, int j, int e) { return base + static_cast<long long>(row0 + 16 * m + g + 8 * e) * p.dv + mine + j * 8 + 2 * c; };
+    const auto held = [&](int m, int j, int e) { return row0 + 16 * m + g + 8 * e < p.dk && mine + j * 8 < p.dv; };
 #pragma unroll
-    for (int j = 0; j < N; ++j)
+    for (int m = 0; m < M; ++m)
 #pragma unroll
-        for (int e = 0; e < 2; ++e) {
-            float2 x = make_float2(0.f, 0.f);
-            if (from && held(j, e)) x = *reinterpret_cast<const float2*>(from + state_at(j, e));
-            s[j][2 * e] = x.x;
-            s[j][2 * e + 1] = x.y;
-        }
+        for (int j = 0; j < N; ++j)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                float2 x = make_float2(0.f, 0.f);
+                if (from && held(m, j, e)) x = *reinterpret_cast<const float2*>(from + state_at(m, j, e));
+                s[m][j][2 * e] = x.x;
+                s[m][j][2 * e + 1] = x.y;
+            }
 
-    const int block = warp & 3;                              // this warp's 16 tokens; warps 0 to 3 form K S, the others Q S and the results
-    const bool queries = warp >= 4;
-    const int brow = lane & 15, bcol = lane >> 4;            // second operands: 16 rows, 16 columns
+    // 16 rows of two parts of tile j of this warp's columns as a product's second operand: the first part in b[0], b[1], the second in b[2], b[3]
+    const auto operand = [&](uint32_t (&b)[4], int matrix, int part, int row, int j) {
+        ldsm_x4_t(b, sm + matrix + (lane >> 4) * part + delta_place<NV>(row + (lane & 15), half * N + j));
+    };
+    // the third part of all tiles
+    const auto third = [&](uint32_t (&b)[N][2], int matrix, int row) {
+        if constexpr (N == 2) {
+            uint32_t r[4];
+            ldsm_x4_t(r, sm + matrix + delta_place<NV>(row + (lane & 15), half * N + (lane >> 4)));
+            b[0][0] = r[0], b[0][1] = r[1], b[1][0] = r[2], b[1][1] = r[3];
+        } else {
+            ldsm_x2_t(b[0][0], b[0][1], sm + matrix + delta_place<NV>(row + (lane & 15), half * N));
+        }
+    };
+    const auto address = [&](int matrix, int row, int j) { return smem + matrix + delta_place<NV>(row, half * N + j) + 4 * c; };
+    bool late = false;
     for (int chunk = begin; chunk < end; ++chunk) {
-        const uint32_t st = sm + (chunk & 1) * C::kStage;
-        const DeltaChunk* info = reinterpret_cast<const DeltaChunk*>(smem + (chunk & 1) * C::kStage + C::kChunk);
+        const int stage = (chunk - begin) & 1;
+        const uint32_t sm_k = sm + C::kK + stage * C::kTile, sm_q = sm + C::kQ + (C::kDeep ? stage * C::kTile : 0);
+        const uint4* blocks = reinterpret_cast<const uint4*>(smem + C::kT + (C::kDeep ? stage * 2 * C::kBlocks : 0));       // T, then (kDeep: behind it) A
+        const DeltaScalars* info = reinterpret_cast<const DeltaScalars*>(smem + C::kX + stage * C::kXPitch);
         const int n = min(DELTA_C, len - chunk * DELTA_C);
         // the state's copy for the products
-        if (keeps) {
+#pragma unroll
+        for (int m = 0; m < M; ++m)
 #pragma unroll
             for (int j = 0; j < N; ++j)
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
-                    uint32_t hi, lo;
-                    delta_split(s[j][2 * e], s[j][2 * e + 1], hi, lo);
-                    const uint32_t at = C::kS + (warp * 16 + g + 8 * e) * C::kPitch + (j * 8 + 2 * c) * 2;
-                    *reinterpret_cast<uint32_t*>(smem + at) = hi;
-                    *reinterpret_cast<uint32_t*>(smem + at + C::kSPart) = lo;
+                    uint32_t r[3];
+                    delta_split3(s[m][j][2 * e], s[m][j][2 * e + 1], r);
+                    uint8_t* at = address(C::kS, row0 + 16 * m + g + 8 * e, j);
+#pragma unroll
+                    for (int part = 0; part < 3; ++part) *reinterpret_cast<uint32_t*>(at + part * C::kSPart) = r[part];
                 }
+        late |= !mbar_wait(&s_k[stage], ((chunk - begin) >> 1) & 1, p.budget_ns);
+        if (!C::kDeep) late |= !mbar_wait(&s_q, (chunk - begin) & 1, p.budget_ns);
+        if (n < DELTA_C && !late) {                          // another sequence's keys: their weights of zero do not hide what is not finite
+            for (int i = tid; i < (DELTA_C - n) * (DK / 8); i += DELTA_THREADS)
+                *reinterpret_cast<uint4*>(smem + C::kK + stage * C::kTile + delta_word(n + i / (DK / 8), i % (DK / 8))) = make_uint4(0u, 0u, 0u, 0u);
+            fence_proxy_async_smem();
         }
-        cp_async_wait<0>();
-        __syncthreads();                                     // this chunk's operands and the state's copy are there
-        if (chunk + 1 < end) fetch(chunk + 1);
-        cp_async_commit();
+        if (__syncthreads_or(late)) {                        // (this chunk's operands and the state's copy are there)
+            given_up(chunk);
+            return;
+        }
+        if (chunk + 1 < end && tid == 0) load_keys(chunk + 1);
+        if (!C::kDeep && chunk > begin && tid == 64) load_blocks(made[static_cast<long long>(chunk) * p.heads].t);
 
-        // ---- K S, Q S ----------------------------------------------------------------------------------------------------------------
-        float x[N][4];
+        // ---- K S, Q S: 16 tokens each ------------------------------------------------------------------------------------------------
+        float x[N][4], y[N][4];
 #pragma unroll
-        for (int j = 0; j < N; ++j) x[j][0] = x[j][1] = x[j][2] = x[j][3] = 0.f;
+        for (int j = 0; j < N; ++j)
 #pragma unroll
-        for (int d = 0; d < DK / 16; ++d) {
-            uint32_t a[4];
-            ldsm_x4(a, st + (queries ? C::kQ : C::kK) + delta_at<DK>(block * 16 + (lane & 15), 2 * d + (lane >> 4)));
+            for (int e = 0; e < 4; ++e) x[j][e] = y[j][e] = 0.f;
+        {
+            uint32_t ak[2][4], aq[2][4], b[2][N][4], b3[2][N][2];                // (the next step's operands while this one's are used)
+            const auto load = [&](int d) {
+                const uint32_t at = delta_word(block * 16 + (lane & 15), 2 * d + (lane >> 4));
+                ldsm_x4(ak[d & 1], sm_k + at);
 #pragma unroll
-            for (int j = 0; j < N; j += 2) {
-                uint32_t hi[4], lo[4];
-                const uint32_t at = sm + C::kS + (d * 16 + brow) * C::kPitch + (j / 2) * 32 + bcol * 16;
-                ldsm_x4_t(hi, at);
-                ldsm_x4_t(lo, at + C::kSPart);
-                mma_16816<true>(x[j], a, hi[0], hi[1]);
-                mma_16816<true>(x[j + 1], a, hi[2], hi[3]);
-                mma_16816<true>(x[j], a, lo[0], lo[1]);
-                mma_16816<true>(x[j + 1], a, lo[2], lo[3]);
+                for (int j = 0; j < N; ++j) operand(b[d & 1][j], C::kS, C::kSPart, d * 16, j);
+                third(b3[d & 1], C::kS + 2 * C::kSPart, d * 16);
+                ldsm_x4(aq[d & 1], sm_q + at);
+            };
+            load(0);
+#pragma unroll
+            for (int d = 0; d < DK / 16; ++d) {
+                if (d + 1 < DK / 16) load(d + 1);
+                const int i = d & 1;
+#pragma unroll
+                for (int j = 0; j < N; ++j) mma_16816<true>(x[j], ak[i], b[i][j][0], b[i][j][1]);
+#pragma unroll
+                for (int j = 0; j < N; ++j) mma_16816<true>(y[j], aq[i], b[i][j][0], b[i][j][1]);
+#pragma unroll
+                for (int j = 0; j < N; ++j) mma_16816<true>(x[j], ak[i], b[i][j][2], b[i][j][3]);
+#pragma unroll
+                for (int j = 0; j < N; ++j) mma_16816<true>(y[j], aq[i], b[i][j][2], b[i][j][3]);
+#pragma unroll
+                for (int j = 0; j < N; ++j) mma_16816<true>(x[j], ak[i], b3[i][j][0], b3[i][j][1]);
             }
         }
+        // ---- R = b (V - exp(G) K S) ----------------------------------------------------------------------------------------------------
         const float past[2] = {info->past[block * 16 + g], info->past[block * 16 + g + 8]};
         bool wild = info->wild != 0;
-        if (!queries) {                                      // R = b (V - exp(G) K S)
+        {
             const float beta[2] = {info->beta[block * 16 + g], info->beta[block * 16 + g + 8]};
 #pragma unroll
             for (int j = 0; j < N; ++j)
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
                     const int row = block * 16 + g + 8 * e;
-                    const uint32_t vv = *reinterpret_cast<const uint32_t*>(smem + (chunk & 1) * C::kStage + C::kV + row * C::kPitch + (j * 8 + 2 * c) * 2);
-                    wild |= (vv & 0x7f80u) == 0x7f80u || (vv & 0x7f800000u) == 0x7f800000u;
-                    const float2 v = unpack_pair<true>(vv);
+                    asm volatile("" : "+r"(v[j][e]));        // (here, and not where the load was issued: it has had the products' time)
+                    wild |= !delta_finite2(v[j][e]);
+                    const float2 w = unpack_pair<true>(v[j][e]);
+                    const bool on = row < n;
+                    x[j][2 * e] = on ? beta[e] * (w.x - past[e] * x[j][2 * e]) : 0.f;
+                    x[j][2 * e + 1] = on ? beta[e] * (w.y - past[e] * x[j][2 * e + 1]) : 0.f;
                     uint32_t hi, lo;
-                    delta_split(beta[e] * (v.x - past[e] * x[j][2 * e]), beta[e] * (v.y - past[e] * x[j][2 * e + 1]), hi, lo);
-                    const uint32_t at = C::kR + row * C::kPitch + (j * 8 + 2 * c) * 2;
-                    *reinterpret_cast<uint32_t*>(smem + at) = hi;
-                    *reinterpret_cast<uint32_t*>(smem + at + C::kRPart) = lo;
+                    delta_split(x[j][2 * e], x[j][2 * e + 1], hi, lo);
+                    uint8_t* at = address(C::kR, row, j);
+                    *reinterpret_cast<uint32_t*>(at) = hi;
+                    *reinterpret_cast<uint32_t*>(at + C::kRPart) = lo;
                 }
         }
+        if (chunk + 1 < end) values(chunk + 1);
+        if (!C::kDeep && !mbar_wait(&s_t, 0, p.budget_ns)) { // (T and A take turns: T's loads complete its even phases)
+            *const_cast<volatile int*>(&s_late) = 1;
+            wild = true;
+        }
         wild = __syncthreads_or(wild);
-        uint16_t* out = p.out + ((static_cast<long long>(tok) + chunk * DELTA_C) * p.heads + h) * p.dv + col0;
+        if (!C::kDeep && chunk + 1 < end && tid == 128) load_queries(chunk + 1);
+        uint16_t* out = p.out + ((static_cast<long long>(tok) + chunk * DELTA_C) * p.heads + h) * p.dv;
         const long long orow = static_cast<long long>(p.heads) * p.dv;
         if (!wild) {
-            // ---- U = T R: 16 tokens, half of the columns ------------------------------------------------------------------------------
-            {
-                constexpr int H = N / 2;
-                const int j0 = queries ? H : 0;
-                float u[H][4], y[H][4];
+            // ---- U = R + (T - 1) R ---------------------------------------------------------------------------------------------------------
+            const uint4* solver = blocks + delta_tile(block, 0) * 32 + lane;
+            float z[N][4];
 #pragma unroll
-                for (int j = 0; j < H; ++j)
+            for (int j = 0; j < N; ++j)
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) u[j][e] = y[j][e] = 0.f;
+                for (int e = 0; e < 4; ++e) z[j][e] = 0.f;
 #pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    if (k > block) break;
-                    const uint4 th = info->t[0][delta_tile(block, 0) + k][lane], tl = info->t[1][delta_tile(block, 0) + k][lane];
-                    const uint32_t ah[4] = {th.x, th.y, th.z, th.w}, al[4] = {tl.x, tl.y, tl.z, tl.w};
+            for (int k = 0; k < 4; ++k) {
+                if (k > block) break;
+                const uint4 th = solver[k * 32], tl = solver[(DELTA_TILES + k) * 32];
+                const uint32_t ah[4] = {th.x, th.y, th.z, th.w}, al[4] = {tl.x, tl.y, tl.z, tl.w};
 #pragma unroll
-                    for (int j = 0; j < H; j += 2) {
-                        uint32_t hi[4], lo[4];
-                        // (an odd number of tiles, NV = 16: the loads' other 8 columns are not used)
-                        const uint32_t at = sm + C::kR + (k * 16 + brow) * C::kPitch + (H == 1 ? j0 * 16 : (j0 + j) * 16 + bcol * 16);
-                        ldsm_x4_t(hi, at);
-                        ldsm_x4_t(lo, at + C::kRPart);
-                        mma_16816<true>(u[j], ah, hi[0], hi[1]);
-                        mma_16816<true>(y[j], al, hi[0], hi[1]);
-                        if (H > 1) {
-                            mma_16816<true>(u[j + 1 < H ? j + 1 : j], ah, hi[2], hi[3]);
-                            mma_16816<true>(y[j + 1 < H ? j + 1 : j], al, hi[2], hi[3]);
-                        }
-                        mma_16816<true>(y[j], ah, lo[0], lo[1]);
-                        if (H > 1) mma_16816<true>(y[j + 1 < H ? j + 1 : j], ah, lo[2], lo[3]);
-                    }
+                for (int j = 0; j < N; ++j) {
+                    uint32_t b[4];
+                    operand(b, C::kR, C::kRPart, k * 16, j);
+                    mma_16816<true>(x[j], ah, b[0], b[1]);
+                    mma_16816<true>(z[j], al, b[0], b[1]);
+                    mma_16816<true>(z[j], ah, b[2], b[3]);
                 }
-                const float left[2] = {info->left[block * 16 + g], info->left[block * 16 + g + 8]};
-#pragma unroll
-                for (int j = 0; j < H; ++j)
-#pragma unroll
-                    for (int e = 0; e < 2; ++e) {
-                        const float a = u[j][2 * e] + y[j][2 * e], b = u[j][2 * e + 1] + y[j][2 * e + 1];
-                        uint32_t hi, lo;
-                        uint8_t* at = smem + C::kU + (block * 16 + g + 8 * e) * C::kPitch + ((j0 + j) * 8 + 2 * c) * 2;
-                        delta_split(a, b, hi, lo);
-                        *reinterpret_cast<uint32_t*>(at) = hi;
-                        *reinterpret_cast<uint32_t*>(at + C::kRPart) = lo;
-                        delta_split(a * left[e], b * left[e], hi, lo);
-                        *reinterpret_cast<uint32_t*>(at + 2 * C::kRPart) = hi;
-                        *reinterpret_cast<uint32_t*>(at + 3 * C::kRPart) = lo;
-                    }
             }
+            const float left[2] = {info->left[block * 16 + g], info->left[block * 16 + g + 8]};
+#pragma unroll
+            for (int j = 0; j < N; ++j)
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    const float a = x[j][2 * e] + z[j][2 * e], b = x[j][2 * e + 1] + z[j][2 * e + 1];
+                    uint32_t r[3];
+                    delta_split(a, b, r[0], r[1]);
+                    uint8_t* at = address(C::kU, block * 16 + g + 8 * e, j);
+                    *reinterpret_cast<uint32_t*>(at) = r[0];
+                    *reinterpret_cast<uint32_t*>(at + C::kRPart) = r[1];
+                    delta_split3(a * left[e], b * left[e], r);
+                    at += C::kW - C::kU;
+#pragma unroll
+                    for (int part = 0; part < 3; ++part) *reinterpret_cast<uint32_t*>(at + part * C::kRPart) = r[part];
+                }
             __syncthreads();
+            if (!C::kDeep && tid == 192) load_blocks(made[static_cast<long long>(chunk) * p.heads].a);
             // ---- S' = exp(G_n) S + K^T (exp(G_n - G) U) -----------------------------------------------------------------------------------
-            if (keeps) {
-                const float wh = info->whole_hi, wl = info->whole_lo;
+            const float wh = info->whole_hi, wl = info->whole_lo;
+#pragma unroll
+            for (int m = 0; m < M; ++m)
 #pragma unroll
                 for (int j = 0; j < N; ++j)
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) s[j][e] = fmaf(s[j][e], wh, s[j][e] * wl);
+                    for (int e = 0; e < 4; ++e) s[m][j][e] = fmaf(s[m][j][e], wh, s[m][j][e] * wl);
+            {
+                uint32_t a[2][M][4], b[2][N][4], b3[2][N][2];
+                const auto load = [&](int k) {
+#pragma unroll
+                    for (int m = 0; m < M; ++m)
+                        ldsm_x4_t(a[k & 1][m], sm_k + delta_word(k * 16 + ((lane >> 4) << 3) + (lane & 7), (row0 >> 3) + 2 * m + ((lane >> 3) & 1)));
+                    third(b3[k & 1], C::kW + 2 * C::kRPart, k * 16);
+#pragma unroll
+                    for (int j = 0; j < N; ++j) operand(b[k & 1][j], C::kW, C::kRPart, k * 16, j);
+                };
+                load(0);
 #pragma unroll
                 for (int k = 0; k < 4; ++k) {
-                    uint32_t a[4];
-                    ldsm_x4_t(a, st + C::kK + delta_at<DK>(k * 16 + ((lane >> 4) << 3) + (lane & 7), warp * 2 + ((lane >> 3) & 1)));
+                    if (k < 3) load(k + 1);
+                    const int i = k & 1;
 #pragma unroll
-                    for (int j = 0; j < N; j += 2) {
-                        uint32_t hi[4], lo[4];
-                        const uint32_t at = sm + C::kU + 2 * C::kRPart + (k * 16 + brow) * C::kPitch + (j / 2) * 32 + bcol * 16;
-                        ldsm_x4_t(hi, at);
-                        ldsm_x4_t(lo, at + C::kRPart);
-                        mma_16816<true>(s[j], a, hi[0], hi[1]);
-                        mma_16816<true>(s[j + 1], a, hi[2], hi[3]);
-                        mma_16816<true>(s[j], a, lo[0], lo[1]);
-                        mma_16816<true>(s[j + 1], a, lo[2], lo[3]);
-                    }
+                    for (int j = 0; j < N; ++j)
+#pragma unroll
+                        for (int m = 0; m < M; ++m) mma_16816<true>(s[m][j], a[i][m], b3[i][j][0], b3[i][j][1]);
+#pragma unroll
+                    for (int j = 0; j < N; ++j)
+#pragma unroll
+                        for (int m = 0; m < M; ++m) mma_16816<true>(s[m][j], a[i][m], b[i][j][2], b[i][j][3]);
+#pragma unroll
+                    for (int j = 0; j < N; ++j)
+#pragma unroll
+                        for (int m = 0; m < M; ++m) mma_16816<true>(s[m][j], a[i][m], b[i][j][0], b[i][j][1]);
                 }
             }
             // ---- O = scale (exp(G) Q S + A U) ---------------------------------------------------------------------------------------------
-            if (queries) {
 #pragma unroll
-                for (int j = 0; j < N; ++j)
+            for (int j = 0; j < N; ++j)
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) x[j][e] *= past[e >> 1];
+                for (int e = 0; e < 4; ++e) y[j][e] *= past[e >> 1];
+            if (!C::kDeep) late |= !mbar_wait(&s_t, 1, p.budget_ns);             // (A's complete the odd ones)
+            const uint4* scores = blocks + (C::kDeep ? 2 * DELTA_TILES * 32 : 0) + delta_tile(block, 0) * 32 + lane;
 #pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    if (k > block) break;
-                    const uint4 th = info->a[0][delta_tile(block, 0) + k][lane], tl = info->a[1][delta_tile(block, 0) + k][lane];
-                    const uint32_t ah[4] = {th.x, th.y, th.z, th.w}, al[4] = {tl.x, tl.y, tl.z, tl.w};
+            for (int k = 0; k < 4; ++k) {
+                if (k > block) break;
+                const uint4 th = scores[k * 32], tl = scores[(DELTA_TILES + k) * 32];
+                const uint32_t ah[4] = {th.x, th.y, th.z, th.w}, al[4] = {tl.x, tl.y, tl.z, tl.w};
 #pragma unroll
-                    for (int j = 0; j < N; j += 2) {
-                        uint32_t hi[4], lo[4];
-                        const uint32_t at = sm + C::kU + (k * 16 + brow) * C::kPitch + (j / 2) * 32 + bcol * 16;
-                        ldsm_x4_t(hi, at);
-                        ldsm_x4_t(lo, at + C::kRPart);
-                        delta_mma3(x[j], ah, al, hi[0], hi[1], lo[0], lo[1]);
-                        delta_mma3(x[j + 1], ah, al, hi[2], hi[3], lo[2], lo[3]);
-                    }
+                for (int j = 0; j < N; ++j) {
+                    uint32_t b[4];
+                    operand(b, C::kU, C::kRPart, k * 16, j);
+                    delta_mma3(y[j], ah, al, b[0], b[1], b[2], b[3]);
                 }
-#pragma unroll
-                for (int j = 0; j < N; ++j)
-#pragma unroll
-                    for (int e = 0; e < 2; ++e) {
-                        const int row = block * 16 + g + 8 * e;
-                        if (row < n && col0 + j * 8 < p.dv)
-                            *reinterpret_cast<uint32_t*>(out + row * orow + j * 8 + 2 * c) = pack_pair<true>(p.scale * x[j][2 * e], p.scale * x[j][2 * e + 1]);
-                    }
             }
-        } else {
-            // ---- token by token: the recurrence as it stands ------------------------------------------------------------------------------
-            float* sums = reinterpret_cast<float*>(smem + C::kSum);
-            const auto column_sums = [&](const float (&w)[2], int j, float (&r)[2]) {       // over this warp's rows
-                r[0] = w[0] * s[j][0] + w[1] * s[j][2];
-                r[1] = w[0] * s[j][1] + w[1] * s[j][3];
 #pragma unroll
-                for (int o = 4; o < 32; o <<= 1) {
-                    r[0] += __shfl_xor_sync(0xffffffffu, r[0], o);
-                    r[1] += __shfl_xor_sync(0xffffffffu, r[1], o);
+            for (int j = 0; j < N; ++j)
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    const int row = block * 16 + g + 8 * e;
+                    if (row < n && mine + j * 8 < p.dv)
+                        *reinterpret_cast<uint32_t*>(out + row * orow + mine + j * 8 + 2 * c) = pack_pair<true>(p.scale * y[j][2 * e], p.scale * y[j][2 * e + 1]);
                 }
-            };
+        } else {
+            if (*const_cast<volatile int*>(&s_late)) {
+                given_up(chunk);
+                return;
+            }
+            if (!C::kDeep && tid == 192) {                   // (not used, but its turn)
+                load_blocks(made[static_cast<long long>(chunk) * p.heads].a);
+                late |= !mbar_wait(&s_t, 1, p.budget_ns);
+            }
+            // ---- token by token: the recurrence as it stands ---------------------------------------------------
+            float* sums = reinterpret_cast<float*>(smem + C::kR);
+            constexpr int PARTS = 4;                         // of the state's rows: warps of one half
             for (int t = 0; t < n; ++t) {
                 const long long at = tok + static_cast<long long>(chunk) * DELTA_C + t;
                 const LinDecay d = lin_decay(p.decay[at * p.decay_tok + h], 1);
-                const float beta = p.beta[at * p.beta_tok + h];
-                float kr[2] = {0.f, 0.f}, qr[2] = {0.f, 0.f};
+                const float b = p.beta[at * p.beta_tok + h];
+                float kr[M][2], qr[M][2];
 #pragma unroll
-                for (int e = 0; e < 2; ++e) {
-                    const int row = warp * 16 + g + 8 * e;
-                    if (keeps && row < p.dk) {
-                        kr[e] = lin_load<true>(p.k + at * p.k_tok + hk * p.k_head + row);
-                        qr[e] = lin_load<true>(p.q + at * p.q_tok + hk * p.q_head + row);
+                for (int m = 0; m < M; ++m)
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        const int row = row0 + 16 * m + g + 8 * e;
+                        kr[m][e] = row < p.dk ? lin_load<true>(p.k + at * p.k_tok + hk * p.k_head + row) : 0.f;
+                        qr[m][e] = row < p.dk ? lin_load<true>(p.q + at * p.q_tok + hk * p.q_head + row) : 0.f;
                     }
-                }
 #pragma unroll 1
                 for (int turn = 0; turn < 2; ++turn) {       // k S, then q S'
 #pragma unroll
                     for (int j = 0; j < N; ++j) {
-                        float r[2];
-                        column_sums(turn ? qr : kr, j, r);
+                        float r[2] = {0.f, 0.f};
+#pragma unroll
+                        for (int m = 0; m < M; ++m)
+#pragma unroll
+                            for (int i = 0; i < 4; ++i)      // (rows past dk hold zero and weigh zero)
+                                r[i & 1] = fmaf(turn ? qr[m][i >> 1] : kr[m][i >> 1], s[m][j][i], r[i & 1]);
+#pragma unroll
+                        for (int o = 4; o < 32; o <<= 1) {
+                            r[0] += __shfl_xor_sync(0xffffffffu, r[0], o);
+                            r[1] += __shfl_xor_sync(0xffffffffu, r[1], o);
+                        }
                         if (g == 0) {
-                            sums[warp * NV + j * 8 + 2 * c] = r[0];
-                            sums[warp * NV + j * 8 + 2 * c + 1] = r[1];
+                            float* to = sums + (warp >> 1) * NV + half * (NV / 2) + j * 8 + 2 * c;
+                            to[0] = r[0];
+                            to[1] = r[1];
                         }
                     }
                     __syncthreads();
                     if (turn) {
                         if (tid < NV && col0 + tid < p.dv) {
-                            float y = 0.f;
-                            for (int w = 0; w < DELTA_THREADS / 32 && w * 16 < p.dk; ++w) y += sums[w * NV + tid];
-                            out[t * orow + tid] = lin_store<true>(p.scale * y);
+                            float sum = 0.f;
+#pragma unroll
+                            for (int w = 0; w < PARTS; ++w) sum += sums[w * NV + tid];
+                            out[t * orow + col0 + tid] = lin_store<true>(p.scale * sum);
                         }
                     } else {
 #pragma unroll
                         for (int j = 0; j < N; ++j)
 #pragma unroll
                             for (int e = 0; e < 2; ++e) {
-                                const int col = j * 8 + 2 * c + e;
-                                float y = 0.f;
-                                for (int w = 0; w < DELTA_THREADS / 32 && w * 16 < p.dk; ++w) y += sums[w * NV + col];
-                                const float v = col0 + col < p.dv ? lin_load<true>(p.v + at * p.v_tok + h * p.v_head + col0 + col) : 0.f;
-                                const float u = beta * (v - fmaf(y, d.hi, y * d.lo));
+                                const int col = half * (NV / 2) + j * 8 + 2 * c + e;
+                                float sum = 0.f;
 #pragma unroll
-                                for (int i = 0; i < 2; ++i)
-                                    if (warp * 16 + g + 8 * i < p.dk) s[j][2 * i + e] = fmaf(s[j][2 * i + e], d.hi, fmaf(s[j][2 * i + e], d.lo, kr[i] * u));
+                                for (int w = 0; w < PARTS; ++w) sum += sums[w * NV + col];
+                                const float value = col0 + col < p.dv ? lin_load<true>(p.v + at * p.v_tok + h * p.v_head + col0 + col) : 0.f;
+                                const float ut = b * (value - fmaf(sum, d.hi, sum * d.lo));
+#pragma unroll
+                                for (int m = 0; m < M; ++m)
+#pragma unroll
+                                    for (int i = 0; i < 2; ++i)
+                                        if (row0 + 16 * m + g + 8 * i < p.dk)
+                                            s[m][j][2 * i + e] = fmaf(s[m][j][2 * i + e], d.hi, fmaf(s[m][j][2 * i + e], d.lo, kr[m][i] * ut));
                             }
                     }
                     __syncthreads();
@@ -746,11 +945,14 @@ __global__ void __launch_bounds__(DELTA_THREADS, 1) delta_chunks_kernel(const De
             }
         }
     }
+    if (late) report_error(p.hdr, 5u);                       // MMV_ERR_TIMEOUT
 #pragma unroll
-    for (int j = 0; j < N; ++j)
+    for (int m = 0; m < M; ++m)
 #pragma unroll
-        for (int e = 0; e < 2; ++e)
-            if (held(j, e)) *reinterpret_cast<float2*>(p.state_out + state_at(j, e)) = make_float2(s[j][2 * e], s[j][2 * e + 1]);
+        for (int j = 0; j < N; ++j)
+#pragma unroll
+            for (int e = 0; e < 2; ++e)
+                if (held(m, j, e)) *reinterpret_cast<float2*>(p.state_out + state_at(m, j, e)) = make_float2(s[m][j][2 * e], s[m][j][2 * e + 1]);
 }
 
 }  // namespace mmv

@@ -119,23 +119,6 @@ int linear_ctas(const mmv_linear_inputs* in, int64_t nseq, int64_t ntok, int sms
 struct LinearMaps {
     CUtensorMap q, k, v;
 };
-// [token][head][column] as boxes of 64 columns of one head of 64 tokens; what lies outside reads as zero.
-bool linear_map(CUtensorMap* map, const void* x, int dim, int heads, int64_t ntok, int64_t stride_head, int64_t stride_token) {
-    EncodeTiledFn enc = get_encode();
-    if (!enc) return false;
-    if (ntok == 0) {                                                  // never read
-        *map = CUtensorMap{};
-        return true;
-    }
-    const cuuint64_t row = static_cast<cuuint64_t>(dim) * 2;
-    const cuuint64_t dims[3] = {static_cast<cuuint64_t>(dim), static_cast<cuuint64_t>(heads), static_cast<cuuint64_t>(ntok)};
-    const cuuint64_t strides[2] = {heads > 1 ? static_cast<cuuint64_t>(stride_head) * 2 : row,
-                                   ntok > 1 ? static_cast<cuuint64_t>(stride_token) * 2 : row * static_cast<cuuint64_t>(heads)};
-    const cuuint32_t box[3] = {64, 1, LIN_C}, estr[3] = {1, 1, 1};
-    return enc(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(x), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
-               CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
-}
-
 template <int DK>
 mmv_status launch_linear(const LinearMaps& m, const LinParams& p, int ctas, cudaStream_t st) {
     const mmv_status rc = launch(linear_chunks_kernel<DK, true>, dim3(static_cast<unsigned>(ctas)), LIN_THREADS, LinCfg<DK, true>::kSmemBytes,
@@ -386,9 +369,9 @@ mmv_status mmv_linear_attention(const mmv_linear_inputs* in, const int32_t* offs
     p.carry = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + sizeof(WorkspaceHeader));
     p.budget_ns = g_budget_ns.load();
     LinearMaps maps;
-    if (!linear_map(&maps.q, in->q, in->dim_k, in->heads, ntok, in->q_stride_head, in->q_stride_token) ||
-        !linear_map(&maps.k, in->k, in->dim_k, in->kv_heads, ntok, in->k_stride_head, in->k_stride_token) ||
-        !linear_map(&maps.v, in->v, in->dim_v, in->kv_heads, ntok, in->v_stride_head, in->v_stride_token))
+    if (!token_map(&maps.q, in->q, in->dim_k, in->heads, ntok, in->q_stride_head, in->q_stride_token) ||
+        !token_map(&maps.k, in->k, in->dim_k, in->kv_heads, ntok, in->k_stride_head, in->k_stride_token) ||
+        !token_map(&maps.v, in->v, in->dim_v, in->kv_heads, ntok, in->v_stride_head, in->v_stride_token))
         return MMV_ERR_INVALID_ARG;
     const int ctas = linear_ctas(in, nseq, ntok, dev->sm_count);
     return in->dim_k <= 64 ? launch_linear<64>(maps, p, ctas, st) : launch_linear<128>(maps, p, ctas, st);

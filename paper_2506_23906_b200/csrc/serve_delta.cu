@@ -1,5 +1,6 @@
 // Host side of the gated delta rule of include/mmv.h: argument checks, workspace carve-up and launches.
 #include <cstdint>
+#include <cuda.h>
 #include <cuda_runtime.h>
 
 #include "../../include/mmv.h"
@@ -67,12 +68,12 @@ int64_t places_at_once(const mmv_delta_inputs* in, int64_t nseq, int64_t ntok) {
 }
 
 template <int DK>
-mmv_status launch_delta(const DeltaParams& p, int64_t places, int nv, cudaStream_t st) {
+mmv_status launch_delta(const CUtensorMap& q, const CUtensorMap& k, const DeltaParams& p, int64_t places, int nv, cudaStream_t st) {
     const unsigned prep = static_cast<unsigned>(places * (p.heads / p.group)), ctas = static_cast<unsigned>(static_cast<int64_t>(p.nseq) * p.heads * p.slices);
-    const mmv_status rc = launch(delta_prep_kernel<DK>, dim3(prep), DELTA_PREP_THREADS, DeltaPrepCfg<DK>::kSmemBytes, st, false, p);
+    const mmv_status rc = launch(delta_prep_kernel<DK>, dim3(prep), DELTA_PREP_THREADS, DeltaPrepCfg<DK>::kSmemBytes, st, false, q, k, p);
     if (rc != MMV_OK) return rc;
-    return nv == 16 ? launch(delta_chunks_kernel<DK, 16>, dim3(ctas), DELTA_THREADS, DeltaCfg<DK, 16>::kSmemBytes, st, true, p)
-                    : launch(delta_chunks_kernel<DK, 32>, dim3(ctas), DELTA_THREADS, DeltaCfg<DK, 32>::kSmemBytes, st, true, p);
+    return nv == 16 ? launch(delta_chunks_kernel<DK, 16>, dim3(ctas), DELTA_THREADS, DeltaCfg<DK, 16>::kSmemBytes, st, true, q, k, p)
+                    : launch(delta_chunks_kernel<DK, 32>, dim3(ctas), DELTA_THREADS, DeltaCfg<DK, 32>::kSmemBytes, st, true, q, k, p);
 }
 
 }  // namespace
@@ -138,7 +139,13 @@ mmv_status mmv_gated_delta(const mmv_delta_inputs* in, const int32_t* offsets, i
     p.ntok = static_cast<int>(ntok);
     p.hdr = static_cast<WorkspaceHeader*>(workspace);
     p.chunks = static_cast<uint8_t*>(workspace) + sizeof(WorkspaceHeader);
-    const int nv = 32;
+    p.budget_ns = g_budget_ns.load();
+    CUtensorMap map_q, map_k;
+    if (!token_map(&map_q, in->q, in->dim_k, in->key_heads, ntok, in->q_stride_head, in->q_stride_token) ||
+        !token_map(&map_k, in->k, in->dim_k, in->key_heads, ntok, in->k_stride_head, in->k_stride_token))
+        return MMV_ERR_INVALID_ARG;
+    // Slices of 32 columns, of 16 where those leave half of the SMs idle.
+    const int nv = nseq * p.heads * ((p.dv + 31) / 32) <= dev->sm_count / 2 ? 16 : 32;
     p.slices = (p.dv + nv - 1) / nv;
     if (nseq * p.heads > INT32_MAX / p.slices) return MMV_ERR_INVALID_ARG;       // one CTA per (sequence, head) and slice
     const int64_t all = all_places(nseq, ntok), step = places_at_once(in, nseq, ntok);
@@ -146,7 +153,7 @@ mmv_status mmv_gated_delta(const mmv_delta_inputs* in, const int32_t* offsets, i
         p.first_slot = at;
         p.last_slot = at + step < all ? at + step : all;
         const int64_t places = p.last_slot - at;
-        const mmv_status rc = in->dim_k <= 64 ? launch_delta<64>(p, places, nv, st) : launch_delta<128>(p, places, nv, st);
+        const mmv_status rc = in->dim_k <= 64 ? launch_delta<64>(map_q, map_k, p, places, nv, st) : launch_delta<128>(map_q, map_k, p, places, nv, st);
         if (rc != MMV_OK) return rc;
     }
     return MMV_OK;

@@ -2,6 +2,7 @@
 #pragma once
 #include <atomic>
 #include <cstdint>
+#include <cuda.h>
 #include <cuda_runtime.h>
 #include <mutex>
 
@@ -72,6 +73,23 @@ mmv_status launch(void (*kernel)(KP...), dim3 grid, int threads, size_t smem, cu
     if (err == cudaSuccess) return MMV_OK;
     cudaGetLastError();
     return MMV_ERR_CUDA;
+}
+
+// [token][head][column] as boxes of 64 columns of one head of 64 tokens, 128-byte swizzle; what lies outside reads as zero.
+inline bool token_map(CUtensorMap* map, const void* x, int dim, int heads, int64_t ntok, int64_t stride_head, int64_t stride_token) {
+    EncodeTiledFn enc = get_encode();
+    if (!enc) return false;
+    if (ntok == 0) {                                                  // never read
+        *map = CUtensorMap{};
+        return true;
+    }
+    const cuuint64_t row = static_cast<cuuint64_t>(dim) * 2;
+    const cuuint64_t dims[3] = {static_cast<cuuint64_t>(dim), static_cast<cuuint64_t>(heads), static_cast<cuuint64_t>(ntok)};
+    const cuuint64_t strides[2] = {heads > 1 ? static_cast<cuuint64_t>(stride_head) * 2 : row,
+                                   ntok > 1 ? static_cast<cuuint64_t>(stride_token) * 2 : row * static_cast<cuuint64_t>(heads)};
+    const cuuint32_t box[3] = {64, 1, 64}, estr[3] = {1, 1, 1};
+    return enc(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(x), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+               CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
 inline bool value_type(int dt) { return dt == MMV_F16_TO_F32 || dt == MMV_BF16_TO_F32; }
