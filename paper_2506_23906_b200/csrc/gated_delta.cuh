@@ -215,6 +215,12 @@ __device__ __forceinline__ bool delta_finite2(uint32_t pair) { return (pair & 0x
 __device__ __forceinline__ void ldsm_x2_t(uint32_t& a, uint32_t& b, uint32_t addr) {
     asm volatile("ldmatrix.sync.aligned.m8n8.x2.trans.shared.b16 {%0, %1}, [%2];" : "=r"(a), "=r"(b) : "r"(addr) : "memory");
 }
+// 2^(a - b) for sums of two values each (2^-22 of it; small results are kept down to the smallest fp32)
+__device__ __forceinline__ float delta_decay(float2 a, float2 b) {
+    float r;
+    asm("ex2.approx.f32 %0, %1;" : "=f"(r) : "f"((a.x - b.x) + (a.y - b.y)));
+    return r;
+}
 // an 8 x 8 matrix of 16-bit values, as a product leaves its results, transposed
 __device__ __forceinline__ uint32_t delta_transpose(uint32_t x) {
     uint32_t r;
@@ -227,12 +233,13 @@ constexpr int DELTA_BOX = DELTA_C * 128;                     // bytes of 64 toke
 __device__ __forceinline__ uint32_t delta_word(int row, int c) { return (c >> 3) * DELTA_BOX + row * 128 + (((c & 7) ^ (row & 7)) << 4); }
 
 // ---------------------------------------------------------------------------------------------------------------------
-// T and A of one chunk, for the value heads of one key head.  Warps 0 to 3 form K K^T and from it T, 16 rows (then 16 columns) each, warps 4 to 7
-// Q K^T and A.  T's diagonal blocks of 16 x 16 are found by substitution in fp32; warp J then goes down block column J, transposed:
+// T and A of one chunk, for the value heads of one key head, 16 x 16 blocks at a time.  Warps 0 to 3 form K K^T on the diagonal and from it T's
+// diagonal blocks by substitution in fp32, warps 4 to 7 the blocks under it and those of Q K^T.  Then warp J goes down T's block column J, transposed:
 //     T_IJ^T = -(sum_K T_KJ^T L_IK^T) T_II^T,  K = J .. I - 1
 // where the results of one product are the first operand of the next as they lie in registers (all operands of three parts).
 // ---------------------------------------------------------------------------------------------------------------------
 constexpr int DELTA_PREP_THREADS = 256;
+constexpr int DELTA_DIAG = 20;                               // floats of a row of a block on the diagonal
 constexpr int DELTA_BLOCK = 16 * 48;                         // bytes of a 16 x 16 block of bfloat16: rows of three 16-byte words, so that eight meet all banks
 
 template <int DK>
@@ -241,7 +248,7 @@ struct DeltaPrepCfg {
     static constexpr int kL = 0;                             // (over the tiles, when those have been read) L's six blocks under the diagonal, three parts
     static constexpr int kT = kL + 3 * 6 * DELTA_BLOCK;      // T's four on the diagonal
     static constexpr int kDiag = kT + 3 * 4 * DELTA_BLOCK;   // L's, fp32
-    static constexpr int kWork = kDiag + 4 * 16 * 17 * 4;
+    static constexpr int kWork = kDiag + 4 * 16 * DELTA_DIAG * 4;
     static constexpr int kSmemBytes = 2 * kTile > kWork ? 2 * kTile : kWork;
 };
 __device__ __forceinline__ int delta_under(int i, int j) { return i * (i - 1) / 2 + j; }       // j < i
@@ -257,13 +264,13 @@ __device__ __forceinline__ void delta_mma6(float (&d)[4], const uint32_t (&a)[3]
 }
 
 template <int DK>
-__global__ void __launch_bounds__(DELTA_PREP_THREADS, 2)
+__global__ void __launch_bounds__(DELTA_PREP_THREADS, 3)
 delta_prep_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k, const DeltaParams p) {
     using C = DeltaPrepCfg<DK>;
     extern __shared__ __align__(1024) uint8_t lin_smem[];    // (the loads' swizzle goes by the address)
     uint8_t* smem = lin_smem;
     __shared__ uint64_t s_full;
-    __shared__ double s_g[DELTA_C];
+    __shared__ float2 s_g[DELTA_C];
     __shared__ float s_beta[DELTA_C];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, c = lane & 3;
     griddep_launch_dependents();
@@ -294,6 +301,54 @@ delta_prep_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_consta
             tma_load_3d(smem + C::kTile + b * DELTA_BOX, &map_q, &s_full, b * 64, hk, first);
         }
     }
+    // decays and betas of a value head (warp 7), on their way while the tiles land
+    float gi[2] = {0.f, 0.f}, bi[2] = {0.f, 0.f};
+    const auto gates = [&](int h) {
+#pragma unroll
+        for (int e = 0; e < 2; ++e)
+            if (2 * lane + e < n) {
+                gi[e] = p.decay[(first + 2 * lane + e) * p.decay_tok + h];
+                bi[e] = p.beta[(first + 2 * lane + e) * p.beta_tok + h];
+            }
+    };
+    // Their sums G / ln 2, in 64 bits and kept as two fp32 values: its differences count.  exp(-200) is 0, whatever is in front of it.
+    bool fine_gates = true;
+    const auto sums = [&](DeltaChunk* to) {
+        double y[2];
+        fine_gates = true;
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            fine_gates &= delta_finite(bi[e]) && gi[e] < INFINITY;
+            y[e] = (gi[e] < -200.f ? -200.0 : static_cast<double>(gi[e])) * 1.4426950408889634;
+            s_beta[2 * lane + e] = bi[e];
+        }
+        double sum = y[0] + y[1];
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const double z = __shfl_up_sync(0xffffffffu, sum, o);
+            if (lane >= o) sum += z;
+        }
+        const double last = __shfl_sync(0xffffffffu, sum, 31);
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            const double at = e ? sum : sum - y[1];
+            const float hi = static_cast<float>(at);
+            s_g[2 * lane + e] = make_float2(hi, static_cast<float>(at - hi));
+            to->x.beta[2 * lane + e] = bi[e];
+            to->x.past[2 * lane + e] = exp2f(static_cast<float>(at));
+            to->x.left[2 * lane + e] = exp2f(static_cast<float>(last - at));
+        }
+        if (lane == 0) {
+            const double w = exp2(last);
+            to->x.whole_hi = static_cast<float>(w);
+            to->x.whole_lo = static_cast<float>(w - static_cast<double>(static_cast<float>(w)));
+        }
+    };
+    if (warp == 7) {
+        gates(hk * p.group);
+        sums(reinterpret_cast<DeltaChunk*>(p.chunks) + (slot - p.first_slot) * p.heads + hk * p.group);
+        if (p.group > 1) gates(hk * p.group + 1);
+    }
     __syncthreads();
     const bool late = !mbar_wait(&s_full, 0, p.budget_ns);
     if (__syncthreads_or(late)) {
@@ -304,115 +359,120 @@ delta_prep_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_consta
         return;
     }
 
-    // ---- K K^T or Q K^T: a warp's 16 rows, columns up to the diagonal's ------------------------------------------------------------
+    // ---- a warp's blocks of K K^T and Q K^T -------------------------------------------------------------------------------------------
     const bool scores = warp >= 4;
     const int block = warp & 3;
     const uint32_t sm = smem_u32(smem);
-    float x[8][4];
+    // block t of this warp: its row of blocks, its column, and whether it is of Q K^T
+    const auto which = [&](int t, int& i, int& j) {
+        const int u = t == 0 ? block : t == 1 && block < 2 ? 4 + block : -1;     // warps 4 to 7: K K^T's blocks 0 to 5 under the diagonal, two, two, one, one ...
+        if (!scores) {
+            i = j = block;
+            return false;
+        }
+        if (u >= 0) {
+            i = u >= 3 ? 3 : u >= 1 ? 2 : 1;
+            j = u - i * (i - 1) / 2;
+            return false;
+        }
+        const int w = block < 2 ? block * 2 + t - 2 : 4 + (block - 2) * 3 + t - 1;                 // ... and Q K^T's 0 to 9: two, two, three, three
+        i = w >= 6 ? 3 : w >= 3 ? 2 : w >= 1 ? 1 : 0;
+        j = w - delta_tile(i, 0);
+        return true;
+    };
+    float x[4][2][4];
 #pragma unroll
-    for (int j = 0; j < 8; ++j)
+    for (int t = 0; t < 4; ++t) {
+        if (t > 0 && !scores) break;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) x[j][e] = 0.f;
+        for (int e = 0; e < 4; ++e) x[t][0][e] = x[t][1][e] = 0.f;
+        int i, j;
+        const bool of_q = which(t, i, j);
+        const uint32_t ta = sm + (of_q ? C::kTile : 0);
 #pragma unroll
-    for (int d = 0; d < DK / 16; ++d) {
-        uint32_t a[4];
-        ldsm_x4(a, sm + (scores ? C::kTile : 0) + delta_word(block * 16 + (lane & 15), 2 * d + (lane >> 4)));
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            if (j > block) break;
-            uint32_t b[4];
+        for (int d = 0; d < DK / 16; ++d) {
+            uint32_t a[4], b[4];
+            ldsm_x4(a, ta + delta_word(i * 16 + (lane & 15), 2 * d + (lane >> 4)));
             ldsm_x4(b, sm + delta_word(j * 16 + (lane & 7) + ((lane >> 4) << 3), 2 * d + ((lane >> 3) & 1)));
-            mma_16816<true>(x[2 * j], a, b[0], b[1]);
-            mma_16816<true>(x[2 * j + 1], a, b[2], b[3]);
+            mma_16816<true>(x[t][0], a, b[0], b[1]);
+            mma_16816<true>(x[t][1], a, b[2], b[3]);
         }
     }
 
-    float* diag = reinterpret_cast<float*>(smem + C::kDiag) + block * 16 * 17;
+    float* diag = reinterpret_cast<float*>(smem + C::kDiag) + block * 16 * DELTA_DIAG;
     for (int rep = 0; rep < p.group; ++rep) {
         const int h = hk * p.group + rep;
         DeltaChunk* to = reinterpret_cast<DeltaChunk*>(p.chunks) + (slot - p.first_slot) * p.heads + h;
-        bool fine = true;
-        if (rep) __syncthreads();                            // (the last head's numbers have been used)
-        if (warp == 7) {                                     // G, in 64 bits: its differences count.  exp(-200) is 0, whatever is in front of it
-            double y[2];
-            float b[2];
-#pragma unroll
-            for (int e = 0; e < 2; ++e) {
-                const int i = 2 * lane + e;
-                float gi = 0.f;
-                b[e] = 0.f;
-                if (i < n) {
-                    gi = p.decay[(first + i) * p.decay_tok + h];
-                    b[e] = p.beta[(first + i) * p.beta_tok + h];
-                }
-                fine &= delta_finite(b[e]) && gi < INFINITY;
-                y[e] = gi < -200.f ? -200.0 : static_cast<double>(gi);
-                s_beta[i] = b[e];
-            }
-            double sum = y[0] + y[1];
-#pragma unroll
-            for (int o = 1; o < 32; o <<= 1) {
-                const double z = __shfl_up_sync(0xffffffffu, sum, o);
-                if (lane >= o) sum += z;
-            }
-            const double last = __shfl_sync(0xffffffffu, sum, 31);
-            s_g[2 * lane] = sum - y[1];
-            s_g[2 * lane + 1] = sum;
-#pragma unroll
-            for (int e = 0; e < 2; ++e) {
-                const double at = e ? sum : sum - y[1];
-                to->x.beta[2 * lane + e] = b[e];
-                to->x.past[2 * lane + e] = expf(static_cast<float>(at));
-                to->x.left[2 * lane + e] = expf(static_cast<float>(last - at));
-            }
-            if (lane == 0) {
-                const double w = exp(last);
-                to->x.whole_hi = static_cast<float>(w);
-                to->x.whole_lo = static_cast<float>(w - static_cast<double>(static_cast<float>(w)));
-            }
+        if (rep) {
+            __syncthreads();                                 // (the last head's numbers have been used)
+            if (warp == 7) sums(to);
+            if (warp == 7 && rep + 1 < p.group) gates(h + 1);
         }
         __syncthreads();                                     // (and the tiles have been read: L and T go over them)
-        const double gr[2] = {s_g[block * 16 + g], s_g[block * 16 + g + 8]};
-        const float br[2] = {s_beta[block * 16 + g], s_beta[block * 16 + g + 8]};
+        bool fine = fine_gates;
+        float odd = 0.f;                                     // a sum of 0 times everything: 0, or NaN
 #pragma unroll
-        for (int t = 0; t < 4; ++t) {                        // blocks of 16 columns
-            if (t > block) break;
-            uint32_t ahi[4], alo[4];
+        for (int t = 0; t < 4; ++t) {
+            if (t > 0 && !scores) break;
+            int bi, bj;
+            const bool of_q = which(t, bi, bj);
+            float y[2][4];
+            if (bi == bj) {                                  // rows g, g + 8 by columns 2 c, + 1, + 8, + 9
+                const float2 gr[2] = {s_g[bi * 16 + g], s_g[bi * 16 + g + 8]};
 #pragma unroll
-            for (int half = 0; half < 2; ++half) {           // 8 columns
-                const int j0 = t * 16 + half * 8 + 2 * c;
-                const double gc[2] = {s_g[j0], s_g[j0 + 1]};
-                float y[4];
+                for (int half = 0; half < 2; ++half) {
+                    const int j0 = half * 8 + 2 * c;
+                    const float2 gc[2] = {s_g[bi * 16 + j0], s_g[bi * 16 + j0 + 1]};
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const int i = block * 16 + g + 8 * (e >> 1), j = j0 + (e & 1);
-                    const bool on = (scores ? j <= i : j < i) && i < n;
-                    const float d = expf(static_cast<float>(gr[e >> 1] - gc[e & 1]));
-                    y[e] = on ? (scores ? d : br[e >> 1] * d) * x[2 * t + half][e] : 0.f;
-                    fine &= delta_finite(y[e]) && (j != i || i >= n || delta_finite(x[2 * t + half][e]));
-                }
-                if (scores) {
-#pragma unroll
-                    for (int e = 0; e < 2; ++e) delta_split(y[2 * e], y[2 * e + 1], ahi[2 * half + e], alo[2 * half + e]);
-                } else if (t == block) {
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) diag[(g + 8 * (e >> 1)) * 17 + half * 8 + 2 * c + (e & 1)] = y[e];
-                } else {
-#pragma unroll
-                    for (int e = 0; e < 2; ++e) {            // rows g, g + 8
-                        uint32_t r[3];
-                        delta_split3(y[2 * e], y[2 * e + 1], r);
-                        uint8_t* at = smem + C::kL + delta_under(block, t) * DELTA_BLOCK + (g + 8 * e) * 48 + half * 16 + c * 4;
-#pragma unroll
-                        for (int part = 0; part < 3; ++part) *reinterpret_cast<uint32_t*>(at + part * 6 * DELTA_BLOCK) = r[part];
+                    for (int e = 0; e < 4; ++e) {
+                        const int i = g + 8 * (e >> 1), j = j0 + (e & 1);
+                        const bool in = bi * 16 + i < n;
+                        y[half][e] = in && (of_q ? j <= i : j < i) ? delta_decay(gr[e >> 1], gc[e & 1]) * x[t][half][e] : 0.f;
+                        if (in && j == i) odd = fmaf(x[t][half][e], 0.f, odd);
                     }
                 }
+            } else {
+                // D_ij = exp(G_i - G_m) exp(G_m - G_j) with m the first of the block's rows: both are 1 at most
+                const float2 gm = s_g[bi * 16];
+                const float rf[2] = {delta_decay(s_g[bi * 16 + g], gm), delta_decay(s_g[bi * 16 + g + 8], gm)};
+#pragma unroll
+                for (int half = 0; half < 2; ++half) {
+                    const int j0 = bj * 16 + half * 8 + 2 * c;
+                    const float cf[2] = {delta_decay(gm, s_g[j0]), delta_decay(gm, s_g[j0 + 1])};
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) y[half][e] = bi * 16 + g + 8 * (e >> 1) < n ? rf[e >> 1] * cf[e & 1] * x[t][half][e] : 0.f;
+                }
             }
-            if (scores) {
-                to->a[0][delta_tile(block, t)][lane] = make_uint4(ahi[0], ahi[1], ahi[2], ahi[3]);
-                to->a[1][delta_tile(block, t)][lane] = make_uint4(alo[0], alo[1], alo[2], alo[3]);
+            if (!of_q) {
+                const float br[2] = {s_beta[bi * 16 + g], s_beta[bi * 16 + g + 8]};
+#pragma unroll
+                for (int e = 0; e < 8; ++e) y[e >> 2][e & 3] *= br[(e >> 1) & 1];
             }
+#pragma unroll
+            for (int e = 0; e < 8; ++e) odd = fmaf(y[e >> 2][e & 3], 0.f, odd);
+            if (of_q) {
+                uint32_t hi[4], lo[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) delta_split(y[e >> 1][2 * (e & 1)], y[e >> 1][2 * (e & 1) + 1], hi[e], lo[e]);
+                to->a[0][delta_tile(bi, bj)][lane] = make_uint4(hi[0], hi[1], hi[2], hi[3]);
+                to->a[1][delta_tile(bi, bj)][lane] = make_uint4(lo[0], lo[1], lo[2], lo[3]);
+            } else if (!scores) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    *reinterpret_cast<float2*>(diag + (g + 8 * (e & 1)) * DELTA_DIAG + (e >> 1) * 8 + 2 * c) = make_float2(y[e >> 1][2 * (e & 1)], y[e >> 1][2 * (e & 1) + 1]);
+            } else {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    uint32_t r[3];
+                    delta_split3(y[e >> 1][2 * (e & 1)], y[e >> 1][2 * (e & 1) + 1], r);
+                    uint8_t* at = smem + C::kL + delta_under(bi, bj) * DELTA_BLOCK + (g + 8 * (e & 1)) * 48 + (e >> 1) * 16 + c * 4;
+#pragma unroll
+                    for (int part = 0; part < 3; ++part) *reinterpret_cast<uint32_t*>(at + part * 6 * DELTA_BLOCK) = r[part];
+                }
+            }
+            if (scores && t == (block < 2 ? 1 : 0)) asm volatile("bar.arrive 1, 256;" ::: "memory");       // (its blocks of L are there)
         }
+        fine &= odd == 0.f;
         if (!scores) {
             // ---- T's diagonal blocks: lane j (and j + 16) has column j -------------------------------------------------------------------
             __syncwarp();
@@ -422,10 +482,19 @@ delta_prep_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_consta
             for (int i = 0; i < 16; ++i) {
                 float z = i == j ? 1.f : 0.f;
 #pragma unroll
-                for (int k = 0; k < i; ++k) z = fmaf(-diag[i * 17 + k], y[k], z);
+                for (int k = 0; k < i; k += 4) {             // (L is zero from the diagonal on)
+                    const float4 l = *reinterpret_cast<const float4*>(diag + i * DELTA_DIAG + k);
+                    z = fmaf(-l.x, y[k], z);
+                    if (k + 1 < i) z = fmaf(-l.y, y[k + 1], z);
+                    if (k + 2 < i) z = fmaf(-l.z, y[k + 2], z);
+                    if (k + 3 < i) z = fmaf(-l.w, y[k + 3], z);
+                }
                 y[i] = z;
-                const __nv_bfloat16 hi = __float2bfloat16_rn(z);
-                const float rest = z - __bfloat162float(hi);
+            }
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                const __nv_bfloat16 hi = __float2bfloat16_rn(y[i]);
+                const float rest = y[i] - __bfloat162float(hi);
                 const __nv_bfloat16 mid = __float2bfloat16_rn(rest);
                 uint8_t* at = smem + C::kT + block * DELTA_BLOCK + i * 48 + j * 2;
                 if (lane < 16) {
@@ -435,7 +504,7 @@ delta_prep_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_consta
                     *reinterpret_cast<__nv_bfloat16*>(at + 8 * DELTA_BLOCK) = __float2bfloat16_rn(rest - __bfloat162float(mid));
                 }
             }
-            asm volatile("bar.sync 1, 128;" ::: "memory");   // (warps 0 to 3)
+            asm volatile("bar.sync 1, 256;" ::: "memory");   // (the other diagonal blocks, and L under them: warps 4 to 7 have arrived)
             // T - 1 on the diagonal: its ones left out
             {
                 uint32_t r[2][4];
