@@ -611,11 +611,22 @@ delta_chunks_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_cons
     extern __shared__ __align__(1024) uint8_t lin_smem[];    // (the loads' swizzle goes by the address)
     uint8_t* smem = lin_smem;
     __shared__ uint64_t s_k[2], s_q, s_t;                    // loads that have landed
-    __shared__ int s_late;
+    __shared__ int s_late, s_seq;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, c = lane & 3;
     const int slice = static_cast<int>(blockIdx.x % p.slices), h = static_cast<int>(blockIdx.x / p.slices % p.heads);
-    const int seq = static_cast<int>(blockIdx.x / p.slices / p.heads), hk = h / p.group, col0 = slice * NV;
-    int tok, len;
+    const int hk = h / p.group, col0 = slice * NV;
+    int seq = static_cast<int>(blockIdx.x / p.slices / p.heads), tok, len;
+    if (p.nseq <= DELTA_THREADS) {                           // the longest sequences first (16 of 32768 tokens in all: a last wave of half of the time)
+        int* s_len = reinterpret_cast<int*>(smem + C::kS);
+        lin_sequence(p.offsets, p.ntok, min(tid, p.nseq - 1), tok, len);
+        s_len[tid] = tid < p.nseq ? len : -1;
+        __syncthreads();
+        int rank = 0;
+        for (int i = 0; i < p.nseq; ++i) rank += s_len[i] > len || (s_len[i] == len && i < tid);
+        if (tid < p.nseq && rank == seq) s_seq = tid;
+        __syncthreads();
+        seq = s_seq;
+    }
     const bool good = lin_sequence(p.offsets, p.ntok, seq, tok, len);
     const int chunks = (len + DELTA_C - 1) / DELTA_C;
     const long long slot0 = delta_slot(tok, seq);

@@ -61,7 +61,7 @@ DeltaParams params_of(const mmv_delta_inputs* in, float scale, void* out) {
 
 // Places of chunks (delta_slot): all of them, and those that one pair of launches takes, whose operands the workspace holds.
 int64_t all_places(int64_t nseq, int64_t ntok) { return ntok / DELTA_C + nseq; }
-constexpr int64_t kPlaces = 8192;                            // (chunk, head)s: 174 MB
+constexpr int64_t kPlaces = 9216;                            // (chunk, head)s: 196 MB
 int64_t places_at_once(const mmv_delta_inputs* in, int64_t nseq, int64_t ntok) {
     const int64_t most = kPlaces / in->heads, all = all_places(nseq, ntok);
     return all < most ? all : most;
