@@ -7,8 +7,7 @@
 #include <cuda_fp16.h>
 #include "common.cuh"
 #include "linear_attn.cuh"
-#include "paged_attn.cuh"
-#include "kv_cache_q8.cuh"
+#include "paged_attn_q8.cuh"
 
 namespace mmv {
 
@@ -221,13 +220,6 @@ __device__ __forceinline__ float delta_decay(float2 a, float2 b) {
     asm("ex2.approx.f32 %0, %1;" : "=f"(r) : "f"((a.x - b.x) + (a.y - b.y)));
     return r;
 }
-// an 8 x 8 matrix of 16-bit values, as a product leaves its results, transposed
-__device__ __forceinline__ uint32_t delta_transpose(uint32_t x) {
-    uint32_t r;
-    asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(x));
-    return r;
-}
-
 constexpr int DELTA_BOX = DELTA_C * 128;                     // bytes of 64 tokens x 64 columns, as the loads leave them
 // Word c of a token's row in a tile of 64 tokens x DK columns: boxes of 64 columns, 128-byte swizzle.
 __device__ __forceinline__ uint32_t delta_word(int row, int c) { return (c >> 3) * DELTA_BOX + row * 128 + (((c & 7) ^ (row & 7)) << 4); }
@@ -566,7 +558,7 @@ delta_prep_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_consta
                     fine &= delta_finite2(r[0]);
                     // the block itself: rows i = 8 (e >> 1) + g, columns j = 8 (e & 1) + 2 c, + 1
 #pragma unroll
-                    for (int part = 0; part < 2; ++part) out[part][(e >> 1) + 2 * (e & 1)] = delta_transpose(r[part]);
+                    for (int part = 0; part < 2; ++part) out[part][(e >> 1) + 2 * (e & 1)] = matrix_transpose(r[part]);
                 }
 #pragma unroll
                 for (int part = 0; part < 2; ++part) to->t[part][delta_tile(I, block)][lane] = make_uint4(out[part][0], out[part][1], out[part][2], out[part][3]);

@@ -2,19 +2,23 @@
 //
 //     s_j = scale (q . code^k_j) ks_j,   out = sum_j softmax(s)_j vs_j code^v_j,   lse = log sum_j exp s_j       (ks, vs: the scales of j's block)
 //
-// The split over CTAs, the order of the units and the join of cut (request, head)s are those of the attention over a 16-bit cache
-// (paged_attn.cuh).  What differs:
+// The split over CTAs and the join of cut parts are those of the attention over a 16-bit cache (paged_attn.cuh).  What differs:
+//   The four warps of a CTA take neighbouring key heads of the same 16 tokens, not 64 tokens of one: a token's codes of one head are 128 bytes or less,
+//     and memory answers at half of its rate where those of the next head are asked for at another time (4 requests of 131072 tokens, 8 heads of 128: 256 us,
+//     whatever the arithmetic).  With two heads, or one, two or four warps share a head's tokens.
 //   Codes become fp16 in registers (every int8 and e4m3 value is one) and both products run in fp16.  A bfloat16 query is brought
 //     into fp16's range by a power of two of its own row, exactly but for values 2^29 times smaller than the row's largest.
+//   Both products are taken transposed: tokens (16), then columns of the result (16) are a product's rows, and up to 8 query heads its columns,
+//     so that codes are the first operand as they come, and few heads cost half as many products and registers. The weights of up to
+//     four heads fill the 8 columns with their high and low parts.
 //   The columns of a query and of a key may be taken in any order that both share: a lane takes 16 neighbouring columns of a token's
 //     key with one load, four of them for each of four products.  Values are read transposed in pairs of columns (8-bit
-//     columns 2d and 2d + 1 are one 16-bit element) and taken apart by a byte permutation: a product's result columns are the even, or
-//     the odd ones.
+//     columns 2d and 2d + 1 are one 16-bit element) and taken apart by a byte permutation: the even columns are a product's first 8
+//     rows, the odd ones the others.
 //   Scales of values are part of the weights that meet the codes: 2^(s_j + log2 vs_j - m'), with a running maximum m' of its own, so that no
 //     scale leaves fp16's range; the weights of the sum are 2^(s_j - m).
 //
-// What bounds it: HBM, 2 dim bytes per token and key head, with about 380 instructions per 16 tokens of a warp beside them (5 for four int8
-// codes), half of what the issue slots allow at that rate: so more warps per SM than the 16-bit kernel has.
+// What bounds it: HBM, 2 dim bytes per token and key head, and the instructions beside them (5 for four int8 codes).
 #pragma once
 #include <cstdint>
 #include "kv_cache_q8.cuh"
@@ -22,28 +26,73 @@
 
 namespace mmv {
 
+constexpr int Q8_TOKENS = 32;                                // of a warp in one tile: two groups of 16
+
 struct PagedQ8Params : PagedParams {                         // (k and v of the base are not used)
     const uint8_t *k8, *v8;
     const float *ks, *vs;
     long long s_block, s_head;
-    float* part_m2;                                          // [grid][2][PA_ROWS]: maximum of the values' weights (less LIFT)
-};
+    uint32_t by_block;                                       // floor(2^32 / block_size)
+    int side;                                                // key heads side by side: 1, 2 or 4
+    int tile, groups;                                        // tokens of a unit: 128 / side; groups of key heads, times parts
+    uint64_t budget_ns;                                      // bound of every wait
+    float* part_m2;                                          // [grid][2][side][PA_ROWS]: maximum of the values' weights (less LIFT)
+};                                                           // (part_ml: [grid][2][side][2][PA_ROWS], part_o: [grid][2][side][rows][dim])
 
-template <int DP>
+__device__ __forceinline__ PagedSpan q8_span(const PagedQ8Params& p, int r) {
+    PagedSpan s = paged_span(p, r);
+    s.tiles = s.len > 0 ? static_cast<int>((static_cast<unsigned>(s.len - s.first) + p.tile - 1) / static_cast<unsigned>(p.tile)) : 0;
+    return s;
+}
+__device__ __forceinline__ void q8_enter(const PagedQ8Params& p, PagedIter& it) {
+    const PagedSpan s = q8_span(p, it.r);
+    it.begin = s.begin;
+    it.len = s.len;
+    it.first = s.first;
+    it.tiles = s.tiles;
+}
+// the next unit (the caller knows that there is one); true where a new (request, heads) begins
+__device__ __forceinline__ bool q8_next(const PagedQ8Params& p, PagedIter& it) {
+    if (++it.tile < it.tiles) return false;
+    it.tile = 0;
+    if (++it.hp == p.groups) {
+        it.hp = 0;
+        do {
+            ++it.r;
+            q8_enter(p, it);
+        } while (it.tiles == 0);
+    }
+    return true;
+}
+
+template <int DP, int ROWS>
 struct PagedQ8Cfg {
     static constexpr int kStages = 2;
-    static constexpr int kPerSm = DP == 256 ? 2 : 3;                           // CTAs that the registers allow
-    static constexpr int kRow = DP;                                            // bytes of a token's codes
-    static constexpr int kChunks = DP / 16;                                    // 16-byte words of it
-    static constexpr int kCodes = PA_TOKENS * kRow * 2;                        // keys and values of a warp's tokens
-    static constexpr int kStage = kCodes + PA_TOKENS * 8;                      // and their scales
-    static constexpr int kQ = PA_ROWS * DP * 2;
-    static constexpr int kQSlots = kStages + 1;
-    static constexpr int kPitch = DP + 8;                                      // floats of a row where warps meet
+    static constexpr int kPerSm = ROWS == 16 && DP == 256 ? 2 : 3;             // CTAs that the registers allow (168 per thread)
+    static constexpr int kChunks = DP / 16;                                    // 16-byte words of a token's codes
+    static constexpr int kBox = DP < 128 ? DP : 128;                           // bytes of a row in shared memory: longer ones lie in two halves
+    static constexpr int kGroup = 16 * DP, kKeys = 2 * kGroup;                 // of 16 tokens' keys; of a warp's, their values behind them
+    static constexpr int kStage = 2 * kKeys;
+    static constexpr int kScales = Q8_TOKENS * 8;
+    static constexpr int kPitch = DP / 2 + 8;                                  // floats of half a row where warps meet
     static constexpr int kAll = PA_WARPS * kStages * kStage;
-    static int smem_bytes(int rows) { return kAll + kQSlots * kQ + PA_WARPS * rows * kPitch * 4; }
+    static constexpr int kOOff = kAll + PA_WARPS * kStages * kScales;
+    static int smem_bytes(int rows) { return kOOff + PA_WARPS * rows * kPitch * 4; }
+    // Where word c of token `row` of 16 lies: eight rows' words of one column are in different banks (128-byte swizzle, 64-byte swizzle for short rows), and the
+    // tokens of a product's columns n = 0 .. 7 are taken in an order in which two neighbouring ones' four words are, too.
+    static __device__ __forceinline__ int place(int row, int c) {
+        return DP < 128 ? row * 64 + ((c ^ ((row >> 1) & 3)) << 4) : (c >> 3) * 2048 + row * 128 + (((c & 7) ^ (row & 7)) << 4);
+    }
+    static __device__ __forceinline__ int token(int n) { return DP < 128 ? n : (n & 8) | ((n & 1) << 2) | ((n & 7) >> 1); }
 };
 
+// Bounded wait that sleeps in the barrier instruction (a turn of a loop that polls takes issue slots from the warps that work).
+static __device__ __noinline__ bool q8_wait(uint64_t* bar, uint32_t parity, uint64_t budget_ns) {
+    const uint64_t t0 = global_timer_ns();
+    while (!mbar_try_wait_for(bar, parity, 20000u))
+        if (global_timer_ns() - t0 > budget_ns) return false;
+    return true;
+}
 __device__ __forceinline__ void cp_async_4_or_zero(uint32_t dst, const void* src, bool on) {
     const int bytes = on ? 4 : 0;
     asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
@@ -58,9 +107,20 @@ __device__ __forceinline__ float2 lds_float2(uint32_t addr) {
     asm volatile("ld.shared.v2.f32 {%0, %1}, [%2];" : "=f"(r.x), "=f"(r.y) : "r"(addr) : "memory");
     return r;
 }
+__device__ __forceinline__ float lds_float(uint32_t addr) {
+    float r;
+    asm volatile("ld.shared.f32 %0, [%1];" : "=f"(r) : "r"(addr) : "memory");
+    return r;
+}
 __device__ __forceinline__ float paged_log2(float x) {
     float r;
     asm("lg2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+    return r;
+}
+// an 8 x 8 matrix of 16-bit values, as a product leaves its results, transposed
+__device__ __forceinline__ uint32_t matrix_transpose(uint32_t x) {
+    uint32_t r;
+    asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(x));
     return r;
 }
 // Four codes as two fp16 pairs: (0, 1) and (2, 3), or with APART (0, 2) and (1, 3).
@@ -79,27 +139,36 @@ __device__ __forceinline__ void q8_halves(uint32_t w, uint32_t& a, uint32_t& b) 
     }
 }
 
-// SMALL: up to 8 query heads per key head, the product's other 8 rows take the low parts of the weights.
-template <bool BF16, bool E4M3, int DP, bool SMALL>
-__global__ void __launch_bounds__(PA_THREADS, PagedQ8Cfg<DP>::kPerSm) paged_attention_q8_kernel(const PagedQ8Params p) {
-    using C = PagedQ8Cfg<DP>;
-    constexpr int HALVES = SMALL ? 1 : 2;                             // of the 16 rows that hold query heads
+// ROWS: 4, 8 or 16, the query heads of a key head (or of a part of them) at most.
+// BOX: blocks of a multiple of 16 tokens, so that a warp's 16 lie in one: they come as one box by TMA each for keys and values, and have one scale.
+template <bool BF16, bool E4M3, int DP, int ROWS, bool BOX>
+__global__ void __launch_bounds__(PA_THREADS, PagedQ8Cfg<DP, ROWS>::kPerSm)
+paged_attention_q8_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v, const PagedQ8Params p) {
+    using C = PagedQ8Cfg<DP, ROWS>;
+    constexpr int HT = ROWS == 16 ? 2 : 1;                            // products' column tiles of 8 query heads
+    constexpr bool PAIRED = ROWS == 4;                                // columns 4 to 7 are the same heads, for the weights' low parts
     constexpr float LIFT = 15.f;                                      // the exponent of the largest weight of a value (a pair of fp16 then reaches 2^-40 of it)
-    extern __shared__ __align__(128) uint8_t smem[];
+    extern __shared__ __align__(1024) uint8_t lin_smem[];             // (the loads' swizzle goes by the address)
+    uint8_t* smem = lin_smem;
+    __shared__ uint64_t s_full[PA_WARPS][C::kStages];
     __shared__ long long s_sum[PA_WARPS];
     __shared__ int s_start[2];
     __shared__ long long s_skip;
     __shared__ float s_m[PA_WARPS][PA_ROWS], s_l[PA_WARPS][PA_ROWS], s_m2[PA_WARPS][PA_ROWS];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     griddep_launch_dependents();
+    if (BOX && tid == 0) {
+        tma_prefetch_desc(&map_k);
+        tma_prefetch_desc(&map_v);
+    }
 
     // ---- the range: units of all requests, and where this CTA's first one lies -------------------------------------
     const int per = (p.nreq + PA_THREADS - 1) / PA_THREADS, r_lo = min(p.nreq, tid * per), r_hi = min(p.nreq, r_lo + per);
-    const long long heads = static_cast<long long>(p.kv_heads) * p.parts;
+    const long long heads = p.groups;
     long long mine = 0;
     bool bad = false;
     for (int r = r_lo; r < r_hi; ++r) {
-        const PagedSpan s = paged_span(p, r);
+        const PagedSpan s = q8_span(p, r);
         mine += s.tiles;
         bad |= s.bad;
     }
@@ -127,13 +196,17 @@ __global__ void __launch_bounds__(PA_THREADS, PagedQ8Cfg<DP>::kPerSm) paged_atte
         desc[2] = any_bad ? 1 : 0;                                    // MMV_ERR_INVALID_ARG
     }
     if (idle) return;
+    if (BOX && tid < PA_WARPS * C::kStages) {
+        mbar_init(&s_full[tid / C::kStages][tid % C::kStages], 2);
+        mbar_fence_init();
+    }
     if (u0 >= before * heads && u0 < (before + mine) * heads) {       // one thread's requests hold unit u0
         long long at = before * heads;
         int r = r_lo;
-        long long n = paged_span(p, r).tiles * heads;
+        long long n = q8_span(p, r).tiles * heads;
         while (u0 >= at + n) {
             at += n;
-            n = paged_span(p, ++r).tiles * heads;
+            n = q8_span(p, ++r).tiles * heads;
         }
         s_start[0] = r;
         s_skip = u0 - at;
@@ -142,99 +215,132 @@ __global__ void __launch_bounds__(PA_THREADS, PagedQ8Cfg<DP>::kPerSm) paged_atte
 
     PagedIter ld;                                                     // the tile to fetch next
     ld.r = s_start[0];
-    paged_enter(p, ld);
+    q8_enter(p, ld);
     ld.hp = static_cast<int>(s_skip / ld.tiles);
     ld.tile = static_cast<int>(s_skip - static_cast<long long>(ld.hp) * ld.tiles);
     PagedIter it = ld;                                                // the tile to work on next
     const bool cut_front = it.tile > 0;                               // the first (request, head) began in an earlier range
 
     const uint32_t sm = smem_u32(smem);
-    const uint32_t sm_stage = sm + warp * C::kStages * C::kStage;
-    const uint32_t sm_q = sm + C::kAll;
-    float* sm_o = reinterpret_cast<float*>(smem + C::kAll + C::kQSlots * C::kQ);
-    const int words = p.dim / 16;
-    // Where word c of a row lies: eight rows' words of one column lie in different banks, and so do four words of two neighbouring rows.
-    const auto place = [](int row, int c) { return c ^ (((row >> 1) & 3) | (C::kChunks >= 8 ? (row & 1) << 2 : 0)); };
+    const uint32_t sm_stage = sm + warp * C::kStages * C::kStage, sm_scale = sm + C::kAll + warp * C::kStages * C::kScales;
+    float* sm_o = reinterpret_cast<float*>(smem + C::kOOff);
+    if (BOX && (sm & 1023u)) {                                        // (never: the declaration asks for it)
+        if (tid == 0) desc[2] = 1;
+        return;
+    }
 
-    // ---- fetch of a tile: 16 tokens' codes and scales per warp; with a new head the query rows too ------------------------
-    int seg_ld = 0;
-    const auto fetch_q = [&] {
-        const int head = ld.hp / p.parts, part = ld.hp - head * p.parts;
-        const int rows = min(p.rows, p.group - part * p.rows);
-        const uint16_t* src = p.q + ld.r * p.q_req + (head * p.group + part * p.rows) * p.q_head;
-        const uint32_t dst = sm_q + (seg_ld % C::kQSlots) * C::kQ;
-        for (int i = tid; i < PA_ROWS * (DP / 8); i += PA_THREADS) {
-            const int row = i / (DP / 8), c = i - row * (DP / 8);
-            const bool on = row < rows && c < p.dim / 8;
-            cp_async_16_or_zero(dst + row * DP * 2 + c * 16, on ? src + row * p.q_head + c * 8 : p.q, on);
-        }
-        ++seg_ld;
-    };
-    const auto fetch = [&](int stage) {
-        const int head = ld.hp / p.parts;
-        const int tok = ld.first + ld.tile * PA_TILE + warp * PA_TOKENS + (lane & 15);
-        long long at = -1, sc = 0;
-        if (tok >= ld.begin && tok < ld.len) {
-            const unsigned b = static_cast<unsigned>(tok) / static_cast<unsigned>(p.block_size);
-            const int page = p.table[ld.r * p.table_stride + b];
-            if (page >= 0 && page < p.num_blocks) {
-                at = page * p.c_block + static_cast<long long>(tok - b * p.block_size) * p.c_tok + head * p.c_head;
-                sc = page * p.s_block + head * p.s_head;
-            } else {
-                desc[2] = 1;                                          // (every writer stores the same value)
+    // this warp's key head among those side by side, and its tokens' place in a tile
+    const int mine_head = warp & (p.side - 1), mine_tok = warp / p.side * Q8_TOKENS;
+    const int words = p.dim / 16;
+
+    // ---- fetch of a tile: 32 tokens' codes and scales per warp --------------------------------------------------------------------
+    int head_ld = ld.hp / p.parts * p.side + mine_head;               // key head of the tile to fetch
+    // BOX: the block of this lane's group of that tile (even lanes the first, odd ones the second), and the group's place in it; looked up one tile ahead
+    int page_ld = -1, at_ld = 0;
+    const auto look_up = [&] {
+        const int tok = ld.first + ld.tile * p.tile + mine_tok + (lane & 1) * 16;
+        page_ld = -1;
+        if (tok < ld.len) {
+            uint32_t b = __umulhi(static_cast<uint32_t>(tok), p.by_block);           // (at most one too small)
+            at_ld = tok - static_cast<int>(b) * p.block_size;
+            if (at_ld >= p.block_size) {
+                ++b;
+                at_ld -= p.block_size;
             }
+            page_ld = p.table[ld.r * p.table_stride + b];
         }
-        const uint32_t dst = sm_stage + stage * C::kStage;
-        constexpr int kPerRow = C::kChunks;                           // lanes on one row
-        constexpr int kRows = 32 / kPerRow;
+    };
+    if (BOX) look_up();
+    const auto fetch = [&](int stage) {
+        const uint32_t scales = sm_scale + stage * C::kScales;
+        if constexpr (BOX) {
+            if (lane < 4) {                                           // scales: the keys' of the first group, the second, the values'
+                const bool there = ld.first + ld.tile * p.tile + mine_tok + (lane & 1) * 16 < ld.len, on = there && page_ld >= 0 && page_ld < p.num_blocks;
+                if (there && !on) desc[2] = 1;                        // (every writer stores the same value)
+                cp_async_4_or_zero(scales + lane * 4, on ? static_cast<const void*>((lane & 2 ? p.vs : p.ks) + page_ld * p.s_block + head_ld * p.s_head) : p.q, on);
+                if (lane < 2) {
+                    uint64_t* bar = &s_full[warp][stage];
+                    if (on) {
+                        mbar_arrive_expect_tx(bar, 2 * C::kGroup);
+                        uint8_t* dst = smem + (warp * C::kStages + stage) * C::kStage + lane * C::kGroup;
 #pragma unroll
-        for (int i = 0; i < PA_TOKENS / kRows; ++i) {
-            const int row = i * kRows + lane / kPerRow, c = lane % kPerRow;
-            const long long a = __shfl_sync(0xffffffffu, at, row);
-            const bool on = a >= 0 && c < words;
-            const uint32_t d = dst + row * C::kRow + (place(row, c) << 4);
-            cp_async_16_or_zero(d, on ? static_cast<const void*>(p.k8 + a + c * 16) : p.q, on);
-            cp_async_16_or_zero(d + PA_TOKENS * C::kRow, on ? static_cast<const void*>(p.v8 + a + c * 16) : p.q, on);
+                        for (int x = 0; x < DP / C::kBox; ++x) {
+                            tma_load_4d(dst + x * 2048, &map_k, bar, x * 128, head_ld, at_ld, page_ld);
+                            tma_load_4d(dst + C::kKeys + x * 2048, &map_v, bar, x * 128, head_ld, at_ld, page_ld);
+                        }
+                    } else {
+                        mbar_arrive(bar);
+                    }
+                }
+            }
+        } else {
+            const int tok = ld.first + ld.tile * p.tile + mine_tok + lane;
+            long long at = -1, sc = 0;
+            if (tok >= ld.begin && tok < ld.len) {
+                const unsigned b = static_cast<unsigned>(tok) / static_cast<unsigned>(p.block_size);
+                const int page = p.table[ld.r * p.table_stride + b];
+                if (page >= 0 && page < p.num_blocks) {
+                    at = page * p.c_block + static_cast<long long>(tok - b * p.block_size) * p.c_tok + head_ld * p.c_head;
+                    sc = page * p.s_block + head_ld * p.s_head;
+                } else {
+                    desc[2] = 1;                                      // (every writer stores the same value)
+                }
+            }
+            const uint32_t dst = sm_stage + stage * C::kStage;
+            constexpr int kRows = 32 / C::kChunks;                    // rows side by side
+#pragma unroll
+            for (int i = 0; i < Q8_TOKENS / kRows; ++i) {
+                const int row = i * kRows + lane / C::kChunks, c = lane % C::kChunks;
+                const long long a = __shfl_sync(0xffffffffu, at, row);
+                const bool on = a >= 0 && c < words;
+                const uint32_t d = dst + (row >> 4) * C::kGroup + C::place(row & 15, c);
+                cp_async_16_or_zero(d, on ? static_cast<const void*>(p.k8 + a + c * 16) : p.q, on);
+                cp_async_16_or_zero(d + C::kKeys, on ? static_cast<const void*>(p.v8 + a + c * 16) : p.q, on);
+            }
+            // scales, the keys' and the values' (zero for what is not a token)
+            cp_async_4_or_zero(scales + lane * 4, at >= 0 ? static_cast<const void*>(p.ks + sc) : p.q, at >= 0);
+            cp_async_4_or_zero(scales + (Q8_TOKENS + lane) * 4, at >= 0 ? static_cast<const void*>(p.vs + sc) : p.q, at >= 0);
         }
-        // scales: lanes 0 to 15 the keys', 16 to 31 the values' (zero for what is not a token)
-        cp_async_4_or_zero(dst + C::kCodes + lane * 4, at >= 0 ? static_cast<const void*>((lane < 16 ? p.ks : p.vs) + sc) : p.q, at >= 0);
     };
     long long u_ld = u0;
-    bool fresh = true;                                                // the next tile to fetch begins a head
 
-    // The query as the product's first operand: of columns 64 g + 16 c + 4 s to + 3 (c = lane modulo 4) in product 4 g + s; rows lane / 4 and, if
-    // not SMALL, lane / 4 + 8 (which are zero otherwise).
-    uint32_t qf[DP / 16][2 * HALVES];
-    float qs[HALVES];                                                 // scale * log2(e), times what the row was divided by
-    float o[DP / 8][4];
-    float m[HALVES], l[HALVES], m2[HALVES];                           // maximum; sum of 2^(s - m); maximum of the values' weights less LIFT
+    // Where this lane reads: word 4 g + c of its key's row is at (k_lane ^ 64 g) + 16 rows of 8, word 2 d + (lane / 16) of its value's at v_lane ^ 32 d (a row's
+    // words lie within its 128 bytes, or 64).
+    const uint32_t k_lane = sm_stage + C::place(C::token(lane >> 2), lane & 3), v_lane = sm_stage + C::kKeys + C::place(C::token(lane & 15), lane >> 4);
+    const auto word = [](uint32_t base, int c) { return (base ^ ((c & 7) << 4)) + (c >> 3) * 2048; };
+    // The query as the product's second operand: of columns 64 g + 16 c + 4 s to + 3 (c = lane modulo 4) in product 4 g + s; head lane / 4 of each tile.
+    uint32_t qf[HT][DP / 16][2];
+    // of heads 2 c and 2 c + 1 of each tile:
+    float qs[HT][2];                                                  // scale * log2(e), times what the head's row was divided by
+    float m[HT][2], l[HT][2], m2[HT][2];                              // maximum; sum of 2^(s - m); maximum of the values' weights less LIFT
+    float o[HT][DP / 16][4];                                          // columns 16 d + 2 g (0, 1) and 16 d + 2 g + 1 (2, 3) of heads 2 c, 2 c + 1, g = lane / 4
     int seg = 0, stage = 0;
-    bool begins = true;
+    bool begins = true, late = false;
+    uint32_t turn = 0;                                                // of the stages' barriers
 #pragma unroll 1
     for (long long u = u0 - C::kStages; u < u1; ++u) {
-        cp_async_wait<C::kStages - 1>();
-        __syncwarp();
         if (begins && u >= u0) {
-            __syncthreads();                                          // every warp's share of the query rows has landed
-            const uint32_t src = sm_q + (seg % C::kQSlots) * C::kQ + (lane & 3) * 32;
+            const int part = it.hp % p.parts, head = it.hp / p.parts * p.side + mine_head, rows = min(p.rows, p.group - part * p.rows);
 #pragma unroll
-            for (int h = 0; h < HALVES; ++h) {
-                const uint32_t row = src + ((lane >> 2) + 8 * h) * DP * 2;
+            for (int h = 0; h < HT; ++h) {
+                const int row = PAIRED ? (lane >> 2) & 3 : (lane >> 2) + 8 * h;
+                const uint16_t* src = p.q + it.r * p.q_req + (static_cast<long long>(head) * p.group + part * p.rows + row) * p.q_head + (lane & 3) * 16;
                 uint32_t most = 0u;
 #pragma unroll
                 for (int g = 0; g < DP / 64; ++g) {
 #pragma unroll
                     for (int half = 0; half < 2; ++half) {
-                        const uint4 w = lds_128(row + g * 128 + half * 16);
+                        uint4 w = make_uint4(0u, 0u, 0u, 0u);
+                        if (row < rows && 64 * g + (lane & 3) * 16 + half * 8 < p.dim) w = *reinterpret_cast<const uint4*>(src + 64 * g + half * 8);
                         const uint32_t in[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
                         for (int e = 0; e < 4; ++e) {
-                            qf[4 * g + 2 * half + (e >> 1)][(e & 1) * HALVES + h] = in[e];
+                            qf[h][4 * g + 2 * half + (e >> 1)][e & 1] = in[e];
                             most = __vmaxu2(most, in[e] & 0x7fff7fffu);
                         }
                     }
                 }
-                qs[h] = p.scale_log2;
+                float divided = 1.f;
                 if constexpr (BF16) {
                     most = max(most & 0xffffu, most >> 16);
                     most = max(most, __shfl_xor_sync(0xffffffffu, most, 1));
@@ -242,132 +348,180 @@ __global__ void __launch_bounds__(PA_THREADS, PagedQ8Cfg<DP>::kPerSm) paged_atte
                     // largest magnitude in [2^e, 2^(e + 1)): times 2^(14 - e)
                     const int e = static_cast<int>(most >> 7) - 127, up = most >= 0x7f80u ? 0 : max(-126, min(126, 14 - e));
                     const float f = __int_as_float((up + 127) << 23);
-                    qs[h] *= __int_as_float((127 - up) << 23);
+                    divided = __int_as_float((127 - up) << 23);
 #pragma unroll
                     for (int d = 0; d < DP / 16; ++d)
 #pragma unroll
                         for (int i = 0; i < 2; ++i) {
-                            const float2 x = unpack_pair<true>(qf[d][i * HALVES + h]);
-                            qf[d][i * HALVES + h] = pack_pair<false>(x.x * f, x.y * f);
+                            const float2 x = unpack_pair<true>(qf[h][d][i]);
+                            qf[h][d][i] = pack_pair<false>(x.x * f, x.y * f);
                         }
                 }
-                m[h] = m2[h] = -INFINITY;
-                l[h] = 0.f;
-            }
 #pragma unroll
-            for (int n = 0; n < DP / 8; ++n) o[n][0] = o[n][1] = o[n][2] = o[n][3] = 0.f;
+                for (int i = 0; i < 2; ++i) {
+                    qs[h][i] = p.scale_log2 * __shfl_sync(0xffffffffu, divided, (2 * (lane & 3) + i) * 4);
+                    m[h][i] = m2[h][i] = -INFINITY;
+                    l[h][i] = 0.f;
+                }
+#pragma unroll
+                for (int d = 0; d < DP / 16; ++d) o[h][d][0] = o[h][d][1] = o[h][d][2] = o[h][d][3] = 0.f;
+            }
             ++seg;
         }
-        const int tok0 = it.first + it.tile * PA_TILE + warp * PA_TOKENS;
+        cp_async_wait<C::kStages - 1>();
+        if (BOX && u >= u0) {
+            if (!mbar_try_wait_for(&s_full[warp][stage], turn, 20000u)) late |= !q8_wait(&s_full[warp][stage], turn, p.budget_ns);
+            if (stage + 1 == C::kStages) turn ^= 1;
+        }
+        __syncwarp();
+        const int tok0 = it.first + it.tile * p.tile + mine_tok;
         if (u >= u0 && tok0 < it.len) {
-            const uint32_t kb = sm_stage + stage * C::kStage, vb = kb + PA_TOKENS * C::kRow, sb = kb + C::kCodes;
-            float s[2][4] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+            const uint32_t sb = sm_scale + stage * C::kScales;
+            const bool edge = tok0 < it.begin || tok0 + Q8_TOKENS > it.len;
+            if (BOX && E4M3 && edge) {                                // codes of no token of this request: a weight of zero does not hide a NaN
+                for (int i = lane; i < Q8_TOKENS * C::kChunks; i += 32) {
+                    const int row = i / C::kChunks;
+                    if (tok0 + row < it.begin || tok0 + row >= it.len)
+                        *reinterpret_cast<uint4*>(smem + (warp * C::kStages + stage) * C::kStage + C::kKeys + (row >> 4) * C::kGroup + C::place(row & 15, i % C::kChunks)) =
+                            make_uint4(0u, 0u, 0u, 0u);
+                }
+                fence_proxy_async_smem();
+                __syncwarp();
+            }
+            // scores of tokens g (0, 1) and g + 8 (2, 3) of each group of 16 for heads 2 c, 2 c + 1
+            float s[HT][2][4], lift[2][2];                            // lift: log2 of the values' scale, of the two tokens
 #pragma unroll
-            for (int g = 0; g < DP / 64; ++g)
+            for (int y = 0; y < 2; ++y) {
 #pragma unroll
-                for (int n = 0; n < 2; ++n) {                         // tokens lane / 4 and lane / 4 + 8
-                    const int row = (lane >> 2) + 8 * n;
-                    const uint4 w = lds_128(kb + row * C::kRow + (place(row, 4 * g + (lane & 3)) << 4));
-                    const uint32_t in[4] = {w.x, w.y, w.z, w.w};
+                for (int h = 0; h < HT; ++h) s[h][y][0] = s[h][y][1] = s[h][y][2] = s[h][y][3] = 0.f;
+#pragma unroll
+                for (int g = 0; g < DP / 64; ++g) {
+                    const uint32_t at = word(k_lane + stage * C::kStage + y * C::kGroup, 4 * g);
+                    const uint4 v0 = lds_128(at), v1 = lds_128(at + 8 * C::kBox);
+                    const uint32_t lo8[4] = {v0.x, v0.y, v0.z, v0.w}, hi8[4] = {v1.x, v1.y, v1.z, v1.w};
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
-                        uint32_t b0, b1;
-                        q8_halves<E4M3, false>(in[e], b0, b1);
-                        const uint32_t(&q)[2 * HALVES] = qf[4 * g + e];
-                        const uint32_t a[4] = {q[0], SMALL ? 0u : q[1], q[HALVES], SMALL ? 0u : q[2 * HALVES - 1]};
-                        mma_16816<false>(s[n], a, b0, b1);
+                        uint32_t a[4];
+                        q8_halves<E4M3, false>(lo8[e], a[0], a[2]);
+                        q8_halves<E4M3, false>(hi8[e], a[1], a[3]);
+#pragma unroll
+                        for (int h = 0; h < HT; ++h) mma_16816<false>(s[h][y], a, qf[h][4 * g + e][0], qf[h][4 * g + e][1]);
                     }
                 }
-            const bool edge = tok0 < it.begin || tok0 + PA_TOKENS > it.len;
-            float lift[2][2];                                         // log2 of the value scales of this lane's tokens
+                float ks[2];
+                if constexpr (BOX) {
+                    ks[0] = ks[1] = lds_float(sb + y * 4);
+                    lift[y][0] = lift[y][1] = paged_log2(lds_float(sb + 8 + y * 4));
+                } else {
 #pragma unroll
-            for (int n = 0; n < 2; ++n) {
-                const float2 ks = lds_float2(sb + (n * 8 + (lane & 3) * 2) * 4), vs = lds_float2(sb + (PA_TOKENS + n * 8 + (lane & 3) * 2) * 4);
-                lift[n][0] = paged_log2(vs.x);
-                lift[n][1] = paged_log2(vs.y);
+                    for (int i = 0; i < 2; ++i) {
+                        const uint32_t at = sb + (y * 16 + C::token((lane >> 2) + 8 * i)) * 4;
+                        ks[i] = lds_float(at);
+                        lift[y][i] = paged_log2(lds_float(at + Q8_TOKENS * 4));
+                    }
+                }
 #pragma unroll
-                for (int i = 0; i < 2 * HALVES; ++i) {
-                    s[n][i] *= qs[i >> 1] * ((i & 1) ? ks.y : ks.x);
-                    if (edge) {
-                        const int tok = tok0 + n * 8 + (lane & 3) * 2 + (i & 1);
+                for (int h = 0; h < HT; ++h)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) s[h][y][i] *= qs[h][i & 1] * ks[i >> 1];
+            }
+            if (edge)
+#pragma unroll
+                for (int y = 0; y < 2; ++y)
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        const int tok = tok0 + y * 16 + C::token((lane >> 2) + 8 * i);
                         if (tok < it.begin || tok >= it.len) {
-                            s[n][i] = -INFINITY;
-                            lift[n][i & 1] = 0.f;
+                            lift[y][i] = 0.f;
+#pragma unroll
+                            for (int h = 0; h < HT; ++h) s[h][y][2 * i] = s[h][y][2 * i + 1] = -INFINITY;
                         }
                     }
-                }
-            }
-            uint32_t hi[4], lo[4];                                    // (SMALL: the low parts are hi[1] and hi[3], rows 8 to 15)
+            uint32_t hi[HT][2][2], lo[HT][2][2];                      // the weights as a product's second operand: tokens 0 to 7, 8 to 15 of each group
 #pragma unroll
-            for (int h = 0; h < HALVES; ++h) {                        // rows lane / 4 and lane / 4 + 8
-                float t[2][2];
+            for (int h = 0; h < HT; ++h) {
+                float w[2][4], fall[2];
 #pragma unroll
-                for (int n = 0; n < 2; ++n)
+                for (int i = 0; i < 2; ++i) {                         // heads 2 c, 2 c + 1
+                    float t[2][2], top = -INFINITY, top2 = -INFINITY;
 #pragma unroll
-                    for (int i = 0; i < 2; ++i) t[n][i] = s[n][2 * h + i] + lift[n][i];
-                float top = fmaxf(fmaxf(s[0][2 * h], s[0][2 * h + 1]), fmaxf(s[1][2 * h], s[1][2 * h + 1]));
-                float top2 = fmaxf(fmaxf(t[0][0], t[0][1]), fmaxf(t[1][0], t[1][1]));
+                    for (int y = 0; y < 2; ++y)
 #pragma unroll
-                for (int x = 1; x <= 2; x <<= 1) {
-                    top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, x));
-                    top2 = fmaxf(top2, __shfl_xor_sync(0xffffffffu, top2, x));
-                }
-                const float now = fmaxf(m[h], top), now2 = fmaxf(m2[h], top2 - LIFT);
-                const float base = now == -INFINITY ? 0.f : now;      // (no token yet: every weight is 2^-inf = 0)
-                const float base2 = now2 == -INFINITY ? 0.f : now2;
-                const float fall = paged_exp2(m2[h] - base2);
-                l[h] *= paged_exp2(m[h] - base);
-                m[h] = now;
-                m2[h] = now2;
-#pragma unroll
-                for (int n = 0; n < 2; ++n) {
-                    l[h] += paged_exp2(s[n][2 * h] - base) + paged_exp2(s[n][2 * h + 1] - base);
-                    const float a = paged_exp2(t[n][0] - base2), b = paged_exp2(t[n][1] - base2);
-                    // The weights enter the product as the sum of two fp16 values (2^-22 of themselves, at least 2^-40 of the largest): rounded to
-                    // one, their error would be as large as the result's own rounding.
-                    hi[n * 2 + h] = pack_pair<false>(a, b);
-                    const float2 back = unpack_pair<false>(hi[n * 2 + h]);
-                    (SMALL ? hi[n * 2 + 1] : lo[n * 2 + h]) = pack_pair<false>(a - back.x, b - back.y);
-                }
-                if (__any_sync(0xffffffffu, fall != 1.f)) {           // (the maximum of a long context soon stands)
-#pragma unroll
-                    for (int n = 0; n < DP / 8; ++n) {
-                        o[n][2 * h] *= fall;
-                        o[n][2 * h + 1] *= fall;
-                        if (SMALL) {
-                            o[n][2] *= fall;
-                            o[n][3] *= fall;
+                        for (int j = 0; j < 2; ++j) {
+                            t[y][j] = s[h][y][2 * j + i] + lift[y][j];
+                            top = fmaxf(top, s[h][y][2 * j + i]);
+                            top2 = fmaxf(top2, t[y][j]);
                         }
+#pragma unroll
+                    for (int x = 4; x < 32; x <<= 1) {
+                        top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, x));
+                        top2 = fmaxf(top2, __shfl_xor_sync(0xffffffffu, top2, x));
                     }
+                    const float now = fmaxf(m[h][i], top), now2 = fmaxf(m2[h][i], top2 - LIFT);
+                    const float base = now == -INFINITY ? 0.f : now;  // (no token yet: every weight is 2^-inf = 0)
+                    const float base2 = now2 == -INFINITY ? 0.f : now2;
+                    fall[i] = paged_exp2(m2[h][i] - base2);
+                    l[h][i] *= paged_exp2(m[h][i] - base);
+                    m[h][i] = now;
+                    m2[h][i] = now2;
+#pragma unroll
+                    for (int y = 0; y < 2; ++y)
+#pragma unroll
+                        for (int j = 0; j < 2; ++j) {
+                            l[h][i] += paged_exp2(s[h][y][2 * j + i] - base);
+                            w[y][2 * j + i] = paged_exp2(t[y][j] - base2);
+                        }
+                }
+#pragma unroll
+                for (int y = 0; y < 2; ++y)
+#pragma unroll
+                    for (int j = 0; j < 2; ++j) {
+                        // The weights enter the product as the sum of two fp16 values (2^-22 of themselves, at least 2^-40 of the largest): rounded to
+                        // one, their error would be as large as the result's own rounding.
+                        uint32_t x = pack_pair<false>(w[y][2 * j], w[y][2 * j + 1]);
+                        const float2 back = unpack_pair<false>(x);
+                        const uint32_t rest = pack_pair<false>(w[y][2 * j] - back.x, w[y][2 * j + 1] - back.y);
+                        if (PAIRED) {
+                            if (lane & 2) x = rest;                   // (columns 4 to 7)
+                        } else {
+                            lo[h][y][j] = matrix_transpose(rest);
+                        }
+                        hi[h][y][j] = matrix_transpose(x);
+                    }
+                if (__any_sync(0xffffffffu, fall[0] != 1.f || fall[1] != 1.f)) {      // (the maximum of a long context soon stands)
+#pragma unroll
+                    for (int d = 0; d < DP / 16; ++d)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) o[h][d][i] *= fall[i & 1];
                 }
             }
-            {
-                // lanes 0-7: tokens 0-7, 16 columns; 8-15: tokens 8-15 of them; 16-31: the next 16 columns
-                const int row = lane & 15;
+            // lanes 0-7: tokens 0-7, 16 columns; 8-15: tokens 8-15 of them; 16-31: the next 16 columns
+#pragma unroll
+            for (int y = 0; y < 2; ++y)
 #pragma unroll
                 for (int d = 0; d < DP / 32; ++d) {
                     uint32_t w[4];
-                    ldsm_x4_t(w, vb + row * C::kRow + (place(row, 2 * d + (lane >> 4)) << 4));
+                    ldsm_x4_t(w, word(v_lane + stage * C::kStage + y * C::kGroup, 2 * d));
 #pragma unroll
-                    for (int x = 0; x < 2; ++x) {                     // 16 columns: the even ones' result in o[4 d + 2 x], the odd ones' in the next
-                        uint32_t even0, odd0, even1, odd1;
-                        q8_halves<E4M3, true>(w[2 * x], even0, odd0);
-                        q8_halves<E4M3, true>(w[2 * x + 1], even1, odd1);
-                        mma_16816<false>(o[4 * d + 2 * x], hi, even0, even1);
-                        mma_16816<false>(o[4 * d + 2 * x + 1], hi, odd0, odd1);
-                        if (!SMALL) {
-                            mma_16816<false>(o[4 * d + 2 * x], lo, even0, even1);
-                            mma_16816<false>(o[4 * d + 2 * x + 1], lo, odd0, odd1);
+                    for (int x = 0; x < 2; ++x) {
+                        uint32_t a[4];
+                        q8_halves<E4M3, true>(w[2 * x], a[0], a[1]);
+                        q8_halves<E4M3, true>(w[2 * x + 1], a[2], a[3]);
+#pragma unroll
+                        for (int h = 0; h < HT; ++h) {
+                            mma_16816<false>(o[h][2 * d + x], a, hi[h][y][0], hi[h][y][1]);
+                            if (!PAIRED) mma_16816<false>(o[h][2 * d + x], a, lo[h][y][0], lo[h][y][1]);
                         }
                     }
                 }
-            }
         }
         __syncwarp();                                                 // the stage has been read by all lanes
         if (u_ld < u1) {
-            if (fresh) fetch_q();
             fetch(stage);
-            if (++u_ld < u1) fresh = paged_next(p, ld);
+            if (++u_ld < u1) {
+                if (q8_next(p, ld)) head_ld = ld.hp / p.parts * p.side + mine_head;
+                if (BOX) look_up();
+            }
         }
         cp_async_commit();
         stage = stage + 1 == C::kStages ? 0 : stage + 1;
@@ -377,105 +531,109 @@ __global__ void __launch_bounds__(PA_THREADS, PagedQ8Cfg<DP>::kPerSm) paged_atte
         const bool ends = it.tile + 1 == it.tiles;                    // of this (request, head part)
         begins = ends;
         const bool last = u + 1 == u1;
-        if (!last) paged_next(p, it);
+        if (!last) q8_next(p, it);
         if (!ends && !last) continue;
 
-        // ---- the warps meet --------------------------------------------------------------------------------------------
-        const int head = done.hp / p.parts, part = done.hp - head * p.parts;
+        // ---- the warps of a head meet ------------------------------------------------------------------------------------
+        const int part = done.hp % p.parts, head0 = done.hp / p.parts * p.side;
         const int rows = min(p.rows, p.group - part * p.rows);
-        if (SMALL)
+        if (PAIRED)
 #pragma unroll
-            for (int n = 0; n < DP / 8; ++n) {
-                o[n][0] += o[n][2];
-                o[n][1] += o[n][3];
+            for (int d = 0; d < DP / 16; ++d)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) o[0][d][i] += __shfl_xor_sync(0xffffffffu, o[0][d][i], 2);
+#pragma unroll
+        for (int h = 0; h < HT; ++h)
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+#pragma unroll
+                for (int x = 4; x < 32; x <<= 1) l[h][i] += __shfl_xor_sync(0xffffffffu, l[h][i], x);
+                if (lane < 4) {
+                    const int row = 8 * h + 2 * lane + i;
+                    s_m[warp][row] = m[h][i];
+                    s_l[warp][row] = l[h][i];
+                    s_m2[warp][row] = m2[h][i];
+                }
             }
-#pragma unroll
-        for (int h = 0; h < HALVES; ++h) {
-            l[h] += __shfl_xor_sync(0xffffffffu, l[h], 1);
-            l[h] += __shfl_xor_sync(0xffffffffu, l[h], 2);
-            const int row = (lane >> 2) + 8 * h;
-            if ((lane & 3) == 0) {
-                s_m[warp][row] = m[h];
-                s_l[warp][row] = l[h];
-                s_m2[warp][row] = m2[h];
-            }
-        }
-        __syncthreads();
-#pragma unroll
-        for (int h = 0; h < HALVES; ++h) {
-            const int row = (lane >> 2) + 8 * h;
-            float top = s_m2[0][row];
-#pragma unroll
-            for (int w = 1; w < PA_WARPS; ++w) top = fmaxf(top, s_m2[w][row]);
-            // (a warp without tokens has maximum -infinity, sum 0 and result 0, and contributes 2^-inf = 0 times that; a NaN stays one)
-            const float f = paged_exp2(m2[h] - (top == -INFINITY ? 0.f : top));
-            if (row < rows) {
-#pragma unroll
-                for (int n = 0; n < DP / 8; n += 2)                   // 16 columns: this lane's four
-                    *reinterpret_cast<float4*>(sm_o + (warp * p.rows + row) * C::kPitch + n * 8 + (lane & 3) * 4) =
-                        make_float4(o[n][2 * h] * f, o[n + 1][2 * h] * f, o[n][2 * h + 1] * f, o[n + 1][2 * h + 1] * f);
-            }
-        }
         __syncthreads();
         const bool began_here = !(cut_front && seg == 1);
         const bool whole = began_here && ends;
         const long long slot = 2ll * blockIdx.x + (began_here ? 1 : 0);
-        for (int i = tid; i < rows * (DP / 4); i += PA_THREADS) {
-            const int row = i / (DP / 4), c = (i - row * (DP / 4)) * 4;
-            float t = s_m[0][row], t2 = s_m2[0][row];
+        for (int half = 0; half < 2; ++half) {                        // half of the columns at a time
 #pragma unroll
-            for (int w = 1; w < PA_WARPS; ++w) {
-                t = fmaxf(t, s_m[w][row]);
-                t2 = fmaxf(t2, s_m2[w][row]);
-            }
-            float sum = 0.f;
-            float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+            for (int h = 0; h < HT; ++h)
 #pragma unroll
-            for (int w = 0; w < PA_WARPS; ++w) {
-                sum += s_l[w][row] * paged_exp2(s_m[w][row] - (t == -INFINITY ? 0.f : t));
-                const float4 y = *reinterpret_cast<const float4*>(sm_o + (w * p.rows + row) * C::kPitch + c);
-                x.x += y.x;
-                x.y += y.y;
-                x.z += y.z;
-                x.w += y.w;
-            }
-            const long long orow = done.r * static_cast<long long>(p.heads) + head * p.group + part * p.rows + row;
-            if (whole) {
-                // (every weight 0: the result is 0)
-                const float inv = sum == 0.f ? 0.f : exp2f((t2 == -INFINITY ? 0.f : t2) - (t == -INFINITY ? 0.f : t)) / sum;
-                if (c < p.dim)
-                    *reinterpret_cast<uint2*>(p.out + orow * p.dim + c) =
-                        make_uint2(pack_pair<BF16>(x.x * inv, x.y * inv), pack_pair<BF16>(x.z * inv, x.w * inv));
-                if (c == 0 && p.lse) p.lse[orow] = sum == 0.f ? -INFINITY : (t + log2f(sum)) * 0.69314718055994531f;
-            } else {
-                if (c < p.dim) *reinterpret_cast<float4*>(p.part_o + (slot * p.rows + row) * p.dim + c) = x;
-                if (c == 0) {
-                    p.part_ml[(slot * 2) * PA_ROWS + row] = t;
-                    p.part_ml[(slot * 2 + 1) * PA_ROWS + row] = sum;
-                    p.part_m2[slot * PA_ROWS + row] = t2;
+                for (int i = 0; i < 2; ++i) {
+                    const int row = 8 * h + 2 * (lane & 3) + i;
+                    float top = s_m2[mine_head][row];
+                    for (int w = mine_head + p.side; w < PA_WARPS; w += p.side) top = fmaxf(top, s_m2[w][row]);
+                    // (a warp without tokens has maximum -infinity, sum 0 and result 0, and contributes 2^-inf = 0 times that; a NaN stays one)
+                    const float f = paged_exp2(m2[h][i] - (top == -INFINITY ? 0.f : top));
+                    if (row < rows) {
+#pragma unroll
+                        for (int d = 0; d < DP / 16; ++d)             // columns 16 d + 2 g, + 1
+                            if (d / (DP / 32) == half)
+                                *reinterpret_cast<float2*>(sm_o + (warp * p.rows + row) * C::kPitch + d % (DP / 32) * 16 + (lane >> 2) * 2) =
+                                    make_float2(o[h][d][i] * f, o[h][d][2 + i] * f);
+                    }
+                }
+            __syncthreads();
+            for (int i = tid; i < p.side * rows * (DP / 8); i += PA_THREADS) {
+                const int line = i / (DP / 8), at = (i - line * (DP / 8)) * 4, c = half * (DP / 2) + at, hh = line / rows, row = line - hh * rows;
+                float t = s_m[hh][row], t2 = s_m2[hh][row];
+                for (int w = hh + p.side; w < PA_WARPS; w += p.side) {
+                    t = fmaxf(t, s_m[w][row]);
+                    t2 = fmaxf(t2, s_m2[w][row]);
+                }
+                float sum = 0.f;
+                float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+                for (int w = hh; w < PA_WARPS; w += p.side) {
+                    sum += s_l[w][row] * paged_exp2(s_m[w][row] - (t == -INFINITY ? 0.f : t));
+                    const float4 y = *reinterpret_cast<const float4*>(sm_o + (w * p.rows + row) * C::kPitch + at);
+                    x.x += y.x;
+                    x.y += y.y;
+                    x.z += y.z;
+                    x.w += y.w;
+                }
+                const long long orow = done.r * static_cast<long long>(p.heads) + static_cast<long long>(head0 + hh) * p.group + part * p.rows + row;
+                if (whole) {
+                    // (every weight 0: the result is 0)
+                    const float inv = sum == 0.f ? 0.f : exp2f((t2 == -INFINITY ? 0.f : t2) - (t == -INFINITY ? 0.f : t)) / sum;
+                    if (c < p.dim)
+                        *reinterpret_cast<uint2*>(p.out + orow * p.dim + c) =
+                            make_uint2(pack_pair<BF16>(x.x * inv, x.y * inv), pack_pair<BF16>(x.z * inv, x.w * inv));
+                    if (c == 0 && p.lse) p.lse[orow] = sum == 0.f ? -INFINITY : (t + log2f(sum)) * 0.69314718055994531f;
+                } else {
+                    const long long to = slot * p.side + hh;
+                    if (c < p.dim) *reinterpret_cast<float4*>(p.part_o + (to * p.rows + row) * p.dim + c) = x;
+                    if (c == 0) {
+                        p.part_ml[(to * 2) * PA_ROWS + row] = t;
+                        p.part_ml[(to * 2 + 1) * PA_ROWS + row] = sum;
+                        p.part_m2[to * PA_ROWS + row] = t2;
+                    }
                 }
             }
+            __syncthreads();
         }
         if (!whole && began_here && tid == 0) {                       // this range joins it; its last unit lies in a later one
             desc[0] = static_cast<int32_t>(done.r);
             desc[1] = static_cast<int32_t>(paged_cta_of(u + (done.tiles - 1 - done.tile), units, ctas));
             desc[3] = done.hp;
         }
-        __syncthreads();
     }
+    if (BOX && late) desc[2] = 5;                                     // MMV_ERR_TIMEOUT
 }
 
-// Joins the partials of the (request, head part) that begins in range blockIdx.x and is cut at its end: one row (query
-// head) per CTA.  Also the requests without tokens and the status word.
+// Joins the partials of the (request, heads) that begins in range blockIdx.x and is cut at its end: one query head per CTA.  Also the requests without tokens and the status word.
 template <bool BF16>
 __global__ void __launch_bounds__(PA_JOIN_THREADS) paged_join_q8_kernel(const PagedQ8Params p, int ctas) {
     __shared__ float s_w[PA_JOIN_THREADS], s_red[4], s_red2[4];
     __shared__ float4 s_x[PA_JOIN_THREADS];
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, row = blockIdx.y;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, hh = blockIdx.y / p.rows, row = blockIdx.y - hh * p.rows;
     griddep_wait();
-    if (row == 0) {
+    if (blockIdx.y == 0) {
         for (int r = blockIdx.x; r < p.nreq; r += gridDim.x) {        // nothing to attend to: 0, and the logarithm of an empty sum
-            if (paged_span(p, r).tiles) continue;
+            if (q8_span(p, r).tiles) continue;
             for (long long i = tid; i < static_cast<long long>(p.heads) * p.dim; i += PA_JOIN_THREADS) p.out[r * static_cast<long long>(p.heads) * p.dim + i] = 0;
             if (p.lse)
                 for (int i = tid; i < p.heads; i += PA_JOIN_THREADS) p.lse[r * static_cast<long long>(p.heads) + i] = -INFINITY;
@@ -483,20 +641,20 @@ __global__ void __launch_bounds__(PA_JOIN_THREADS) paged_join_q8_kernel(const Pa
         if (blockIdx.x == 0) {
             int e = 0;
             for (int i = tid; i < ctas; i += PA_JOIN_THREADS) e |= p.desc[4 * i + 2];
-            e = __syncthreads_or(e);
+            const bool late = __syncthreads_or(e & 4), bad = __syncthreads_or(e & 1);
             if (tid == 0) {
                 p.hdr->tile_counter = 0u;
-                p.hdr->error = e ? 1u : 0u;
+                p.hdr->error = late ? 5u : bad ? 1u : 0u;             // MMV_ERR_TIMEOUT, MMV_ERR_INVALID_ARG
             }
         }
     }
     const int32_t* desc = p.desc + 4 * blockIdx.x;
     const int r = desc[0];
     if (r < 0) return;
-    const int last = desc[1], hp = desc[3], head = hp / p.parts, part = hp - head * p.parts;
+    const int last = desc[1], hp = desc[3], head = hp / p.parts * p.side + hh, part = hp % p.parts;
     if (row >= min(p.rows, p.group - part * p.rows)) return;
     const int first = blockIdx.x, n = last - first + 1;
-    const auto place = [&](int i) { return 2ll * (first + i) + (i == 0 ? 1 : 0); };
+    const auto place = [&](int i) { return (2ll * (first + i) + (i == 0 ? 1 : 0)) * p.side + hh; };
     // the maxima, then the weights' sum
     float top = -INFINITY, top2 = -INFINITY;
     for (int i = tid; i < n; i += PA_JOIN_THREADS) {
@@ -555,7 +713,7 @@ __global__ void __launch_bounds__(PA_JOIN_THREADS) paged_join_q8_kernel(const Pa
             x.z += y.z;
             x.w += y.w;
         }
-        const long long orow = r * static_cast<long long>(p.heads) + head * p.group + part * p.rows + row;
+        const long long orow = r * static_cast<long long>(p.heads) + static_cast<long long>(head) * p.group + part * p.rows + row;
         const float inv = sum == 0.f ? 0.f : exp2f(base2 - base) / sum;
         *reinterpret_cast<uint2*>(p.out + orow * p.dim + c * 4) =
             make_uint2(pack_pair<BF16>(x.x * inv, x.y * inv), pack_pair<BF16>(x.z * inv, x.w * inv));

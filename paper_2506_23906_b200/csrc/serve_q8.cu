@@ -1,5 +1,6 @@
 // Host side of the operators on a key-value cache in 8 bits of include/mmv.h: argument checks, workspace carve-up and launches.
 #include <cstdint>
+#include <cuda.h>
 #include <cuda_runtime.h>
 
 #include "../../include/mmv.h"
@@ -14,14 +15,18 @@ namespace {
 
 ServeDevice g_devices[kMaxDevices];
 
-template <bool BF16, bool E4M3, int DP>
+template <bool BF16, bool E4M3, int DP, int ROWS>
 bool allow_one() {
-    return allow_smem(paged_attention_q8_kernel<BF16, E4M3, DP, false>, PagedQ8Cfg<DP>::smem_bytes(PA_ROWS)) &&
-           allow_smem(paged_attention_q8_kernel<BF16, E4M3, DP, true>, PagedQ8Cfg<DP>::smem_bytes(PA_ROWS / 2));
+    return allow_smem(paged_attention_q8_kernel<BF16, E4M3, DP, ROWS, false>, PagedQ8Cfg<DP, ROWS>::smem_bytes(ROWS)) &&
+           allow_smem(paged_attention_q8_kernel<BF16, E4M3, DP, ROWS, true>, PagedQ8Cfg<DP, ROWS>::smem_bytes(ROWS));
+}
+template <int DP, int ROWS>
+bool allow_rows() {
+    return allow_one<false, false, DP, ROWS>() && allow_one<false, true, DP, ROWS>() && allow_one<true, false, DP, ROWS>() && allow_one<true, true, DP, ROWS>();
 }
 template <int DP>
 bool allow_paged() {
-    return allow_one<false, false, DP>() && allow_one<false, true, DP>() && allow_one<true, false, DP>() && allow_one<true, true, DP>();
+    return allow_rows<DP, 4>() && allow_rows<DP, 8>() && allow_rows<DP, 16>();
 }
 ServeDevice* device() {
     return device_once(g_devices, [] { return allow_paged<64>() && allow_paged<128>() && allow_paged<256>(); });
@@ -59,41 +64,73 @@ CacheQ8 cache_params(const mmv_kv_cache_q8* c) {
 }
 uint32_t reciprocal(uint32_t d) { return d == 1 ? 0u : static_cast<uint32_t>(((1ull << 32) + d - 1) / d); }
 
-// Resident CTAs per SM: what the shared memory allows (codes' stages, query rows, rows where the warps meet), and the registers (168 per thread, 255
-// where a row is longer than 128).
+// Resident CTAs per SM: what the shared memory allows (codes' stages, query rows, rows where the warps meet), and the registers.
+template <int DP, int ROWS>
+int fit(int rows) {
+    using C = PagedQ8Cfg<DP, ROWS>;
+    const int shared = 228 * 1024 / (C::smem_bytes(rows) + 3 * 1024);           // (the kernel's other arrays, and 1 KB of every CTA's that is not its own)
+    return shared < C::kPerSm ? shared : C::kPerSm;
+}
 template <int DP>
 int fit(int rows) {
-    const int shared = 227 * 1024 / (PagedQ8Cfg<DP>::smem_bytes(rows) + 2048);
-    return shared < PagedQ8Cfg<DP>::kPerSm ? shared : PagedQ8Cfg<DP>::kPerSm;
+    return rows <= 4 ? fit<DP, 4>(rows) : rows <= 8 ? fit<DP, 8>(rows) : fit<DP, 16>(rows);
 }
 int per_sm(int padded, int rows) { return padded == 64 ? fit<64>(rows) : padded == 128 ? fit<128>(rows) : fit<256>(rows); }
 
 struct Plan {
     size_t desc_off, ml_off, m2_off, o_off, total;
 };
-Plan plan_of(const PagedHeads& h, int dim) {
+int heads_side_by_side(int kv_heads) { return kv_heads % 4 == 0 ? 4 : kv_heads % 2 == 0 ? 2 : 1; }
+Plan plan_of(const PagedHeads& h, int kv_heads, int dim) {
+    const size_t parts = 2 * static_cast<size_t>(heads_side_by_side(kv_heads));       // of a CTA
     const size_t ctas = static_cast<size_t>(kPagedMaxSms) * per_sm(paged_padded(dim), h.rows);
     Plan w;
     w.desc_off = sizeof(WorkspaceHeader);
     w.ml_off = round_up(w.desc_off + ctas * 4 * sizeof(int32_t), 256);
-    w.m2_off = round_up(w.ml_off + ctas * 4 * PA_ROWS * sizeof(float), 256);
-    w.o_off = round_up(w.m2_off + ctas * 2 * PA_ROWS * sizeof(float), 256);
-    w.total = round_up(w.o_off + ctas * 2 * h.rows * dim * sizeof(float), 256);
+    w.m2_off = round_up(w.ml_off + ctas * parts * 2 * PA_ROWS * sizeof(float), 256);
+    w.o_off = round_up(w.m2_off + ctas * parts * PA_ROWS * sizeof(float), 256);
+    w.total = round_up(w.o_off + ctas * parts * h.rows * dim * sizeof(float), 256);
     return w;
 }
 
-template <bool BF16, bool E4M3, int DP>
-mmv_status launch_dim(const PagedQ8Params& p, int ctas, cudaStream_t st) {
-    const size_t smem = static_cast<size_t>(PagedQ8Cfg<DP>::smem_bytes(p.rows));
+// The cache's codes as boxes of 16 tokens of one head of one block, 128-byte swizzle (64-byte for rows of 64); false where they cannot be described so.
+bool code_map(CUtensorMap* map, const void* x, const mmv_kv_cache_q8* c, int padded) {
+    EncodeTiledFn enc = get_encode();
+    if (!enc) return false;
+    const cuuint64_t row = static_cast<cuuint64_t>(c->dim);
+    const cuuint64_t dims[4] = {row, static_cast<cuuint64_t>(c->heads), static_cast<cuuint64_t>(c->block_size), static_cast<cuuint64_t>(c->num_blocks)};
+    const cuuint64_t strides[3] = {c->heads > 1 ? static_cast<cuuint64_t>(c->stride_head) : row, static_cast<cuuint64_t>(c->stride_token),
+                                   c->num_blocks > 1 ? static_cast<cuuint64_t>(c->stride_block) : row};
+    const cuuint32_t box[4] = {padded < 128 ? 64u : 128u, 1, 16, 1}, estr[4] = {1, 1, 1, 1};
+    return enc(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 4, const_cast<void*>(x), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+               padded < 128 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) ==
+           CUDA_SUCCESS;
+}
+
+struct CodeMaps {
+    CUtensorMap k, v;
+    bool box;
+};
+template <bool BF16, bool E4M3, int DP, int ROWS>
+mmv_status launch_rows(const CodeMaps& m, const PagedQ8Params& p, int ctas, cudaStream_t st) {
+    const size_t smem = static_cast<size_t>(PagedQ8Cfg<DP, ROWS>::smem_bytes(p.rows));
     const dim3 grid(static_cast<unsigned>(ctas));
-    const mmv_status rc = p.rows <= 8 ? launch(paged_attention_q8_kernel<BF16, E4M3, DP, true>, grid, PA_THREADS, smem, st, false, p)
-                                      : launch(paged_attention_q8_kernel<BF16, E4M3, DP, false>, grid, PA_THREADS, smem, st, false, p);
+    const mmv_status rc = m.box ? launch(paged_attention_q8_kernel<BF16, E4M3, DP, ROWS, true>, grid, PA_THREADS, smem, st, false, m.k, m.v, p)
+                                : launch(paged_attention_q8_kernel<BF16, E4M3, DP, ROWS, false>, grid, PA_THREADS, smem, st, false, m.k, m.v, p);
     if (rc != MMV_OK) return rc;
-    return launch(paged_join_q8_kernel<BF16>, dim3(static_cast<unsigned>(ctas), static_cast<unsigned>(p.rows)), PA_JOIN_THREADS, 0, st, true, p, ctas);
+    return launch(paged_join_q8_kernel<BF16>, dim3(static_cast<unsigned>(ctas), static_cast<unsigned>(p.rows * p.side)), PA_JOIN_THREADS, 0, st, true, p, ctas);
+}
+template <bool BF16, bool E4M3, int DP>
+mmv_status launch_dim(const CodeMaps& m, const PagedQ8Params& p, int ctas, cudaStream_t st) {
+    return p.rows <= 4   ? launch_rows<BF16, E4M3, DP, 4>(m, p, ctas, st)
+           : p.rows <= 8 ? launch_rows<BF16, E4M3, DP, 8>(m, p, ctas, st)
+                         : launch_rows<BF16, E4M3, DP, 16>(m, p, ctas, st);
 }
 template <bool BF16, bool E4M3>
-mmv_status launch_paged(const PagedQ8Params& p, int padded, int ctas, cudaStream_t st) {
-    return padded == 64 ? launch_dim<BF16, E4M3, 64>(p, ctas, st) : padded == 128 ? launch_dim<BF16, E4M3, 128>(p, ctas, st) : launch_dim<BF16, E4M3, 256>(p, ctas, st);
+mmv_status launch_paged(const CodeMaps& m, const PagedQ8Params& p, int padded, int ctas, cudaStream_t st) {
+    return padded == 64    ? launch_dim<BF16, E4M3, 64>(m, p, ctas, st)
+           : padded == 128 ? launch_dim<BF16, E4M3, 128>(m, p, ctas, st)
+                           : launch_dim<BF16, E4M3, 256>(m, p, ctas, st);
 }
 
 template <bool BF16, bool E4M3>
@@ -198,7 +235,7 @@ mmv_status mmv_kv_read_q8(const mmv_kv_cache_q8* cache, const int32_t* table, in
 
 size_t mmv_paged_attention_q8_workspace_bytes(int32_t heads, const mmv_kv_cache_q8* cache) {
     if (check_cache(cache) != MMV_OK || heads < 1 || heads > kMaxHeads || heads % cache->heads) return 0;
-    return plan_of(paged_heads(heads, cache->heads, PA_ROWS), cache->dim).total;
+    return plan_of(paged_heads(heads, cache->heads, PA_ROWS), cache->heads, cache->dim).total;
 }
 
 mmv_status mmv_paged_attention_q8(const void* q, int64_t q_stride_request, int64_t q_stride_head, int32_t heads, mmv_dtype dtype,
@@ -212,7 +249,7 @@ mmv_status mmv_paged_attention_q8(const void* q, int64_t q_stride_request, int64
     if (nreq && (!q || !aligned(q, 16) || !lens || !aligned(lens, 4) || !out || !aligned(out, 16) || (lse && !aligned(lse, 4)))) return MMV_ERR_INVALID_ARG;
     if (!check_table(table, table_stride, max_blocks, nreq)) return MMV_ERR_INVALID_ARG;
     const PagedHeads h = paged_heads(heads, cache->heads, PA_ROWS);
-    const Plan plan = plan_of(h, cache->dim);
+    const Plan plan = plan_of(h, cache->heads, cache->dim);
     if (workspace_bytes < plan.total) return MMV_ERR_WORKSPACE_TOO_SMALL;
     cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
     if (nreq == 0) return cudaMemsetAsync(workspace, 0, sizeof(WorkspaceHeader), st) == cudaSuccess ? MMV_OK : MMV_ERR_CUDA;
@@ -237,7 +274,7 @@ mmv_status mmv_paged_attention_q8(const void* q, int64_t q_stride_request, int64
     p.lens = lens;
     p.table_stride = table_stride;
     p.num_blocks = cache->num_blocks;
-    const int64_t longest = INT32_MAX - 4 * PA_TILE;                 // (positions past a tile's end stay within 32 bits)
+    const int64_t longest = INT32_MAX - 16 * PA_TILE;                // (positions past a tile's end stay within 32 bits)
     p.capacity = max_blocks > longest / cache->block_size ? longest : max_blocks * cache->block_size;
     p.window = window;
     p.nreq = static_cast<int>(nreq);
@@ -257,14 +294,22 @@ mmv_status mmv_paged_attention_q8(const void* q, int64_t q_stride_request, int64
     p.part_m2 = reinterpret_cast<float*>(ws + plan.m2_off);
     p.part_o = reinterpret_cast<float*>(ws + plan.o_off);
     const int padded = paged_padded(p.dim);
+    p.budget_ns = g_budget_ns.load();
+    p.by_block = 0;
+    CodeMaps maps{};
+    maps.box = cache->num_blocks > 0 && cache->block_size % 16 == 0 && code_map(&maps.k, cache->k, cache, padded) && code_map(&maps.v, cache->v, cache, padded);
+    if (maps.box) p.by_block = static_cast<uint32_t>((1ull << 32) / static_cast<uint32_t>(cache->block_size));
     // one CTA per tile that the tables could hold, up to all that are resident at once
     const int sms = dev->sm_count < kPagedMaxSms ? dev->sm_count : kPagedMaxSms;
-    const double most = static_cast<double>(nreq) * p.kv_heads * p.parts * (static_cast<double>(p.capacity) / PA_TILE + 2.0);
+    p.side = heads_side_by_side(p.kv_heads);
+    p.tile = 4 * Q8_TOKENS / p.side;
+    p.groups = p.kv_heads / p.side * p.parts;
+    const double most = static_cast<double>(nreq) * p.groups * (static_cast<double>(p.capacity) / p.tile + 2.0);
     int ctas = sms * per_sm(padded, p.rows);
     if (most < ctas) ctas = static_cast<int>(most);
     const bool e4m3 = cache->code == MMV_CODE_E4M3;
-    if (dtype == MMV_BF16_TO_F32) return e4m3 ? launch_paged<true, true>(p, padded, ctas, st) : launch_paged<true, false>(p, padded, ctas, st);
-    return e4m3 ? launch_paged<false, true>(p, padded, ctas, st) : launch_paged<false, false>(p, padded, ctas, st);
+    if (dtype == MMV_BF16_TO_F32) return e4m3 ? launch_paged<true, true>(maps, p, padded, ctas, st) : launch_paged<true, false>(maps, p, padded, ctas, st);
+    return e4m3 ? launch_paged<false, true>(maps, p, padded, ctas, st) : launch_paged<false, false>(maps, p, padded, ctas, st);
 }
 
 }  // extern "C"
