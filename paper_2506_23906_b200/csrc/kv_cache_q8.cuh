@@ -89,6 +89,30 @@ __device__ __forceinline__ uint32_t q8_narrow(float a, float b) {
     }
 }
 
+// n / d for n * d < 2^32, by = ceil(2^32 / d); 0 for a divisor of 1
+__device__ __forceinline__ int q8_quotient(int n, uint32_t by) { return by ? static_cast<int>(__umulhi(static_cast<uint32_t>(n), by)) : n; }
+
+// 32 bytes in one access where `wide` says that they are aligned so (a lane's two accesses of 16 each leave half of every 32-byte sector to the other)
+__device__ __forceinline__ void q8_load(uint4 (&v)[2], const void* p, bool wide) {
+    if (wide) {
+        asm volatile("ld.global.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                     : "=r"(v[0].x), "=r"(v[0].y), "=r"(v[0].z), "=r"(v[0].w), "=r"(v[1].x), "=r"(v[1].y), "=r"(v[1].z), "=r"(v[1].w)
+                     : "l"(p));
+    } else {
+        v[0] = static_cast<const uint4*>(p)[0];
+        v[1] = static_cast<const uint4*>(p)[1];
+    }
+}
+__device__ __forceinline__ void q8_store(void* p, const uint32_t (&v)[8], bool wide) {
+    if (wide) {
+        asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
+                     ::"l"(p), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]) : "memory");
+    } else {
+        static_cast<uint4*>(p)[0] = make_uint4(v[0], v[1], v[2], v[3]);
+        static_cast<uint4*>(p)[1] = make_uint4(v[4], v[5], v[6], v[7]);
+    }
+}
+
 // How many of offsets[1 .. n] are <= t: the sequence that token t belongs to (n: none).  32 samples per trip to memory; any values in
 // offsets give a result in [0, n].
 __device__ __forceinline__ int q8_sequence_of(const int32_t* offsets, int n, int t) {
@@ -105,10 +129,10 @@ __device__ __forceinline__ int q8_sequence_of(const int32_t* offsets, int n, int
 
 // ---------------------------------------------------------------------------------------------------------------------
 // The write.  3 bytes of traffic per value: bound by HBM for prompts, by the launch and a chain of dependent trips (offsets, page,
-// old scale, store) for a decoding step.
+// old scale and values, store) for a decoding step.
 //
-// Split: a unit is (window of tokens, head, keys or values), taken by a group of threads (a warp where a run is short, else the CTA); a
-// group takes the RUNS that begin in its window.  A run is a request's tokens that lie in one block: all that a scale depends on
+// Split: a unit is (window of tokens, group of heads, keys or values), taken by a group of threads (a warp where a run is short, else the CTA); it
+// takes the RUNS that begin in its window, head by head.  A run is a request's tokens that lie in one block: all that a scale depends on
 // besides the old one, so that no unit meets another's and nothing has to be joined.  The run's values are loaded once and stay in
 // registers (Q8_KEEP elements of 16 per thread; what is longer is read a second time, from the L2) between the maximum and the codes.
 // ---------------------------------------------------------------------------------------------------------------------
@@ -121,34 +145,40 @@ struct AppendQ8Params {
     long long x_tok[2], x_head[2];
     const int32_t *offsets, *total, *table;
     long long table_stride, max_blocks;
-    int nreq, ntok, window;
+    int nreq, ntok, window, side;                            // side: heads of a unit
+    bool wide;                                               // rows on 32-byte words
+    uint32_t by_row;                                         // reciprocal (q8_quotient) of dim / 16
     long long units;
 };
 
 template <bool BF16, bool E4M3, bool WARP>
-__global__ void __launch_bounds__(Q8_THREADS) kv_append_q8_kernel(const AppendQ8Params p) {
+__global__ void __launch_bounds__(Q8_THREADS, 6) kv_append_q8_kernel(const AppendQ8Params p) {
     constexpr int G = WARP ? 32 : Q8_THREADS;
     constexpr float top = E4M3 ? 448.f : 127.f;
     __shared__ uint32_t s_max[2][Q8_THREADS / 32];
     const int me = threadIdx.x % G, per = p.c.dim / 16;      // elements of 16 values per row
     const long long unit = static_cast<long long>(blockIdx.x) * (Q8_THREADS / G) + threadIdx.x / G;
     if (unit >= p.units) return;
-    const int head = static_cast<int>(unit % p.c.heads), kv = static_cast<int>(unit / p.c.heads % 2);
-    const int t0 = static_cast<int>(unit / (2 * p.c.heads)) * p.window, t1 = min(p.ntok, t0 + p.window);       // (below 2^31: window divides it up)
-    const uint16_t* x = p.x[kv] + head * p.x_head[kv];
-    uint8_t* codes = p.c.code[kv] + head * p.c.head;
-    float* scales = p.c.scale[kv] + head * p.c.s_head;
+    const int groups = (p.c.heads + p.side - 1) / p.side;
+    const int head0 = static_cast<int>(unit % groups) * p.side, head1 = min(p.c.heads, head0 + p.side), kv = static_cast<int>(unit / groups % 2);
+    const int t0 = static_cast<int>(unit / (2 * groups)) * p.window, t1 = min(p.ntok, t0 + p.window);       // (below 2^31: window divides it up)
     int turn = 0;
+    // the request that token t belongs to: its rows [lo, hi), and what it holds with them (one token of every request: request t)
+    int r = t0 < p.nreq ? t0 : 0, lo = p.offsets[r], hi = p.offsets[r + 1], total = p.total[r];
     for (int t = t0; t < t1;) {
-        const int r = q8_sequence_of(p.offsets, p.nreq, t);
-        if (r >= p.nreq) return;
-        const int lo = p.offsets[r], hi = p.offsets[r + 1];
+        if (t < lo || t >= hi) {
+            r = q8_sequence_of(p.offsets, p.nreq, t);
+            if (r >= p.nreq) return;
+            lo = p.offsets[r];
+            hi = p.offsets[r + 1];
+            total = p.total[r];
+        }
         if (lo < 0 || hi > p.ntok || hi <= t) return;        // (not offsets: nothing is written)
         if (lo > t) {                                        // tokens in front of the first request
             t = lo;
             continue;
         }
-        const long long past = static_cast<long long>(p.total[r]) - (hi - lo), at = past + (t - lo);
+        const long long past = static_cast<long long>(total) - (hi - lo), at = past + (t - lo);
         if (past < 0) {
             t = hi;
             continue;
@@ -161,87 +191,100 @@ __global__ void __launch_bounds__(Q8_THREADS) kv_append_q8_kernel(const AppendQ8
         if (b >= p.max_blocks) continue;
         const long long page = p.table[r * p.table_stride + b];
         if (page < 0 || page >= p.c.num_blocks) continue;
-        float* scale = scales + page * p.c.s_block;
-        const float old = place > 0 ? *scale : 0.f;
 
-        // the run's values and their largest magnitude (as bits: a NaN is above infinity)
         const int n = len * per;
         uint4 w[Q8_KEEP][2];
-        uint32_t most = 0u;
-        const auto load = [&](int i, uint4 (&v)[2]) {
+        float old;                                           // the old scale
+        // this thread's elements: offsets in the values and in the block
+        long long src[Q8_KEEP], to[Q8_KEEP];
+#pragma unroll
+        for (int i = 0; i < Q8_KEEP; ++i) {
+            const int row = q8_quotient(me + i * G, p.by_row), col = me + i * G - row * per;
+            src[i] = (first + row) * p.x_tok[kv] + col * 16;
+            to[i] = (place + row) * p.c.tok + col * 16;
+        }
+        const auto fetch = [&](int i, int head, uint4 (&v)[2]) {                 // (elements past those)
             const int row = i / per, col = i - row * per;
-            const uint4* src = reinterpret_cast<const uint4*>(x + (first + row) * p.x_tok[kv] + col * 16);
-            v[0] = src[0];
-            v[1] = src[1];
+            q8_load(v, p.x[kv] + (first + row) * p.x_tok[kv] + head * p.x_head[kv] + col * 16, p.wide);
         };
-        const auto widest = [&](const uint4 (&v)[2]) {
+        const auto load = [&](int head) {
+            old = place > 0 ? p.c.scale[kv][page * p.c.s_block + head * p.c.s_head] : 0.f;
 #pragma unroll
-            for (int j = 0; j < 2; ++j) {
-                most = __vmaxu2(most, v[j].x & 0x7fff7fffu);
-                most = __vmaxu2(most, v[j].y & 0x7fff7fffu);
-                most = __vmaxu2(most, v[j].z & 0x7fff7fffu);
-                most = __vmaxu2(most, v[j].w & 0x7fff7fffu);
+            for (int i = 0; i < Q8_KEEP; ++i)
+                if (me + i * G < n) q8_load(w[i], p.x[kv] + head * p.x_head[kv] + src[i], p.wide);
+        };
+        const auto process = [&](int head) {
+            // the run's largest magnitude (as bits: a NaN is above infinity)
+            uint32_t most = 0u;
+            const auto widest = [&](const uint4 (&v)[2]) {
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {
+                    most = __vmaxu2(most, v[j].x & 0x7fff7fffu);
+                    most = __vmaxu2(most, v[j].y & 0x7fff7fffu);
+                    most = __vmaxu2(most, v[j].z & 0x7fff7fffu);
+                    most = __vmaxu2(most, v[j].w & 0x7fff7fffu);
+                }
+            };
+#pragma unroll
+            for (int i = 0; i < Q8_KEEP; ++i)
+                if (me + i * G < n) widest(w[i]);
+            for (int i = me + Q8_KEEP * G; i < n; i += G) {
+                uint4 v[2];
+                fetch(i, head, v);
+                widest(v);
             }
-        };
+            most = __reduce_max_sync(0xffffffffu, max(most & 0xffffu, most >> 16));
+            if constexpr (!WARP) {
+                if ((threadIdx.x & 31) == 0) s_max[turn][threadIdx.x / 32] = most;
+                __syncthreads();
 #pragma unroll
-        for (int i = 0; i < Q8_KEEP; ++i)
-            if (me + i * G < n) load(me + i * G, w[i]);
+                for (int i = 0; i < Q8_THREADS / 32; ++i) most = max(most, s_max[turn][i]);
+                turn ^= 1;                                   // (the next maxima go elsewhere: one barrier is enough)
+            }
+            const bool wild = most >= (BF16 ? 0x7f80u : 0x7c00u) || !(old >= 0.f && old < INFINITY);
+            const float amax = q8_widen<BF16>(most).x;
+            const float now = wild ? __uint_as_float(0x7fc00000u) : amax <= old * top ? old : q8_scale_of<E4M3>(amax);
+            const float inv = q8_inverse<E4M3>(now);         // (0 for a scale that is 0 or NaN: the codes are 0)
+            uint8_t* dst = p.c.code[kv] + page * p.c.block + head * p.c.head;
+            if (place > 0 && now > old) {                    // the scale grows: the codes in front of the run are converted
+                for (int i = me; i < place * per; i += G) {
+                    const int row = i / per, col = i - row * per;
+                    uint4* q = reinterpret_cast<uint4*>(dst + row * p.c.tok + col * 16);
+                    uint4 v = *q;
+                    uint32_t* word = reinterpret_cast<uint32_t*>(&v);
 #pragma unroll
-        for (int i = 0; i < Q8_KEEP; ++i)
-            if (me + i * G < n) widest(w[i]);
-        for (int i = me + Q8_KEEP * G; i < n; i += G) {
-            uint4 v[2];
-            load(i, v);
-            widest(v);
-        }
-        most = __reduce_max_sync(0xffffffffu, max(most & 0xffffu, most >> 16));
-        if constexpr (!WARP) {
-            if ((threadIdx.x & 31) == 0) s_max[turn][threadIdx.x / 32] = most;
-            __syncthreads();
-#pragma unroll
-            for (int i = 0; i < Q8_THREADS / 32; ++i) most = max(most, s_max[turn][i]);
-            turn ^= 1;                                       // (the next run's maxima go elsewhere: one barrier per run is enough)
-        }
-        const bool wild = most >= (BF16 ? 0x7f80u : 0x7c00u) || !(old >= 0.f && old < INFINITY);
-        const float amax = q8_widen<BF16>(most).x;
-        const float now = wild ? __uint_as_float(0x7fc00000u) : amax <= old * top ? old : q8_scale_of<E4M3>(amax);
-        const float inv = q8_inverse<E4M3>(now);             // (0 for a scale that is 0 or NaN: the codes are 0)
-        uint8_t* dst = codes + page * p.c.block;
-        if (place > 0 && now > old) {                        // the scale grows: the codes in front of the run are converted
-            for (int i = me; i < place * per; i += G) {
-                const int row = i / per, col = i - row * per;
-                uint4* q = reinterpret_cast<uint4*>(dst + row * p.c.tok + col * 16);
-                uint4 v = *q;
-                uint32_t* word = reinterpret_cast<uint32_t*>(&v);
+                    for (int j = 0; j < 4; ++j) {
+                        const float4 y = q8_unpack<E4M3>(word[j]);
+                        word[j] = q8_pack<E4M3>(y.x * old, y.y * old, y.z * old, y.w * old, inv);
+                    }
+                    *q = v;
+                }
+            }
+            const auto store = [&](long long at, const uint4 (&v)[2]) {
+                uint32_t out[4];
+                const uint32_t in[8] = {v[0].x, v[0].y, v[0].z, v[0].w, v[1].x, v[1].y, v[1].z, v[1].w};
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
-                    const float4 y = q8_unpack<E4M3>(word[j]);
-                    word[j] = q8_pack<E4M3>(y.x * old, y.y * old, y.z * old, y.w * old, inv);
+                    const float2 a = q8_widen<BF16>(in[2 * j]), c = q8_widen<BF16>(in[2 * j + 1]);
+                    out[j] = wild ? 0u : q8_pack<E4M3>(a.x, a.y, c.x, c.y, inv);
                 }
-                *q = v;
-            }
-        }
-        const auto store = [&](int i, const uint4 (&v)[2]) {
-            const int row = i / per, col = i - row * per;
-            uint32_t out[4];
-            const uint32_t in[8] = {v[0].x, v[0].y, v[0].z, v[0].w, v[1].x, v[1].y, v[1].z, v[1].w};
+                *reinterpret_cast<uint4*>(dst + at) = make_uint4(out[0], out[1], out[2], out[3]);
+            };
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const float2 a = q8_widen<BF16>(in[2 * j]), c = q8_widen<BF16>(in[2 * j + 1]);
-                out[j] = wild ? 0u : q8_pack<E4M3>(a.x, a.y, c.x, c.y, inv);
+            for (int i = 0; i < Q8_KEEP; ++i)
+                if (me + i * G < n) store(to[i], w[i]);
+            for (int i = me + Q8_KEEP * G; i < n; i += G) {
+                uint4 v[2];
+                fetch(i, head, v);
+                store((place + i / per) * p.c.tok + i % per * 16, v);
             }
-            *reinterpret_cast<uint4*>(dst + (place + row) * p.c.tok + col * 16) = make_uint4(out[0], out[1], out[2], out[3]);
+            if constexpr (WARP) __syncwarp();                // (every lane has read the old scale)
+            if (me == 0 && !(now == old && place > 0)) p.c.scale[kv][page * p.c.s_block + head * p.c.s_head] = now;
         };
-#pragma unroll
-        for (int i = 0; i < Q8_KEEP; ++i)
-            if (me + i * G < n) store(me + i * G, w[i]);
-        for (int i = me + Q8_KEEP * G; i < n; i += G) {
-            uint4 v[2];
-            load(i, v);
-            store(i, v);
+        for (int head = head0; head < head1; ++head) {
+            load(head);
+            process(head);
         }
-        if constexpr (WARP) __syncwarp();                    // (every lane has read the old scale)
-        if (me == 0 && !(now == old && place > 0)) *scale = now;
     }
 }
 
@@ -258,11 +301,10 @@ struct ReadQ8Params {
     const int32_t *offsets, *table;
     long long table_stride, max_blocks;
     int nreq, ntok, tile;
+    bool wide;                                               // results on 32-byte words
     int words;                                               // of a token: heads * dim / 16
-    uint32_t by_words, by_head;                              // ceil(2^32 / words), ceil(2^32 / (dim / 16)); 0 for a divisor of 1
+    uint32_t by_words, by_head;                              // reciprocals (q8_quotient) of words and dim / 16
 };
-// n / d for n * d < 2^32, by the reciprocal above
-__device__ __forceinline__ int q8_quotient(int n, uint32_t by) { return by ? static_cast<int>(__umulhi(static_cast<uint32_t>(n), by)) : n; }
 
 template <bool BF16, bool E4M3>
 __global__ void __launch_bounds__(READ_Q8_THREADS) kv_read_q8_kernel(const ReadQ8Params p) {
@@ -331,9 +373,7 @@ __global__ void __launch_bounds__(READ_Q8_THREADS) kv_read_q8_kernel(const ReadQ
                         out[2 * e] = q8_narrow<BF16>(y.x * s[u][kv], y.y * s[u][kv]);
                         out[2 * e + 1] = q8_narrow<BF16>(y.z * s[u][kv], y.w * s[u][kv]);
                     }
-                    uint4* to = reinterpret_cast<uint4*>(p.out[kv] + dst[u]);
-                    to[0] = make_uint4(out[0], out[1], out[2], out[3]);
-                    to[1] = make_uint4(out[4], out[5], out[6], out[7]);
+                    q8_store(p.out[kv] + dst[u], out, p.wide);
                 }
             }
         }

@@ -157,7 +157,8 @@ mmv_status mmv_kv_append_q8(const void* k, int64_t k_stride_token, int64_t k_str
         return MMV_ERR_INVALID_ARG;
     if (ntok == 0 || nreq == 0 || cache->num_blocks == 0 || max_blocks == 0) return MMV_OK;
     if (!k || !v || !aligned(k, 16) || !aligned(v, 16) || !offsets || !aligned(offsets, 4) || !total || !aligned(total, 4)) return MMV_ERR_INVALID_ARG;
-    if (!device()) return MMV_ERR_CUDA;
+    ServeDevice* dev = device();
+    if (!dev) return MMV_ERR_CUDA;
     AppendQ8Params p;
     p.c = cache_params(cache);
     p.x[0] = static_cast<const uint16_t*>(k);
@@ -173,18 +174,22 @@ mmv_status mmv_kv_append_q8(const void* k, int64_t k_stride_token, int64_t k_str
     p.max_blocks = max_blocks;
     p.nreq = static_cast<int>(nreq);
     p.ntok = static_cast<int>(ntok);
+    p.wide = aligned(k, 32) && aligned(v, 32) && word_stride(k_stride_token, ntok, 16) && word_stride(k_stride_head, cache->heads, 16) &&
+             word_stride(v_stride_token, ntok, 16) && word_stride(v_stride_head, cache->heads, 16);
+    p.by_row = reciprocal(static_cast<uint32_t>(cache->dim / 16));
     // A window of a run's mean length: what a request adds, cut at the blocks' ends.
     const int64_t runs = ntok / cache->block_size + nreq;
     int64_t window = (ntok + runs - 1) / runs;
     if (window < 1) window = 1;
+    // Heads of a unit: as many as leave 32 units per SM (eight CTAs' worth are resident).
+    int64_t side = (ntok + window - 1) / window * 2 * cache->heads / (32ll * dev->sm_count);
+    side = side < 1 ? 1 : side > cache->heads ? cache->heads : side;
+    const int64_t per_window = 2 * ((cache->heads + side - 1) / side);
+    const int64_t most = INT32_MAX / per_window;             // (a grid's first axis ends at 2^31 - 1)
+    if ((ntok + window - 1) / window > most) window = (ntok + most - 1) / most;
     p.window = static_cast<int>(window);
-    p.units = (ntok + window - 1) / window * 2 * cache->heads;
-    if (p.units > INT32_MAX) {                               // (wider windows: a grid's first axis ends at 2^31 - 1)
-        const int64_t most = INT32_MAX / (2 * cache->heads);
-        window = (ntok + most - 1) / most;
-        p.window = static_cast<int>(window);
-        p.units = (ntok + window - 1) / window * 2 * cache->heads;
-    }
+    p.side = static_cast<int>(side);
+    p.units = (ntok + window - 1) / window * per_window;
     const bool warp = window * (cache->dim / 16) <= 32 * Q8_KEEP;
     cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
     const bool e4m3 = cache->code == MMV_CODE_E4M3;
@@ -211,6 +216,7 @@ mmv_status mmv_kv_read_q8(const mmv_kv_cache_q8* cache, const int32_t* table, in
     p.max_blocks = max_blocks;
     p.nreq = static_cast<int>(nreq);
     p.ntok = static_cast<int>(ntok);
+    p.wide = aligned(k_out, 32) && aligned(v_out, 32);
     p.words = cache->heads * (cache->dim / 16);
     p.by_words = reciprocal(static_cast<uint32_t>(p.words));
     p.by_head = reciprocal(static_cast<uint32_t>(cache->dim / 16));
