@@ -153,9 +153,10 @@ __global__ void __launch_bounds__(LIN_STEP_THREADS) delta_step_kernel(const Delt
 // T and A do not depend on the state: a first kernel forms them for all chunks side by side; the second one walks along a sequence's chunks, one
 // CTA per (sequence, head, slice of columns), whose columns never meet others'.
 //
-// Operands that are formed here enter their products as sums of bfloat16 values, of two (2^-17 of the value; products of two such leave
-// out the two low parts', 2^-18) or, where the fp32 state would lose by it, of three: its own copy in K S and the update's exp(G_n - G) U.
-// U is R + (T - 1) R, the first term in fp32.  With two parts everywhere and T R as a product the state was off by 4.0e-6 of itself.
+// Operands that are formed here enter their products as sums of bfloat16 values, of two (2^-17 of the value) or, where the fp32 state would lose by
+// it, of three: its own copy in K S, R and the update's exp(G_n - G) U.  U is R + (T - 1) R, the first term in fp32; what is added to a
+// state or to R is summed up by itself, since the tensor core cuts a sum's last digits.  With two parts everywhere, T R as one product and the sums
+// begun at S and R the state was off by 4.0e-6 of itself; it is by 0.9e-6 (fp32 throughout: 0.16e-6).
 //
 // A chunk that holds a value that is not finite (or whose products are not) is taken token by token: zeros of the triangles would carry it to
 // tokens in front of it.
@@ -584,8 +585,10 @@ struct DeltaCfg {
     static constexpr int kK = 0, kQ = 2 * kTile, kT = kQ + (kDeep ? 2 : 1) * kTile;          // T, A or both in turn
     static constexpr int kX = kT + (kDeep ? 4 : 1) * kBlocks, kXPitch = 1024;    // the scalars
     static constexpr int kS = kX + 2 * kXPitch, kSPart = DK * kPitch;            // the state, three parts
-    static constexpr int kR = kS + 3 * kSPart, kRPart = DELTA_C * kPitch;        // two
-    static constexpr int kU = kR + 2 * kRPart;                                   // two
+    // R: three parts, two where a third would not leave room for two CTAs per SM (keys of more than 64 columns overlap less, and T - 1 is smaller)
+    static constexpr int kRParts = DK == 64 || kDeep ? 3 : 2;
+    static constexpr int kR = kS + 3 * kSPart, kRPart = DELTA_C * kPitch;
+    static constexpr int kU = kR + kRParts * kRPart;                             // two
     static constexpr int kW = kU + 2 * kRPart;                                   // exp(G_n - G) U, three
     static constexpr int kSmemBytes = kW + 3 * kRPart;
     static_assert(4 * NV * 4 <= 2 * kRPart, "token by token: sums in R's place");
@@ -819,11 +822,12 @@ delta_chunks_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_cons
                     const bool on = row < n;
                     x[j][2 * e] = on ? beta[e] * (w.x - past[e] * x[j][2 * e]) : 0.f;
                     x[j][2 * e + 1] = on ? beta[e] * (w.y - past[e] * x[j][2 * e + 1]) : 0.f;
-                    uint32_t hi, lo;
-                    delta_split(x[j][2 * e], x[j][2 * e + 1], hi, lo);
+                    uint32_t r[3];
+                    if (C::kRParts == 3) delta_split3(x[j][2 * e], x[j][2 * e + 1], r);
+                    else delta_split(x[j][2 * e], x[j][2 * e + 1], r[0], r[1]);
                     uint8_t* at = address(C::kR, row, j);
-                    *reinterpret_cast<uint32_t*>(at) = hi;
-                    *reinterpret_cast<uint32_t*>(at + C::kRPart) = lo;
+#pragma unroll
+                    for (int part = 0; part < C::kRParts; ++part) *reinterpret_cast<uint32_t*>(at + part * C::kRPart) = r[part];
                 }
         }
         if (chunk + 1 < end) values(chunk + 1);
@@ -838,21 +842,25 @@ delta_chunks_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_cons
         if (!wild) {
             // ---- U = R + (T - 1) R ---------------------------------------------------------------------------------------------------------
             const uint4* solver = blocks + delta_tile(block, 0) * 32 + lane;
-            float z[N][4];
+            float u[N][4], z[N][4];                          // (sums of their own: the tensor core's cut digits at the end, and R's are not to be cut)
 #pragma unroll
             for (int j = 0; j < N; ++j)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) z[j][e] = 0.f;
+                for (int e = 0; e < 4; ++e) u[j][e] = z[j][e] = 0.f;
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
                 if (k > block) break;
                 const uint4 th = solver[k * 32], tl = solver[(DELTA_TILES + k) * 32];
                 const uint32_t ah[4] = {th.x, th.y, th.z, th.w}, al[4] = {tl.x, tl.y, tl.z, tl.w};
+                uint32_t b3[N][2];
+                if (C::kRParts == 3) third(b3, C::kR + 2 * C::kRPart, k * 16);
 #pragma unroll
                 for (int j = 0; j < N; ++j) {
                     uint32_t b[4];
                     operand(b, C::kR, C::kRPart, k * 16, j);
-                    mma_16816<true>(x[j], ah, b[0], b[1]);
+                    if (C::kRParts == 3) mma_16816<true>(z[j], ah, b3[j][0], b3[j][1]);
+                    mma_16816<true>(u[j], ah, b[0], b[1]);
+                    mma_16816<true>(z[j], al, b[2], b[3]);
                     mma_16816<true>(z[j], al, b[0], b[1]);
                     mma_16816<true>(z[j], ah, b[2], b[3]);
                 }
@@ -862,7 +870,7 @@ delta_chunks_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_cons
             for (int j = 0; j < N; ++j)
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
-                    const float a = x[j][2 * e] + z[j][2 * e], b = x[j][2 * e + 1] + z[j][2 * e + 1];
+                    const float a = x[j][2 * e] + (u[j][2 * e] + z[j][2 * e]), b = x[j][2 * e + 1] + (u[j][2 * e + 1] + z[j][2 * e + 1]);
                     uint32_t r[3];
                     delta_split(a, b, r[0], r[1]);
                     uint8_t* at = address(C::kU, block * 16 + g + 8 * e, j);
@@ -876,15 +884,15 @@ delta_chunks_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_cons
             __syncthreads();
             if (!C::kDeep && tid == 192) load_blocks(made[static_cast<long long>(chunk) * p.heads].a);
             // ---- S' = exp(G_n) S + K^T (exp(G_n - G) U) -----------------------------------------------------------------------------------
-            const float wh = info->whole_hi, wl = info->whole_lo;
-#pragma unroll
-            for (int m = 0; m < M; ++m)
-#pragma unroll
-                for (int j = 0; j < N; ++j)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) s[m][j][e] = fmaf(s[m][j][e], wh, s[m][j][e] * wl);
             {
                 uint32_t a[2][M][4], b[2][N][4], b3[2][N][2];
+                float d[M][N][4];                            // (a sum of its own, as above: the state is not to be cut every time)
+#pragma unroll
+                for (int m = 0; m < M; ++m)
+#pragma unroll
+                    for (int j = 0; j < N; ++j)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) d[m][j][e] = 0.f;
                 const auto load = [&](int k) {
 #pragma unroll
                     for (int m = 0; m < M; ++m)
@@ -901,16 +909,23 @@ delta_chunks_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_cons
 #pragma unroll
                     for (int j = 0; j < N; ++j)
 #pragma unroll
-                        for (int m = 0; m < M; ++m) mma_16816<true>(s[m][j], a[i][m], b3[i][j][0], b3[i][j][1]);
+                        for (int m = 0; m < M; ++m) mma_16816<true>(d[m][j], a[i][m], b3[i][j][0], b3[i][j][1]);
 #pragma unroll
                     for (int j = 0; j < N; ++j)
 #pragma unroll
-                        for (int m = 0; m < M; ++m) mma_16816<true>(s[m][j], a[i][m], b[i][j][2], b[i][j][3]);
+                        for (int m = 0; m < M; ++m) mma_16816<true>(d[m][j], a[i][m], b[i][j][2], b[i][j][3]);
 #pragma unroll
                     for (int j = 0; j < N; ++j)
 #pragma unroll
-                        for (int m = 0; m < M; ++m) mma_16816<true>(s[m][j], a[i][m], b[i][j][0], b[i][j][1]);
+                        for (int m = 0; m < M; ++m) mma_16816<true>(d[m][j], a[i][m], b[i][j][0], b[i][j][1]);
                 }
+                const float wh = info->whole_hi, wl = info->whole_lo;
+#pragma unroll
+                for (int m = 0; m < M; ++m)
+#pragma unroll
+                    for (int j = 0; j < N; ++j)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) s[m][j][e] = fmaf(s[m][j][e], wh, fmaf(s[m][j][e], wl, d[m][j][e]));
             }
             // ---- O = scale (exp(G) Q S + A U) ---------------------------------------------------------------------------------------------
 #pragma unroll
