@@ -257,8 +257,7 @@ __device__ __forceinline__ void delta_mma6(float (&d)[4], const uint32_t (&a)[3]
 }
 
 template <int DK>
-__global__ void __launch_bounds__(DELTA_PREP_THREADS, 3)
-delta_prep_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k, const DeltaParams p) {
+__device__ __forceinline__ void delta_prep(const CUtensorMap& map_q, const CUtensorMap& map_k, const DeltaParams& p) {
     using C = DeltaPrepCfg<DK>;
     extern __shared__ __align__(1024) uint8_t lin_smem[];    // (the loads' swizzle goes by the address)
     uint8_t* smem = lin_smem;
@@ -266,7 +265,6 @@ delta_prep_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_consta
     __shared__ float2 s_g[DELTA_C];
     __shared__ float s_beta[DELTA_C];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, c = lane & 3;
-    griddep_launch_dependents();
     if (blockIdx.x == 0 && tid == 0 && p.first_slot == 0) {
         p.hdr->tile_counter = 0u;
         p.hdr->error = 0u;
@@ -569,6 +567,15 @@ delta_prep_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_consta
         if (tid == 0) to->x.wild = wild ? 1 : 0;
     }
 }
+// Behind the first part of a batch it runs beside the second kernel of the part in front of it (in the workspace's other half): it reads nothing of that,
+// but ends after it, so that the kernel behind it, which waits for this one, finds the states.
+template <int DK>
+__global__ void __launch_bounds__(DELTA_PREP_THREADS, 3)
+delta_prep_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k, const DeltaParams p) {
+    griddep_launch_dependents();
+    delta_prep<DK>(map_q, map_k, p);
+    if (blockIdx.x == gridDim.x - 1) griddep_wait();
+}
 
 // ---------------------------------------------------------------------------------------------------------------------
 // The walk along the chunks.  Eight warps share a chunk's products and meet three times a chunk: when the state's copy, R and U are in shared
@@ -637,6 +644,7 @@ delta_chunks_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_cons
         mbar_fence_init();
     }
     griddep_wait();
+    griddep_launch_dependents();                             // (of the next part, whose first kernel may begin)
     if (!good && slice == 0 && h == 0 && tid == 0) report_error(p.hdr, 4u);      // MMV_ERR_BAD_SEGMENTS
     if (smem_u32(smem) & 1023u) {                            // (never: the declaration asks for it)
         if (tid == 0) report_error(p.hdr, 6u);               // MMV_ERR_CUDA

@@ -59,18 +59,26 @@ DeltaParams params_of(const mmv_delta_inputs* in, float scale, void* out) {
     return p;
 }
 
-// Places of chunks (delta_slot): all of them, and those that one pair of launches takes, whose operands the workspace holds.
-int64_t all_places(int64_t nseq, int64_t ntok) { return ntok / DELTA_C + nseq; }
+// Places of chunks (delta_slot): all of them, and those of one part, a pair of launches, whose operands the workspace holds.  A batch that is longer is taken in parts,
+// two of which the workspace holds then: the first kernel of a part runs beside the second one of the part in front of it.
+struct DeltaParts {
+    int64_t all, step;
+    int halves;
+};
 constexpr int64_t kPlaces = 9216;                            // (chunk, head)s: 196 MB
-int64_t places_at_once(const mmv_delta_inputs* in, int64_t nseq, int64_t ntok) {
-    const int64_t most = kPlaces / in->heads, all = all_places(nseq, ntok);
-    return all < most ? all : most;
+DeltaParts parts_of(const mmv_delta_inputs* in, int64_t nseq, int64_t ntok) {
+    const int64_t all = ntok / DELTA_C + nseq, most = kPlaces / in->heads;
+    // Few sequences: the chain of chunks takes its time on few CTAs, and the first kernels of small parts all but the first hide behind it.
+    const bool few = nseq * in->heads <= 64;
+    if (all <= (few ? most / 4 : most)) return {all, all, 1};
+    const int64_t step = few ? most / 4 : most / 2;
+    return {all, step < 1 ? 1 : step, 2};
 }
 
 template <int DK>
-mmv_status launch_delta(const CUtensorMap& q, const CUtensorMap& k, const DeltaParams& p, int64_t places, int nv, cudaStream_t st) {
+mmv_status launch_delta(const CUtensorMap& q, const CUtensorMap& k, const DeltaParams& p, int64_t places, bool beside, int nv, cudaStream_t st) {
     const unsigned prep = static_cast<unsigned>(places * (p.heads / p.group)), ctas = static_cast<unsigned>(static_cast<int64_t>(p.nseq) * p.heads * p.slices);
-    const mmv_status rc = launch(delta_prep_kernel<DK>, dim3(prep), DELTA_PREP_THREADS, DeltaPrepCfg<DK>::kSmemBytes, st, false, q, k, p);
+    const mmv_status rc = launch(delta_prep_kernel<DK>, dim3(prep), DELTA_PREP_THREADS, DeltaPrepCfg<DK>::kSmemBytes, st, beside, q, k, p);
     if (rc != MMV_OK) return rc;
     return nv == 16 ? launch(delta_chunks_kernel<DK, 16>, dim3(ctas), DELTA_THREADS, DeltaCfg<DK, 16>::kSmemBytes, st, true, q, k, p)
                     : launch(delta_chunks_kernel<DK, 32>, dim3(ctas), DELTA_THREADS, DeltaCfg<DK, 32>::kSmemBytes, st, true, q, k, p);
@@ -114,7 +122,8 @@ mmv_status mmv_gated_delta_step(const mmv_delta_inputs* in, int64_t nreq, float 
 
 size_t mmv_gated_delta_workspace_bytes(const mmv_delta_inputs* in, int64_t nseq, int64_t ntok) {
     if (nseq < 0 || nseq >= (1ll << 20) || ntok < 0 || ntok > INT32_MAX || check_inputs(in, ntok) != MMV_OK) return 0;
-    return round_up(sizeof(WorkspaceHeader) + static_cast<size_t>(places_at_once(in, nseq, ntok)) * in->heads * sizeof(DeltaChunk), 256);
+    const DeltaParts parts = parts_of(in, nseq, ntok);
+    return round_up(sizeof(WorkspaceHeader) + static_cast<size_t>(parts.step) * parts.halves * in->heads * sizeof(DeltaChunk), 256);
 }
 
 mmv_status mmv_gated_delta(const mmv_delta_inputs* in, const int32_t* offsets, int64_t nseq, int64_t ntok, float scale, const float* state,
@@ -138,7 +147,6 @@ mmv_status mmv_gated_delta(const mmv_delta_inputs* in, const int32_t* offsets, i
     p.nseq = static_cast<int>(nseq);
     p.ntok = static_cast<int>(ntok);
     p.hdr = static_cast<WorkspaceHeader*>(workspace);
-    p.chunks = static_cast<uint8_t*>(workspace) + sizeof(WorkspaceHeader);
     p.budget_ns = g_budget_ns.load();
     CUtensorMap map_q, map_k;
     if (!token_map(&map_q, in->q, in->dim_k, in->key_heads, ntok, in->q_stride_head, in->q_stride_token) ||
@@ -148,12 +156,14 @@ mmv_status mmv_gated_delta(const mmv_delta_inputs* in, const int32_t* offsets, i
     const int nv = nseq * p.heads * ((p.dv + 31) / 32) <= dev->sm_count / 2 ? 16 : 32;
     p.slices = (p.dv + nv - 1) / nv;
     if (nseq * p.heads > INT32_MAX / p.slices) return MMV_ERR_INVALID_ARG;       // one CTA per (sequence, head) and slice
-    const int64_t all = all_places(nseq, ntok), step = places_at_once(in, nseq, ntok);
-    for (int64_t at = 0; at < all; at += step) {
+    const DeltaParts parts = parts_of(in, nseq, ntok);
+    uint8_t* const chunks = static_cast<uint8_t*>(workspace) + sizeof(WorkspaceHeader);
+    for (int64_t at = 0, part = 0; at < parts.all; at += parts.step, ++part) {
         p.first_slot = at;
-        p.last_slot = at + step < all ? at + step : all;
+        p.last_slot = at + parts.step < parts.all ? at + parts.step : parts.all;
+        p.chunks = chunks + static_cast<size_t>(part & (parts.halves - 1)) * parts.step * p.heads * sizeof(DeltaChunk);
         const int64_t places = p.last_slot - at;
-        const mmv_status rc = in->dim_k <= 64 ? launch_delta<64>(map_q, map_k, p, places, nv, st) : launch_delta<128>(map_q, map_k, p, places, nv, st);
+        const mmv_status rc = in->dim_k <= 64 ? launch_delta<64>(map_q, map_k, p, places, at > 0, nv, st) : launch_delta<128>(map_q, map_k, p, places, at > 0, nv, st);
         if (rc != MMV_OK) return rc;
     }
     return MMV_OK;

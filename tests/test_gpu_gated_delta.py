@@ -195,6 +195,21 @@ def test_delta_in_parts(mmv, hk, rep, lens):
     check_delta(mmv, delta_case(1, lens, hk, rep, 16, 8))
 
 
+def test_delta_in_parts_back_to_back(mmv):
+    """Parts whose first kernels run beside the second ones in front of them, call after call in one workspace: always the same bits."""
+    q, k, v, off, g, beta, state = delta_case(2, [9000, 700], 1, 1, 64, 64, odd=False)
+    q2, k2, v2, off2, g2, beta2, state2 = delta_case(3, [150] * 20, 32, 2, 16, 24)
+    ws = torch.empty(220 << 20, dtype=torch.uint8, device="cuda")
+    want = mmv.gated_delta(q, k, v, ints(off), g, beta, state=state), mmv.gated_delta(q2, k2, v2, ints(off2), g2, beta2, state=state2)
+    torch.cuda.synchronize()
+    for _ in range(3):
+        got = (mmv.gated_delta(q, k, v, ints(off), g, beta, state=state, workspace=ws), mmv.gated_delta(q2, k2, v2, ints(off2), g2, beta2, state=state2, workspace=ws))
+        for a, b in zip(got, want):
+            assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
+    exact, bound, last, room = delta_plain(q, k, v, off, g, beta, 1.0, state)
+    inside(want[0][0], exact, U[q.dtype] * exact.abs() + bound)
+
+
 def test_delta_rows_outside_the_sequences(mmv):
     check_delta(mmv, delta_case(1, [70, 64, 3], 3, 1, 64, 64, first=37, behind=50))
 
