@@ -579,41 +579,41 @@ delta_prep_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_consta
 
 // ---------------------------------------------------------------------------------------------------------------------
 // The walk along the chunks.  Eight warps share a chunk's products and meet three times a chunk: when the state's copy, R and U are in shared
-// memory.  Slices of 32 columns leave room for two CTAs per SM: K and the scalars are two chunks deep, Q's place is filled again behind the
-// chunk's first products, T and A take turns in one.  Slices of 16 (where there are few CTAs) have all of the next chunk's operands on their way.
+// memory.  All of the next chunk's operands are on their way meanwhile (one CTA per SM; with Q, T and A loaded into the places that the chunk had
+// done with, two fit an SM: 750 instead of 860 us for 16 prompts of nearly one length, 1030 where one is three times as long as their mean, since
+// a chunk then takes 5.3 instead of 3.1 us).
 // ---------------------------------------------------------------------------------------------------------------------
 constexpr int DELTA_THREADS = 256;
 
 template <int DK, int NV>
 struct DeltaCfg {
-    static constexpr bool kDeep = NV == 16;                  // two of everything
-    static constexpr int kTile = DELTA_C * DK * 2, kBlocks = DELTA_TILES * 2 * 512;
+    static constexpr int kTile = DELTA_C * DK * 2, kBlocks = 2 * DELTA_TILES * 512;
     static constexpr int kPitch = NV * 2;                    // bytes of a row of NV bfloat16
-    static constexpr int kK = 0, kQ = 2 * kTile, kT = kQ + (kDeep ? 2 : 1) * kTile;          // T, A or both in turn
-    static constexpr int kX = kT + (kDeep ? 4 : 1) * kBlocks, kXPitch = 1024;    // the scalars
-    static constexpr int kS = kX + 2 * kXPitch, kSPart = DK * kPitch;            // the state, three parts
-    // R: three parts, two where a third would not leave room for two CTAs per SM (keys of more than 64 columns overlap less, and T - 1 is smaller)
-    static constexpr int kRParts = DK == 64 || kDeep ? 3 : 2;
-    static constexpr int kR = kS + 3 * kSPart, kRPart = DELTA_C * kPitch;
-    static constexpr int kU = kR + kRParts * kRPart;                             // two
+    // what is loaded for a chunk, twice: K, Q, T - 1 and A, the scalars
+    static constexpr int kK = 0, kQ = kTile, kT = 2 * kTile, kX = kT + 2 * kBlocks, kStage = kX + 1024;
+    static constexpr uint32_t kLoad = 2 * kTile + 2 * kBlocks + sizeof(DeltaScalars);
+    static constexpr int kS = 2 * kStage, kSPart = DK * kPitch;                  // the state, three parts
+    static constexpr int kR = kS + 3 * kSPart, kRPart = DELTA_C * kPitch;        // three
+    static constexpr int kU = kR + 3 * kRPart;                                   // two
     static constexpr int kW = kU + 2 * kRPart;                                   // exp(G_n - G) U, three
     static constexpr int kSmemBytes = kW + 3 * kRPart;
-    static_assert(4 * NV * 4 <= 2 * kRPart, "token by token: sums in R's place");
+    static_assert(kStage % 1024 == 0 && sizeof(DeltaScalars) <= 1024, "the loads' swizzle goes by the address");
+    static_assert(4 * NV * 4 <= 3 * kRPart, "token by token: sums in R's place");
 };
 // Where word w of a row lies: eight rows' words of one column in different banks.
 template <int NV>
 __device__ __forceinline__ int delta_place(int row, int w) { return row * (NV * 2) + ((NV == 32 ? w ^ ((row >> 1) & 3) : w ^ ((row >> 2) & 1)) << 4); }
 
 template <int DK, int NV>
-__global__ void __launch_bounds__(DELTA_THREADS, DeltaCfg<DK, NV>::kDeep ? 1 : 2)
+__global__ void __launch_bounds__(DELTA_THREADS, 1)
 delta_chunks_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k, const DeltaParams p) {
     using C = DeltaCfg<DK, NV>;
     constexpr int N = NV / 16;                               // product tiles of 8 columns of a warp: half of the slice
     constexpr int M = DK / 64;                               // and of 16 rows of the state
     extern __shared__ __align__(1024) uint8_t lin_smem[];    // (the loads' swizzle goes by the address)
     uint8_t* smem = lin_smem;
-    __shared__ uint64_t s_k[2], s_q, s_t;                    // loads that have landed
-    __shared__ int s_late, s_seq;
+    __shared__ uint64_t s_full[2];                           // loads that have landed
+    __shared__ int s_seq;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, c = lane & 3;
     const int slice = static_cast<int>(blockIdx.x % p.slices), h = static_cast<int>(blockIdx.x / p.slices % p.heads);
     const int hk = h / p.group, col0 = slice * NV;
@@ -636,11 +636,8 @@ delta_chunks_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_cons
     const int begin = static_cast<int>(max(0ll, min(static_cast<long long>(chunks), p.first_slot - slot0)));
     const int end = static_cast<int>(max(0ll, min(static_cast<long long>(chunks), p.last_slot - slot0)));
     if (tid == 0) {
-        s_late = 0;
-        mbar_init(&s_k[0], 1);
-        mbar_init(&s_k[1], 1);
-        mbar_init(&s_q, 1);
-        mbar_init(&s_t, 1);
+        mbar_init(&s_full[0], 1);
+        mbar_init(&s_full[1], 1);
         mbar_fence_init();
     }
     griddep_wait();
@@ -655,45 +652,20 @@ delta_chunks_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_cons
 
     const uint32_t sm = smem_u32(smem);
     const DeltaChunk* made = reinterpret_cast<const DeltaChunk*>(p.chunks) + (slot0 - p.first_slot) * p.heads + h;       // of chunk i: made[i * heads]
-    // ---- loads, each by one thread of another warp ---------------------------------------------------------------------------------
-    const auto load_keys = [&](int chunk) {                  // (kDeep: and all the rest)
+    const auto fetch = [&](int chunk) {                      // (one thread)
         const int i = (chunk - begin) & 1;
+        uint8_t* dst = smem + i * C::kStage;
         const DeltaChunk* from = made + static_cast<long long>(chunk) * p.heads;
-        mbar_arrive_expect_tx(&s_k[i], (C::kDeep ? 2 * C::kTile + 2 * C::kBlocks : C::kTile) + sizeof(DeltaScalars));
+        mbar_arrive_expect_tx(&s_full[i], C::kLoad);
 #pragma unroll
         for (int b = 0; b < DK / 64; ++b) {
-            tma_load_3d(smem + C::kK + i * C::kTile + b * DELTA_BOX, &map_k, &s_k[i], b * 64, hk, tok + chunk * DELTA_C);
-            if (C::kDeep) tma_load_3d(smem + C::kQ + i * C::kTile + b * DELTA_BOX, &map_q, &s_k[i], b * 64, hk, tok + chunk * DELTA_C);
+            tma_load_3d(dst + C::kK + b * DELTA_BOX, &map_k, &s_full[i], b * 64, hk, tok + chunk * DELTA_C);
+            tma_load_3d(dst + C::kQ + b * DELTA_BOX, &map_q, &s_full[i], b * 64, hk, tok + chunk * DELTA_C);
         }
-        tma_load_1d(smem + C::kX + i * C::kXPitch, &from->x, sizeof(DeltaScalars), &s_k[i]);
-        if (C::kDeep) tma_load_1d(smem + C::kT + i * 2 * C::kBlocks, from->t, 2 * C::kBlocks, &s_k[i]);
+        tma_load_1d(dst + C::kX, &from->x, sizeof(DeltaScalars), &s_full[i]);
+        tma_load_1d(dst + C::kT, from->t, 2 * C::kBlocks, &s_full[i]);
     };
-    const auto load_queries = [&](int chunk) {
-        mbar_arrive_expect_tx(&s_q, C::kTile);
-#pragma unroll
-        for (int b = 0; b < DK / 64; ++b) tma_load_3d(smem + C::kQ + b * DELTA_BOX, &map_q, &s_q, b * 64, hk, tok + chunk * DELTA_C);
-    };
-    const auto load_blocks = [&](const void* from) {
-        mbar_arrive_expect_tx(&s_t, C::kBlocks);
-        tma_load_1d(smem + C::kT, from, C::kBlocks, &s_t);
-    };
-    if (begin < end && tid == 0) {
-        load_keys(begin);
-        if (!C::kDeep) {
-            load_queries(begin);
-            load_blocks(made[static_cast<long long>(begin) * p.heads].t);
-        }
-    }
-    // A load did not land in time: those in flight do before the CTA leaves.
-    const auto given_up = [&](int chunk) {
-        if (tid != 0) return;
-        report_error(p.hdr, 5u);                             // MMV_ERR_TIMEOUT
-        for (int i = 0; i < 2; ++i)
-            for (int parity = 0; parity < 2; ++parity) {
-                mbar_wait(&s_k[i], parity, 1000000);
-                mbar_wait(i ? &s_q : &s_t, parity, 1000000);
-            }
-    };
+    if (begin < end && tid == 0) fetch(begin);
 
     // Of the tokens a warp has 16 (two warps of a scheduler together five of the triangles' blocks), of the state 16 M rows; of both, half of the
     // slice's columns.
@@ -747,12 +719,11 @@ delta_chunks_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_cons
         }
     };
     const auto address = [&](int matrix, int row, int j) { return smem + matrix + delta_place<NV>(row, half * N + j) + 4 * c; };
-    bool late = false;
     for (int chunk = begin; chunk < end; ++chunk) {
         const int stage = (chunk - begin) & 1;
-        const uint32_t sm_k = sm + C::kK + stage * C::kTile, sm_q = sm + C::kQ + (C::kDeep ? stage * C::kTile : 0);
-        const uint4* blocks = reinterpret_cast<const uint4*>(smem + C::kT + (C::kDeep ? stage * 2 * C::kBlocks : 0));       // T, then (kDeep: behind it) A
-        const DeltaScalars* info = reinterpret_cast<const DeltaScalars*>(smem + C::kX + stage * C::kXPitch);
+        const uint32_t sm_k = sm + stage * C::kStage + C::kK, sm_q = sm + stage * C::kStage + C::kQ;
+        const uint4* blocks = reinterpret_cast<const uint4*>(smem + stage * C::kStage + C::kT) + lane;           // T - 1, and A behind it
+        const DeltaScalars* info = reinterpret_cast<const DeltaScalars*>(smem + stage * C::kStage + C::kX);
         const int n = min(DELTA_C, len - chunk * DELTA_C);
         // the state's copy for the products
 #pragma unroll
@@ -767,19 +738,20 @@ delta_chunks_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_cons
 #pragma unroll
                     for (int part = 0; part < 3; ++part) *reinterpret_cast<uint32_t*>(at + part * C::kSPart) = r[part];
                 }
-        late |= !mbar_wait(&s_k[stage], ((chunk - begin) >> 1) & 1, p.budget_ns);
-        if (!C::kDeep) late |= !mbar_wait(&s_q, (chunk - begin) & 1, p.budget_ns);
+        const bool late = !mbar_wait(&s_full[stage], ((chunk - begin) >> 1) & 1, p.budget_ns);
         if (n < DELTA_C && !late) {                          // another sequence's keys: their weights of zero do not hide what is not finite
             for (int i = tid; i < (DELTA_C - n) * (DK / 8); i += DELTA_THREADS)
-                *reinterpret_cast<uint4*>(smem + C::kK + stage * C::kTile + delta_word(n + i / (DK / 8), i % (DK / 8))) = make_uint4(0u, 0u, 0u, 0u);
+                *reinterpret_cast<uint4*>(smem + stage * C::kStage + C::kK + delta_word(n + i / (DK / 8), i % (DK / 8))) = make_uint4(0u, 0u, 0u, 0u);
             fence_proxy_async_smem();
         }
         if (__syncthreads_or(late)) {                        // (this chunk's operands and the state's copy are there)
-            given_up(chunk);
+            if (tid == 0) {
+                report_error(p.hdr, 5u);                     // MMV_ERR_TIMEOUT
+                mbar_wait(&s_full[stage], ((chunk - begin) >> 1) & 1, 1000000);               // (the loads in flight land before the CTA leaves)
+            }
             return;
         }
-        if (chunk + 1 < end && tid == 0) load_keys(chunk + 1);
-        if (!C::kDeep && chunk > begin && tid == 64) load_blocks(made[static_cast<long long>(chunk) * p.heads].t);
+        if (tid == 0 && chunk + 1 < end) fetch(chunk + 1);
 
         // ---- K S, Q S: 16 tokens each ------------------------------------------------------------------------------------------------
         float x[N][4], y[N][4];
@@ -831,25 +803,19 @@ delta_chunks_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_cons
                     x[j][2 * e] = on ? beta[e] * (w.x - past[e] * x[j][2 * e]) : 0.f;
                     x[j][2 * e + 1] = on ? beta[e] * (w.y - past[e] * x[j][2 * e + 1]) : 0.f;
                     uint32_t r[3];
-                    if (C::kRParts == 3) delta_split3(x[j][2 * e], x[j][2 * e + 1], r);
-                    else delta_split(x[j][2 * e], x[j][2 * e + 1], r[0], r[1]);
+                    delta_split3(x[j][2 * e], x[j][2 * e + 1], r);
                     uint8_t* at = address(C::kR, row, j);
 #pragma unroll
-                    for (int part = 0; part < C::kRParts; ++part) *reinterpret_cast<uint32_t*>(at + part * C::kRPart) = r[part];
+                    for (int part = 0; part < 3; ++part) *reinterpret_cast<uint32_t*>(at + part * C::kRPart) = r[part];
                 }
         }
         if (chunk + 1 < end) values(chunk + 1);
-        if (!C::kDeep && !mbar_wait(&s_t, 0, p.budget_ns)) { // (T and A take turns: T's loads complete its even phases)
-            *const_cast<volatile int*>(&s_late) = 1;
-            wild = true;
-        }
         wild = __syncthreads_or(wild);
-        if (!C::kDeep && chunk + 1 < end && tid == 128) load_queries(chunk + 1);
         uint16_t* out = p.out + ((static_cast<long long>(tok) + chunk * DELTA_C) * p.heads + h) * p.dv;
         const long long orow = static_cast<long long>(p.heads) * p.dv;
         if (!wild) {
             // ---- U = R + (T - 1) R ---------------------------------------------------------------------------------------------------------
-            const uint4* solver = blocks + delta_tile(block, 0) * 32 + lane;
+            const uint4* solver = blocks + delta_tile(block, 0) * 32;
             float u[N][4], z[N][4];                          // (sums of their own: the tensor core's cut digits at the end, and R's are not to be cut)
 #pragma unroll
             for (int j = 0; j < N; ++j)
@@ -861,12 +827,12 @@ delta_chunks_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_cons
                 const uint4 th = solver[k * 32], tl = solver[(DELTA_TILES + k) * 32];
                 const uint32_t ah[4] = {th.x, th.y, th.z, th.w}, al[4] = {tl.x, tl.y, tl.z, tl.w};
                 uint32_t b3[N][2];
-                if (C::kRParts == 3) third(b3, C::kR + 2 * C::kRPart, k * 16);
+                third(b3, C::kR + 2 * C::kRPart, k * 16);
 #pragma unroll
                 for (int j = 0; j < N; ++j) {
                     uint32_t b[4];
                     operand(b, C::kR, C::kRPart, k * 16, j);
-                    if (C::kRParts == 3) mma_16816<true>(z[j], ah, b3[j][0], b3[j][1]);
+                    mma_16816<true>(z[j], ah, b3[j][0], b3[j][1]);
                     mma_16816<true>(u[j], ah, b[0], b[1]);
                     mma_16816<true>(z[j], al, b[2], b[3]);
                     mma_16816<true>(z[j], al, b[0], b[1]);
@@ -890,7 +856,6 @@ delta_chunks_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_cons
                     for (int part = 0; part < 3; ++part) *reinterpret_cast<uint32_t*>(at + part * C::kRPart) = r[part];
                 }
             __syncthreads();
-            if (!C::kDeep && tid == 192) load_blocks(made[static_cast<long long>(chunk) * p.heads].a);
             // ---- S' = exp(G_n) S + K^T (exp(G_n - G) U) -----------------------------------------------------------------------------------
             {
                 uint32_t a[2][M][4], b[2][N][4], b3[2][N][2];
@@ -940,8 +905,7 @@ delta_chunks_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_cons
             for (int j = 0; j < N; ++j)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) y[j][e] *= past[e >> 1];
-            if (!C::kDeep) late |= !mbar_wait(&s_t, 1, p.budget_ns);             // (A's complete the odd ones)
-            const uint4* scores = blocks + (C::kDeep ? 2 * DELTA_TILES * 32 : 0) + delta_tile(block, 0) * 32 + lane;
+            const uint4* scores = blocks + (2 * DELTA_TILES + delta_tile(block, 0)) * 32;
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
                 if (k > block) break;
@@ -963,14 +927,6 @@ delta_chunks_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_cons
                         *reinterpret_cast<uint32_t*>(out + row * orow + mine + j * 8 + 2 * c) = pack_pair<true>(p.scale * y[j][2 * e], p.scale * y[j][2 * e + 1]);
                 }
         } else {
-            if (*const_cast<volatile int*>(&s_late)) {
-                given_up(chunk);
-                return;
-            }
-            if (!C::kDeep && tid == 192) {                   // (not used, but its turn)
-                load_blocks(made[static_cast<long long>(chunk) * p.heads].a);
-                late |= !mbar_wait(&s_t, 1, p.budget_ns);
-            }
             // ---- token by token: the recurrence as it stands ---------------------------------------------------
             float* sums = reinterpret_cast<float*>(smem + C::kR);
             constexpr int PARTS = 4;                         // of the state's rows: warps of one half
@@ -1040,7 +996,6 @@ delta_chunks_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_cons
             }
         }
     }
-    if (late) report_error(p.hdr, 5u);                       // MMV_ERR_TIMEOUT
 #pragma unroll
     for (int m = 0; m < M; ++m)
 #pragma unroll
