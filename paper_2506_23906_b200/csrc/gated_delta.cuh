@@ -31,6 +31,7 @@ struct DeltaParams {
     int nseq, ntok;
     long long first_slot, last_slot;                         // chunks that this launch takes, by their place in the workspace
     int slices;                                              // column parts of a (sequence, head)
+    int present;                                             // sequences that a launch of the second kernel has CTAs for
     WorkspaceHeader* hdr;
     uint8_t* chunks;                                         // [last_slot - first_slot][heads] DeltaChunk
     uint64_t budget_ns;                                      // bound of every wait
@@ -604,6 +605,44 @@ struct DeltaCfg {
 template <int NV>
 __device__ __forceinline__ int delta_place(int row, int w) { return row * (NV * 2) + ((NV == 32 ? w ^ ((row >> 1) & 3) : w ^ ((row >> 2) & 1)) << 4); }
 
+// Which sequence the index-th CTAs of a launch take, and its chunks [begin, end) that the launch has the operands of.  The sequences that lie in the part
+// [first_slot, last_slot) of the places follow one another, `present` of them at most; the ones with the most tokens in it come first (16 of 32768 tokens in all:
+// a last wave of half of the time) where a thread can look at each.  (With CTAs for every sequence in every part, 256 prompts of 512 tokens and 32 heads took
+// 18.7 instead of 9.3 ms.  Out of line: in the kernel it cost the chunks' loop 2 %.)
+struct DeltaPart {
+    int seq, tok, len, begin, end;                           // seq -1: none
+};
+__device__ __forceinline__ bool delta_part_of(const int32_t* offsets, int ntok, long long first_slot, long long last_slot, DeltaPart& r) {
+    lin_sequence(offsets, ntok, r.seq, r.tok, r.len);
+    const long long at = delta_slot(r.tok, r.seq), chunks = lin_chunks(r.len);
+    r.begin = static_cast<int>(max(0ll, min(chunks, first_slot - at)));
+    r.end = static_cast<int>(max(0ll, min(chunks, last_slot - at)));
+    return r.begin < r.end || (chunks == 0 && at >= first_slot && at < last_slot);       // (an empty sequence's state is copied where its place is)
+}
+static __device__ __noinline__ DeltaPart delta_part(const int32_t* offsets, int ntok, int nseq, int present, long long first_slot, long long last_slot,
+                                                    int index, int* s_len /* DELTA_THREADS + 1 */) {
+    const int tid = threadIdx.x, first = present < nseq && first_slot ? delta_sequence_of(offsets, nseq, first_slot) : 0;
+    DeltaPart r{};
+    r.seq = first + index;
+    bool here = r.seq < nseq;
+    if (present <= DELTA_THREADS) {
+        DeltaPart x{};
+        x.seq = first + tid;
+        const int n = tid < present && x.seq < nseq && delta_part_of(offsets, ntok, first_slot, last_slot, x) ? min(x.len - x.begin * DELTA_C, (x.end - x.begin) * DELTA_C) : -1;
+        s_len[tid] = n;
+        here = __syncthreads_count(n >= 0) > index;
+        if (here) {
+            int rank = 0;
+            for (int i = 0; i < present; ++i) rank += s_len[i] > n || (s_len[i] == n && i < tid);
+            if (n >= 0 && rank == index) s_len[DELTA_THREADS] = x.seq;
+            __syncthreads();
+            r.seq = s_len[DELTA_THREADS];
+        }
+    }
+    if (!here || !delta_part_of(offsets, ntok, first_slot, last_slot, r)) r.seq = -1;
+    return r;
+}
+
 template <int DK, int NV>
 __global__ void __launch_bounds__(DELTA_THREADS, 1)
 delta_chunks_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k, const DeltaParams p) {
@@ -613,28 +652,25 @@ delta_chunks_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_cons
     extern __shared__ __align__(1024) uint8_t lin_smem[];    // (the loads' swizzle goes by the address)
     uint8_t* smem = lin_smem;
     __shared__ uint64_t s_full[2];                           // loads that have landed
-    __shared__ int s_seq;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, c = lane & 3;
     const int slice = static_cast<int>(blockIdx.x % p.slices), h = static_cast<int>(blockIdx.x / p.slices % p.heads);
     const int hk = h / p.group, col0 = slice * NV;
-    int seq = static_cast<int>(blockIdx.x / p.slices / p.heads), tok, len;
-    if (p.nseq <= DELTA_THREADS) {                           // the longest sequences first (16 of 32768 tokens in all: a last wave of half of the time)
-        int* s_len = reinterpret_cast<int*>(smem + C::kS);
-        lin_sequence(p.offsets, p.ntok, min(tid, p.nseq - 1), tok, len);
-        s_len[tid] = tid < p.nseq ? len : -1;
-        __syncthreads();
-        int rank = 0;
-        for (int i = 0; i < p.nseq; ++i) rank += s_len[i] > len || (s_len[i] == len && i < tid);
-        if (tid < p.nseq && rank == seq) s_seq = tid;
-        __syncthreads();
-        seq = s_seq;
+    const int index = static_cast<int>(blockIdx.x / p.slices / p.heads);
+    bool bad = false;
+    if (p.first_slot == 0) {
+        for (long long i = static_cast<long long>(blockIdx.x) * DELTA_THREADS + tid; i < p.nseq; i += static_cast<long long>(gridDim.x) * DELTA_THREADS) {
+            int at, n;
+            bad |= !lin_sequence(p.offsets, p.ntok, static_cast<int>(i), at, n);
+        }
     }
-    const bool good = lin_sequence(p.offsets, p.ntok, seq, tok, len);
-    const int chunks = (len + DELTA_C - 1) / DELTA_C;
+    const DeltaPart part = delta_part(p.offsets, p.ntok, p.nseq, p.present, p.first_slot, p.last_slot, index, reinterpret_cast<int*>(smem + C::kS));
+    if (part.seq < 0) {                                      // (the launch ends behind the one in front of it all the same)
+        if (bad || blockIdx.x == 0) griddep_wait();
+        if (bad) report_error(p.hdr, 4u);                    // MMV_ERR_BAD_SEGMENTS
+        return;
+    }
+    const int seq = part.seq, tok = part.tok, len = part.len, begin = part.begin, end = part.end;
     const long long slot0 = delta_slot(tok, seq);
-    // the chunks that this launch has the operands of
-    const int begin = static_cast<int>(max(0ll, min(static_cast<long long>(chunks), p.first_slot - slot0)));
-    const int end = static_cast<int>(max(0ll, min(static_cast<long long>(chunks), p.last_slot - slot0)));
     if (tid == 0) {
         mbar_init(&s_full[0], 1);
         mbar_init(&s_full[1], 1);
@@ -642,12 +678,11 @@ delta_chunks_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_cons
     }
     griddep_wait();
     griddep_launch_dependents();                             // (of the next part, whose first kernel may begin)
-    if (!good && slice == 0 && h == 0 && tid == 0) report_error(p.hdr, 4u);      // MMV_ERR_BAD_SEGMENTS
+    if (bad) report_error(p.hdr, 4u);                        // MMV_ERR_BAD_SEGMENTS
     if (smem_u32(smem) & 1023u) {                            // (never: the declaration asks for it)
         if (tid == 0) report_error(p.hdr, 6u);               // MMV_ERR_CUDA
         return;
     }
-    if (begin >= end && !(chunks == 0 && p.first_slot == 0)) return;
     __syncthreads();
 
     const uint32_t sm = smem_u32(smem);

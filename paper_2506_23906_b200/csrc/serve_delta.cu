@@ -66,6 +66,7 @@ struct DeltaParts {
     int halves;
 };
 constexpr int64_t kPlaces = 9216;                            // (chunk, head)s: 196 MB
+constexpr int64_t kMostTokens = INT32_MAX - DELTA_C;         // (positions past a chunk's end stay within 32 bits)
 DeltaParts parts_of(const mmv_delta_inputs* in, int64_t nseq, int64_t ntok) {
     const int64_t all = ntok / DELTA_C + nseq, most = kPlaces / in->heads;
     // Few sequences: the chain of chunks takes its time on few CTAs, and the first kernels of small parts all but the first hide behind it.
@@ -77,7 +78,7 @@ DeltaParts parts_of(const mmv_delta_inputs* in, int64_t nseq, int64_t ntok) {
 
 template <int DK>
 mmv_status launch_delta(const CUtensorMap& q, const CUtensorMap& k, const DeltaParams& p, int64_t places, bool beside, int nv, cudaStream_t st) {
-    const unsigned prep = static_cast<unsigned>(places * (p.heads / p.group)), ctas = static_cast<unsigned>(static_cast<int64_t>(p.nseq) * p.heads * p.slices);
+    const unsigned prep = static_cast<unsigned>(places * (p.heads / p.group)), ctas = static_cast<unsigned>(static_cast<int64_t>(p.present) * p.heads * p.slices);
     const mmv_status rc = launch(delta_prep_kernel<DK>, dim3(prep), DELTA_PREP_THREADS, DeltaPrepCfg<DK>::kSmemBytes, st, beside, q, k, p);
     if (rc != MMV_OK) return rc;
     return nv == 16 ? launch(delta_chunks_kernel<DK, 16>, dim3(ctas), DELTA_THREADS, DeltaCfg<DK, 16>::kSmemBytes, st, true, q, k, p)
@@ -121,14 +122,14 @@ mmv_status mmv_gated_delta_step(const mmv_delta_inputs* in, int64_t nreq, float 
 }
 
 size_t mmv_gated_delta_workspace_bytes(const mmv_delta_inputs* in, int64_t nseq, int64_t ntok) {
-    if (nseq < 0 || nseq >= (1ll << 20) || ntok < 0 || ntok > INT32_MAX || check_inputs(in, ntok) != MMV_OK) return 0;
+    if (nseq < 0 || nseq >= (1ll << 20) || ntok < 0 || ntok > kMostTokens || check_inputs(in, ntok) != MMV_OK) return 0;
     const DeltaParts parts = parts_of(in, nseq, ntok);
     return round_up(sizeof(WorkspaceHeader) + static_cast<size_t>(parts.step) * parts.halves * in->heads * sizeof(DeltaChunk), 256);
 }
 
 mmv_status mmv_gated_delta(const mmv_delta_inputs* in, const int32_t* offsets, int64_t nseq, int64_t ntok, float scale, const float* state,
                            float* state_out, void* out, void* workspace, size_t workspace_bytes, void* cuda_stream) {
-    if (nseq < 0 || nseq >= (1ll << 20) || ntok < 0 || ntok > INT32_MAX || check_inputs(in, ntok) != MMV_OK || in->dtype != MMV_BF16_TO_F32)
+    if (nseq < 0 || nseq >= (1ll << 20) || ntok < 0 || ntok > kMostTokens || check_inputs(in, ntok) != MMV_OK || in->dtype != MMV_BF16_TO_F32)
         return MMV_ERR_INVALID_ARG;
     if (!workspace || !aligned(workspace, 256)) return MMV_ERR_INVALID_ARG;
     if (nseq && (!offsets || !aligned(offsets, 4) || !state_out || !aligned(state_out, 16) || (state && !aligned(state, 16)))) return MMV_ERR_INVALID_ARG;
@@ -163,6 +164,8 @@ mmv_status mmv_gated_delta(const mmv_delta_inputs* in, const int32_t* offsets, i
         p.last_slot = at + parts.step < parts.all ? at + parts.step : parts.all;
         p.chunks = chunks + static_cast<size_t>(part & (parts.halves - 1)) * parts.step * p.heads * sizeof(DeltaChunk);
         const int64_t places = p.last_slot - at;
+        // (a sequence has a place of its own at least, and one may reach in from the part in front)
+        p.present = static_cast<int>(nseq < places + 1 ? nseq : places + 1);
         const mmv_status rc = in->dim_k <= 64 ? launch_delta<64>(map_q, map_k, p, places, at > 0, nv, st) : launch_delta<128>(map_q, map_k, p, places, at > 0, nv, st);
         if (rc != MMV_OK) return rc;
     }

@@ -65,6 +65,15 @@ def test_gated_delta(lib):
     assert lib.mmv_gated_delta_workspace_bytes(i, 1, 1 << 30) <= 200 << 20                                 # (taken in parts)
 
 
+def test_most_tokens(lib):
+    """Positions past the last chunk's end are 32-bit numbers too."""
+    i = ctypes.byref(inputs())
+    most = (1 << 31) - 1 - 64
+    need = lib.mmv_gated_delta_workspace_bytes(i, 2, most)
+    assert need >= 256 and lib.mmv_gated_delta_workspace_bytes(i, 2, most + 1) == 0
+    assert lib.mmv_gated_delta(i, 16, 2, most + 1, 1.0, 1 << 25, 1 << 26, 16, 256, need, None) == INVALID
+
+
 def test_states_that_overlap_in_part(lib):
     i, size = ctypes.byref(inputs()), 4 * 5 * 4 * 64 * 64
     need = lib.mmv_gated_delta_workspace_bytes(i, 5, 70)

@@ -195,6 +195,23 @@ def test_delta_in_parts(mmv, hk, rep, lens):
     check_delta(mmv, delta_case(1, lens, hk, rep, 16, 8))
 
 
+@pytest.mark.parametrize("hk,rep,count,most,first,behind", [(8, 1, 300, 400, 0, 0), (32, 2, 400, 100, 37, 3000), (256, 4, 9, 150, 0, 900), (64, 1, 200, 3, 5, 64)])
+def test_delta_many_sequences_in_parts(mmv, hk, rep, count, most, first, behind):
+    """A part's launches have CTAs for the sequences that may lie in it alone; empty sequences, parts without one, rows around them.  The bits are those of
+    the sequences a few at a time."""
+    lens = torch.randint(0, most + 1, (count,), generator=torch.Generator().manual_seed(count)).tolist()
+    q, k, v, off, g, beta, state = delta_case(count, lens, hk, rep, 16, 8, first=first, behind=behind)
+    out = torch.full((v.shape[0], hk * rep, 8), 7.0, dtype=q.dtype, device="cuda")
+    last = mmv.gated_delta(q, k, v, ints(off), g, beta, state=state, out=out)[1]
+    assert (out[:off[0]] == 7).all() and (out[off[-1]:] == 7).all()
+    group = 40 if hk * rep < 64 else 4 if hk * rep < 1024 else 1
+    for i in range(0, count, group):
+        j = min(count, i + group)
+        a, b = off[i], off[j]
+        o, s = mmv.gated_delta(q[a:b], k[a:b], v[a:b], ints([x - a for x in off[i:j + 1]]), g[a:b], beta[a:b], state=state[i:j])
+        assert torch.equal(o, out[a:b]) and torch.equal(s, last[i:j])
+
+
 def test_delta_in_parts_back_to_back(mmv):
     """Parts whose first kernels run beside the second ones in front of them, call after call in one workspace: always the same bits."""
     q, k, v, off, g, beta, state = delta_case(2, [9000, 700], 1, 1, 64, 64, odd=False)
