@@ -477,7 +477,7 @@ mmv_status mmv_paged_attention(const void *q, int64_t q_stride_request, int64_t 
  * and the same of the values.  code: MMV_CODE_INT8 (-127 to 127) or
  * MMV_CODE_E4M3 (finite up to 448).  Any order of the axes; dim is a multiple of
  * 16 up to 256, the codes' strides are multiples of 16 and k, v 16-byte aligned;
- * the scales are fp32, >= 0, any strides.
+ * the scales are fp32, >= 0, any strides; block_size is below 2^27 - 128.
  */
 typedef enum { MMV_CODE_INT8 = 0, MMV_CODE_E4M3 = 1 } mmv_code;
 typedef struct {

@@ -36,6 +36,7 @@ mmv_status check_cache(const mmv_kv_cache_q8* c) {
     if (!c || (c->code != MMV_CODE_INT8 && c->code != MMV_CODE_E4M3)) return MMV_ERR_INVALID_ARG;
     if (c->num_blocks < 0 || c->num_blocks > INT32_MAX || c->block_size < 1 || c->heads < 1 || c->heads > kMaxHeads) return MMV_ERR_INVALID_ARG;
     if (c->dim < 16 || c->dim > 256 || c->dim % 16) return MMV_ERR_INVALID_ARG;
+    if (c->block_size > INT32_MAX / 16 - Q8_THREADS) return MMV_ERR_INVALID_ARG;             // (words of a block's rows are counted in 32 bits)
     if (!word_stride(c->stride_block, c->num_blocks, 16) || !word_stride(c->stride_token, c->block_size, 16) || !word_stride(c->stride_head, c->heads, 16))
         return MMV_ERR_INVALID_ARG;
     if (c->num_blocks && (!c->k || !c->v || !aligned(c->k, 16) || !aligned(c->v, 16))) return MMV_ERR_INVALID_ARG;

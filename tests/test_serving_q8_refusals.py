@@ -43,7 +43,7 @@ ATTEND = [16, 256, 64, 4, BF16, None, 16, 8, 8, 16, 3, 1.0, 0, 16, 16, 256, 1 <<
 
 
 @pytest.mark.parametrize("change", [
-    dict(code=2), dict(code=-1), dict(num_blocks=-1), dict(num_blocks=1 << 31), dict(block_size=0), dict(heads=0), dict(heads=1025), dict(dim=0), dict(dim=8),
+    dict(code=2), dict(code=-1), dict(num_blocks=-1), dict(num_blocks=1 << 31), dict(block_size=0), dict(block_size=1 << 27), dict(heads=0), dict(heads=1025), dict(dim=0), dict(dim=8),
     dict(dim=72), dict(dim=272), dict(stride_block=1000), dict(stride_token=136), dict(stride_head=60), dict(k=None), dict(v=None), dict(k=(1 << 20) + 8),
     dict(v=(1 << 24) + 2), dict(k_scale=None), dict(v_scale=None), dict(k_scale=(1 << 26) + 2), dict(v_scale=(1 << 27) + 1)])
 def test_caches(lib, change):
