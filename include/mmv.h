@@ -646,7 +646,7 @@ mmv_status mmv_gated_delta_step(const mmv_delta_inputs *in, int64_t nreq, float 
  * are held to 2^-17 of themselves, states in fp32.  Offsets that decrease or leave [0, ntok] are reported as
  * MMV_ERR_BAD_SEGMENTS in the workspace; nothing outside the buffers is touched.
  * ntok < 2^31 - 64, nseq < 2^20.  Workspace: mmv_gated_delta_workspace_bytes(in, nseq, ntok), 256-byte
- * aligned: 21 KB per chunk of 64 tokens and head, 196 MB at most (longer batches are taken in parts).
+ * aligned: 21 KB per chunk of 64 tokens and head, 784 MB at most (longer batches are taken in parts).
  */
 size_t mmv_gated_delta_workspace_bytes(const mmv_delta_inputs *in, int64_t nseq, int64_t ntok);
 mmv_status mmv_gated_delta(const mmv_delta_inputs *in, const int32_t *offsets, int64_t nseq, int64_t ntok, float scale,

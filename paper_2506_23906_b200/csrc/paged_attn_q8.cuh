@@ -33,7 +33,7 @@ struct PagedQ8Params : PagedParams {                         // (k and v of the 
     const float *ks, *vs;
     long long s_block, s_head;
     uint32_t by_block;                                       // floor(2^32 / block_size)
-    int side;                                                // key heads side by side: 1, 2 or 4
+    int side;                                                // key heads side by side: 1 or 2
     int tile, groups;                                        // tokens of a unit: 128 / side; groups of key heads, times parts
     uint64_t budget_ns;                                      // bound of every wait
     float* part_m2;                                          // [grid][2][side][PA_ROWS]: maximum of the values' weights (less LIFT)

@@ -65,14 +65,17 @@ struct DeltaParts {
     int64_t all, step;
     int halves;
 };
-constexpr int64_t kPlaces = 9216;                            // (chunk, head)s: 196 MB
+constexpr int64_t kPlaces = 36864;                           // (chunk, head)s: 784 MB
 constexpr int64_t kMostTokens = INT32_MAX - DELTA_C;         // (positions past a chunk's end stay within 32 bits)
 DeltaParts parts_of(const mmv_delta_inputs* in, int64_t nseq, int64_t ntok) {
     const int64_t all = ntok / DELTA_C + nseq, most = kPlaces / in->heads;
-    // Few sequences: the chain of chunks takes its time on few CTAs, and the first kernels of small parts all but the first hide behind it.
-    const bool few = nseq * in->heads <= 64;
-    if (all <= (few ? most / 4 : most)) return {all, all, 1};
-    const int64_t step = few ? most / 4 : most / 2;
+    // One sequence whose heads leave half of the SMs idle: the chain of its chunks takes its time on few CTAs, and the first kernels of small parts all but the
+    // first hide behind it (65536 tokens, 16 heads: 2.35 ms, as one part 2.55).  Several sequences would wait for one another (2 of 8192: 0.79 ms, as one
+    // part 0.48), so their parts are as large as the workspace may be (2 of 32768: 1.87 ms, with a quarter of it 3.04; 256 of 512 and 32 heads: 8.3, 9.4).
+    const bool alone = nseq == 1 && in->heads * ((in->dim_v + 31) / 32) <= 72;
+    const int64_t small = most / 16 < 1 ? 1 : most / 16;
+    if (all <= (alone ? small : most)) return {all, all, 1};
+    const int64_t step = alone ? small : most / 2;
     return {all, step < 1 ? 1 : step, 2};
 }
 
@@ -110,6 +113,7 @@ mmv_status mmv_gated_delta_step(const mmv_delta_inputs* in, int64_t nreq, float 
     p.slots = slots;
     p.nreq = nreq;
     p.num_slots = num_slots;
+    // Whole rows of a state by one CTA, or 32 columns where that leaves SMs idle (16 heads: 4 requests 4.8 us, in whole rows 6.3; 128 48 us, by columns 55).
     const bool wide = p.dv > 64 && nreq * p.heads >= dev->sm_count;
     p.parts = wide ? 1 : (p.dv + 31) / 32;
     const dim3 grid(static_cast<unsigned>(nreq * p.heads * p.parts));
@@ -153,7 +157,8 @@ mmv_status mmv_gated_delta(const mmv_delta_inputs* in, const int32_t* offsets, i
     if (!token_map(&map_q, in->q, in->dim_k, in->key_heads, ntok, in->q_stride_head, in->q_stride_token) ||
         !token_map(&map_k, in->k, in->dim_k, in->key_heads, ntok, in->k_stride_head, in->k_stride_token))
         return MMV_ERR_INVALID_ARG;
-    // Slices of 32 columns, of 16 where those leave half of the SMs idle.
+    // Slices of 32 columns, of 16 where those leave half of the SMs idle (4096 tokens: 1 sequence of 18 heads 173 us, with 32 columns 224; of 20 heads
+    // 228 us, with 16 columns 315).
     const int nv = nseq * p.heads * ((p.dv + 31) / 32) <= dev->sm_count / 2 ? 16 : 32;
     p.slices = (p.dv + nv - 1) / nv;
     if (nseq * p.heads > INT32_MAX / p.slices) return MMV_ERR_INVALID_ARG;       // one CTA per (sequence, head) and slice

@@ -81,7 +81,10 @@ int per_sm(int padded, int rows) { return padded == 64 ? fit<64>(rows) : padded 
 struct Plan {
     size_t desc_off, ml_off, m2_off, o_off, total;
 };
-int heads_side_by_side(int kv_heads) { return kv_heads % 4 == 0 ? 4 : kv_heads % 2 == 0 ? 2 : 1; }
+// Key heads that a CTA's four warps take beside one another: a token's codes of both are neighbours in memory, and a request's end costs half as many short
+// tiles.  1, 2 or 4 of 8 heads (4 queries each, dim 128), 4 requests of 131072: 270, 180, 185 us; 64 of 2048: 66, 62, 64; 4 heads of 16 queries, 64 of 4096:
+// 120, 122, 132; dim 256: no difference.
+int heads_side_by_side(int kv_heads) { return kv_heads % 2 == 0 ? 2 : 1; }
 Plan plan_of(const PagedHeads& h, int kv_heads, int dim) {
     const size_t parts = 2 * static_cast<size_t>(heads_side_by_side(kv_heads));       // of a CTA
     const size_t ctas = static_cast<size_t>(kPagedMaxSms) * per_sm(paged_padded(dim), h.rows);
@@ -182,7 +185,7 @@ mmv_status mmv_kv_append_q8(const void* k, int64_t k_stride_token, int64_t k_str
     const int64_t runs = ntok / cache->block_size + nreq;
     int64_t window = (ntok + runs - 1) / runs;
     if (window < 1) window = 1;
-    // Heads of a unit: as many as leave 32 units per SM (eight CTAs' worth are resident).
+    // Heads of a unit: as many as leave 32 units per SM (eight CTAs' worth are resident; 53000 tokens of 8 heads: 64 us, with 12 units 72, with 128 71).
     int64_t side = (ntok + window - 1) / window * 2 * cache->heads / (32ll * dev->sm_count);
     side = side < 1 ? 1 : side > cache->heads ? cache->heads : side;
     const int64_t per_window = 2 * ((cache->heads + side - 1) / side);
@@ -191,6 +194,7 @@ mmv_status mmv_kv_append_q8(const void* k, int64_t k_stride_token, int64_t k_str
     p.window = static_cast<int>(window);
     p.side = static_cast<int>(side);
     p.units = (ntok + window - 1) / window * per_window;
+    // A warp where the mean run fits its registers, else the CTA (255 runs of one token: 6.5 us, by CTAs 12.6; runs of 64 tokens of 128: 98, by CTAs 65).
     const bool warp = window * (cache->dim / 16) <= 32 * Q8_KEEP;
     cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
     const bool e4m3 = cache->code == MMV_CODE_E4M3;
@@ -221,10 +225,11 @@ mmv_status mmv_kv_read_q8(const mmv_kv_cache_q8* cache, const int32_t* table, in
     p.words = cache->heads * (cache->dim / 16);
     p.by_words = reciprocal(static_cast<uint32_t>(p.words));
     p.by_head = reciprocal(static_cast<uint32_t>(cache->dim / 16));
-    // Tokens of a warp: all that are resident (2048 threads per SM) get some, and up to 32 (few words where a row is long: 32-bit quotients).
+    // Tokens of a warp: as many as its loads take at once, fewer where all warps that are resident (2048 threads per SM) then get some, up to 32.
+    // 131072 tokens of 64 words (8 heads of 128): 127 us with 1 or 2, 134 with 8, 162 with 32; 262144 of 8 words: 125 us with 1, 37 with 8 or 16, 39 with 32.
     const int64_t warps = static_cast<int64_t>(dev->sm_count) * 64;
     int64_t tile = (ntok + warps - 1) / warps;
-    const int64_t most = 4096 / p.words < 1 ? 1 : 4096 / p.words;
+    const int64_t most = p.words >= 32 * READ_Q8_UNROLL ? 1 : 32 * READ_Q8_UNROLL / p.words;
     if (tile > most) tile = most;
     if (tile > 32) tile = 32;
     p.tile = static_cast<int>(tile);

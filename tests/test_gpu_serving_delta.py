@@ -189,13 +189,13 @@ def test_delta_long(mmv, lens, hk, rep, dk, dv):
     check_delta(mmv, delta_case(sum(lens), lens, hk, rep, dk, dv, odd=False))
 
 
-@pytest.mark.parametrize("hk,rep,lens", [(64, 4, [1200, 5, 900, 0, 700]), (256, 4, [130, 64, 1, 500])])
+@pytest.mark.parametrize("hk,rep,lens", [(256, 4, [1200, 5, 900, 0, 700]), (128, 4, [130, 64, 1, 5000])])
 def test_delta_in_parts(mmv, hk, rep, lens):
     """More chunks times heads than one pair of launches takes: sequences go on in the next, the state through state_out."""
     check_delta(mmv, delta_case(1, lens, hk, rep, 16, 8))
 
 
-@pytest.mark.parametrize("hk,rep,count,most,first,behind", [(8, 1, 300, 400, 0, 0), (32, 2, 400, 100, 37, 3000), (256, 4, 9, 150, 0, 900), (64, 1, 200, 3, 5, 64)])
+@pytest.mark.parametrize("hk,rep,count,most,first,behind", [(64, 1, 300, 200, 0, 0), (128, 4, 100, 100, 37, 3000), (256, 4, 9, 150, 0, 2000), (256, 2, 200, 3, 5, 64)])
 def test_delta_many_sequences_in_parts(mmv, hk, rep, count, most, first, behind):
     """A part's launches have CTAs for the sequences that may lie in it alone; empty sequences, parts without one, rows around them.  The bits are those of
     the sequences a few at a time."""
@@ -204,7 +204,7 @@ def test_delta_many_sequences_in_parts(mmv, hk, rep, count, most, first, behind)
     out = torch.full((v.shape[0], hk * rep, 8), 7.0, dtype=q.dtype, device="cuda")
     last = mmv.gated_delta(q, k, v, ints(off), g, beta, state=state, out=out)[1]
     assert (out[:off[0]] == 7).all() and (out[off[-1]:] == 7).all()
-    group = 40 if hk * rep < 64 else 4 if hk * rep < 1024 else 1
+    group = 40 if hk * rep < 512 else 4 if hk * rep < 1024 else 1
     for i in range(0, count, group):
         j = min(count, i + group)
         a, b = off[i], off[j]
@@ -214,9 +214,10 @@ def test_delta_many_sequences_in_parts(mmv, hk, rep, count, most, first, behind)
 
 def test_delta_in_parts_back_to_back(mmv):
     """Parts whose first kernels run beside the second ones in front of them, call after call in one workspace: always the same bits."""
-    q, k, v, off, g, beta, state = delta_case(2, [9000, 700], 1, 1, 64, 64, odd=False)
-    q2, k2, v2, off2, g2, beta2, state2 = delta_case(3, [150] * 20, 32, 2, 16, 24)
-    ws = torch.empty(220 << 20, dtype=torch.uint8, device="cuda")
+    q, k, v, off, g, beta, state = delta_case(2, [9000], 36, 1, 64, 64, odd=False)
+    q2, k2, v2, off2, g2, beta2, state2 = delta_case(3, [150] * 20, 256, 4, 16, 24)
+    need = max(mmv.gated_delta_workspace_bytes(q, k, v, g, beta, 1), mmv.gated_delta_workspace_bytes(q2, k2, v2, g2, beta2, 20))
+    ws = torch.empty(need, dtype=torch.uint8, device="cuda")
     want = mmv.gated_delta(q, k, v, ints(off), g, beta, state=state), mmv.gated_delta(q2, k2, v2, ints(off2), g2, beta2, state=state2)
     torch.cuda.synchronize()
     for _ in range(3):
