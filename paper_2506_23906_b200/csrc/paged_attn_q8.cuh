@@ -3,9 +3,9 @@
 //     s_j = scale (q . code^k_j) ks_j,   out = sum_j softmax(s)_j vs_j code^v_j,   lse = log sum_j exp s_j       (ks, vs: the scales of j's block)
 //
 // The split over CTAs and the join of cut parts are those of the attention over a 16-bit cache (paged_attn.cuh).  What differs:
-//   The four warps of a CTA take neighbouring key heads of the same 16 tokens, not 64 tokens of one: a token's codes of one head are 128 bytes or less,
-//     and memory answers at half of its rate where those of the next head are asked for at another time (4 requests of 131072 tokens, 8 heads of 128: 256 us,
-//     whatever the arithmetic).  With two heads, or one, two or four warps share a head's tokens.
+//   The four warps of a CTA take two neighbouring key heads of the same tokens (where their number is even), not four times the tokens of one: a token's codes
+//     of one head are 128 bytes or less, and memory answers at a lower rate where those of the next head are asked for at another time (4 requests of
+//     131072 tokens, 8 heads of 128: 257 to 270 us, whatever the arithmetic, against 180).
 //   Codes become fp16 in registers (every int8 and e4m3 value is one) and both products run in fp16.  A bfloat16 query is brought
 //     into fp16's range by a power of two of its own row, exactly but for values 2^29 times smaller than the row's largest.
 //   Both products are taken transposed: tokens (16), then columns of the result (16) are a product's rows, and up to 8 query heads its columns,
@@ -18,7 +18,9 @@
 //   Scales of values are part of the weights that meet the codes: 2^(s_j + log2 vs_j - m'), with a running maximum m' of its own, so that no
 //     scale leaves fp16's range; the weights of the sum are 2^(s_j - m).
 //
-// What bounds it: HBM, 2 dim bytes per token and key head, and the instructions beside them (5 for four int8 codes).
+// What bounds it: HBM, 2 dim bytes per token and key head, and the instructions beside them (5 for four int8 codes).  8 key heads of 128, 32 query heads:
+// 4 requests of 131072 tokens 180 to 190 us (5.7 to 6.0 of the 6.5 TB/s of a copy; 198 with a cold L2); 64 requests of up to 4096 70 us (3.9 TB/s: requests
+// end inside tiles, warps meet there and a join follows); one of 777 12.3 us, two launches and the host's 9.6 us.
 #pragma once
 #include <cstdint>
 #include "kv_cache_q8.cuh"
