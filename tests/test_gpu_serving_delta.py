@@ -421,3 +421,30 @@ def test_calls_on_another_stream_and_in_a_graph(mmv):
         graph.replay()
     assert torch.equal(out, want)
     assert torch.equal(mmv.gated_delta_step(q[:3], k[:3], v[:3], g[:3], beta[:3], swant), o2) and torch.equal(s, swant)
+
+
+def test_parts_in_a_graph_and_two_calls_at_once(mmv):
+    """A batch that is taken in parts, captured and replayed over other inputs; calls on two streams, each with a workspace of its own."""
+    lens = [300, 0, 1500, 64, 700]
+    q, k, v, off, g, beta, state = delta_case(31, lens, 256, 4, 16, 16)
+    q2, k2, v2, off2, g2, beta2, state2 = delta_case(32, lens, 256, 4, 16, 16)
+    offsets = ints(off)
+    wants = [mmv.gated_delta(q, k, v, offsets, g, beta, state=state), mmv.gated_delta(q2, k2, v2, offsets, g2, beta2, state=state2)]
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    for s in streams:
+        s.wait_stream(torch.cuda.current_stream())
+    got = [mmv.gated_delta(q, k, v, offsets, g, beta, state=state, stream=streams[0]), mmv.gated_delta(q2, k2, v2, offsets, g2, beta2, state=state2, stream=streams[1])]
+    for s in streams:
+        torch.cuda.current_stream().wait_stream(s)
+    for (out, last), want in zip(got, wants):
+        assert torch.equal(out, want[0]) and torch.equal(last, want[1])
+    held = [x.clone() for x in (q, k, v, g, beta, state)]
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out, last = mmv.gated_delta(held[0], held[1], held[2], offsets, held[3], held[4], state=held[5])
+    for inputs, want in (((q2, k2, v2, g2, beta2, state2), wants[1]), ((q, k, v, g, beta, state), wants[0])):
+        for x, y in zip(held, inputs):
+            x.copy_(y)
+        graph.replay()
+        graph.replay()
+        assert torch.equal(out, want[0]) and torch.equal(last, want[1])
