@@ -599,8 +599,8 @@ paged_attention_q8_kernel(const __grid_constant__ CUtensorMap map_k, const __gri
                 }
                 const long long orow = done.r * static_cast<long long>(p.heads) + static_cast<long long>(head0 + hh) * p.group + part * p.rows + row;
                 if (whole) {
-                    // (every weight 0: the result is 0)
-                    const float inv = sum == 0.f ? 0.f : exp2f((t2 == -INFINITY ? 0.f : t2) - (t == -INFINITY ? 0.f : t)) / sum;
+                    // (every weight 0, or every value's scale 0: the result is 0, or NaN if x is)
+                    const float inv = sum == 0.f ? 0.f : t2 == -INFINITY ? 1.f : exp2f(t2 - (t == -INFINITY ? 0.f : t)) / sum;
                     if (c < p.dim)
                         *reinterpret_cast<uint2*>(p.out + orow * p.dim + c) =
                             make_uint2(pack_pair<BF16>(x.x * inv, x.y * inv), pack_pair<BF16>(x.z * inv, x.w * inv));
@@ -716,7 +716,7 @@ __global__ void __launch_bounds__(PA_JOIN_THREADS) paged_join_q8_kernel(const Pa
             x.w += y.w;
         }
         const long long orow = r * static_cast<long long>(p.heads) + static_cast<long long>(head) * p.group + part * p.rows + row;
-        const float inv = sum == 0.f ? 0.f : exp2f(base2 - base) / sum;
+        const float inv = sum == 0.f ? 0.f : top2 == -INFINITY ? 1.f : exp2f(base2 - base) / sum;
         *reinterpret_cast<uint2*>(p.out + orow * p.dim + c * 4) =
             make_uint2(pack_pair<BF16>(x.x * inv, x.y * inv), pack_pair<BF16>(x.z * inv, x.w * inv));
         if (c == 0 && p.lse) p.lse[orow] = sum == 0.f ? -INFINITY : (top + log2f(sum)) * 0.69314718055994531f;
