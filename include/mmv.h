@@ -535,9 +535,11 @@ mmv_status mmv_kv_read_q8(const mmv_kv_cache_q8 *cache, const int32_t *table, in
 /*
  * mmv_paged_attention over a cache in 8 bits: the same arguments, results and
  * reports, with keys and values code * scale.  dtype: q's and out's type.  Codes
- * enter the products exactly; a value's scale enters with its weight, and a
+ * enter the products exactly; a value's scale enters with its weight, through its
+ * base-2 logarithm (which is held to 2^-22 of itself, and to 2^-22), and a
  * weight with its scale is a sum of two fp16 values (2^-22 of it, no less than
- * 2^-40 of the request's and head's largest such product).  A bfloat16 query's columns below 2^-29
+ * 2^-40 of the request's and head's largest such product), whatever the scores'
+ * size.  A bfloat16 query's columns below 2^-29
  * of its head's largest one lose accuracy, and below 2^-39 count as 0.  Scales that are NaN or negative make the
  * results that read their block NaN.
  */

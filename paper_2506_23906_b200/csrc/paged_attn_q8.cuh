@@ -15,8 +15,9 @@
 //     key with one load, four of them for each of four products.  Values are read transposed in pairs of columns (8-bit
 //     columns 2d and 2d + 1 are one 16-bit element) and taken apart by a byte permutation: the even columns are a product's first 8
 //     rows, the odd ones the others.
-//   Scales of values are part of the weights that meet the codes: 2^(s_j + log2 vs_j - m'), with a running maximum m' of its own, so that no
-//     scale leaves fp16's range; the weights of the sum are 2^(s_j - m).
+//   Scales of values are part of the weights that meet the codes: 2^((s_j - m) + log2 vs_j - d), with a running maximum d of its own, so that no
+//     scale leaves fp16's range; the weights of the sum are 2^(s_j - m).  d is counted from m: a logarithm added to the score itself would lose by
+//     the score's size (of a score of 2^17 all but 7 binary places), while s_j - m is exact where the weight is large.
 //
 // What bounds it: HBM, 2 dim bytes per token and key head, and the instructions beside them (5 for four int8 codes).  8 key heads of 128, 32 query heads:
 // 4 requests of 131072 tokens 180 to 190 us (5.7 to 6.0 of the 6.5 TB/s of a copy; 198 with a cold L2); 64 requests of up to 4096 70 us (3.9 TB/s: requests
@@ -29,6 +30,7 @@
 namespace mmv {
 
 constexpr int Q8_TOKENS = 32;                                // of a warp in one tile: two groups of 16
+constexpr float Q8_FLOOR = -1024.f;                          // the least maximum of the values' weights: 2^-1024 times anything is 0
 
 struct PagedQ8Params : PagedParams {                         // (k and v of the base are not used)
     const uint8_t *k8, *v8;
@@ -38,7 +40,7 @@ struct PagedQ8Params : PagedParams {                         // (k and v of the 
     int side;                                                // key heads side by side: 1 or 2
     int tile, groups;                                        // tokens of a unit: 128 / side; groups of key heads, times parts
     uint64_t budget_ns;                                      // bound of every wait
-    float* part_m2;                                          // [grid][2][side][PA_ROWS]: maximum of the values' weights (less LIFT)
+    float* part_m2;                                          // [grid][2][side][PA_ROWS]: maximum of the values' weights, above that of the scores
 };                                                           // (part_ml: [grid][2][side][2][PA_ROWS], part_o: [grid][2][side][rows][dim])
 
 __device__ __forceinline__ PagedSpan q8_span(const PagedQ8Params& p, int r) {
@@ -141,6 +143,8 @@ __device__ __forceinline__ void q8_halves(uint32_t w, uint32_t& a, uint32_t& b) 
     }
 }
 
+__device__ __forceinline__ float q8_base(float top) { return top == -INFINITY ? 0.f : top; }
+
 // ROWS: 4, 8 or 16, the query heads of a key head (or of a part of them) at most.
 // BOX: blocks of a multiple of 16 tokens, so that a warp's 16 lie in one: they come as one box by TMA each for keys and values, and have one scale.
 template <bool BF16, bool E4M3, int DP, int ROWS, bool BOX>
@@ -149,7 +153,7 @@ paged_attention_q8_kernel(const __grid_constant__ CUtensorMap map_k, const __gri
     using C = PagedQ8Cfg<DP, ROWS>;
     constexpr int HT = ROWS == 16 ? 2 : 1;                            // products' column tiles of 8 query heads
     constexpr bool PAIRED = ROWS == 4;                                // columns 4 to 7 are the same heads, for the weights' low parts
-    constexpr float LIFT = 15.f;                                      // the exponent of the largest weight of a value (a pair of fp16 then reaches 2^-40 of it)
+    constexpr float LIFT = 32768.f;                                   // the largest weight of a value (a pair of fp16 then reaches 2^-40 of it)
     extern __shared__ __align__(1024) uint8_t lin_smem[];             // (the loads' swizzle goes by the address)
     uint8_t* smem = lin_smem;
     __shared__ uint64_t s_full[PA_WARPS][C::kStages];
@@ -157,6 +161,8 @@ paged_attention_q8_kernel(const __grid_constant__ CUtensorMap map_k, const __gri
     __shared__ int s_start[2];
     __shared__ long long s_skip;
     __shared__ float s_m[PA_WARPS][PA_ROWS], s_l[PA_WARPS][PA_ROWS], s_m2[PA_WARPS][PA_ROWS];
+    __shared__ float s_f[PA_WARPS][PA_ROWS];                          // what a warp's results are multiplied with where the warps meet
+    __shared__ float2 s_top[2][PA_ROWS];                              // there: the maxima of a head
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     griddep_launch_dependents();
     if (BOX && tid == 0) {
@@ -314,7 +320,7 @@ paged_attention_q8_kernel(const __grid_constant__ CUtensorMap map_k, const __gri
     uint32_t qf[HT][DP / 16][2];
     // of heads 2 c and 2 c + 1 of each tile:
     float qs[HT][2];                                                  // scale * log2(e), times what the head's row was divided by
-    float m[HT][2], l[HT][2], m2[HT][2];                              // maximum; sum of 2^(s - m); maximum of the values' weights less LIFT
+    float m[HT][2], l[HT][2], m2[HT][2];                              // maximum; sum of 2^(s - m); maximum of the values' weights, above m
     float o[HT][DP / 16][4];                                          // columns 16 d + 2 g (0, 1) and 16 d + 2 g + 1 (2, 3) of heads 2 c, 2 c + 1, g = lane / 4
     int seg = 0, stage = 0;
     bool begins = true, late = false;
@@ -362,7 +368,8 @@ paged_attention_q8_kernel(const __grid_constant__ CUtensorMap map_k, const __gri
 #pragma unroll
                 for (int i = 0; i < 2; ++i) {
                     qs[h][i] = p.scale_log2 * __shfl_sync(0xffffffffu, divided, (2 * (lane & 3) + i) * 4);
-                    m[h][i] = m2[h][i] = -INFINITY;
+                    m[h][i] = -INFINITY;
+                    m2[h][i] = Q8_FLOOR;
                     l[h][i] = 0.f;
                 }
 #pragma unroll
@@ -413,7 +420,7 @@ paged_attention_q8_kernel(const __grid_constant__ CUtensorMap map_k, const __gri
                 float ks[2];
                 if constexpr (BOX) {
                     ks[0] = ks[1] = lds_float(sb + y * 4);
-                    lift[y][0] = lift[y][1] = paged_log2(lds_float(sb + 8 + y * 4));
+                    lift[y][0] = paged_log2(lds_float(sb + 8 + y * 4));
                 } else {
 #pragma unroll
                     for (int i = 0; i < 2; ++i) {
@@ -434,7 +441,6 @@ paged_attention_q8_kernel(const __grid_constant__ CUtensorMap map_k, const __gri
                     for (int i = 0; i < 2; ++i) {
                         const int tok = tok0 + y * 16 + C::token((lane >> 2) + 8 * i);
                         if (tok < it.begin || tok >= it.len) {
-                            lift[y][i] = 0.f;
 #pragma unroll
                             for (int h = 0; h < HT; ++h) s[h][y][2 * i] = s[h][y][2 * i + 1] = -INFINITY;
                         }
@@ -445,33 +451,43 @@ paged_attention_q8_kernel(const __grid_constant__ CUtensorMap map_k, const __gri
                 float w[2][4], fall[2];
 #pragma unroll
                 for (int i = 0; i < 2; ++i) {                         // heads 2 c, 2 c + 1
-                    float t[2][2], top = -INFINITY, top2 = -INFINITY;
+                    float top[2];                                     // of each group of 16 tokens
+#pragma unroll
+                    for (int y = 0; y < 2; ++y) {
+                        top[y] = fmaxf(s[h][y][i], s[h][y][2 + i]);
+#pragma unroll
+                        for (int x = 4; x < 32; x <<= 1) top[y] = fmaxf(top[y], __shfl_xor_sync(0xffffffffu, top[y], x));
+                    }
+                    const float now = fmaxf(m[h][i], fmaxf(top[0], top[1]));
+                    const float base = now == -INFINITY ? 0.f : now;  // (no token yet: every weight is 2^-inf = 0)
+                    float t[2][2], top2;
 #pragma unroll
                     for (int y = 0; y < 2; ++y)
 #pragma unroll
-                        for (int j = 0; j < 2; ++j) {
-                            t[y][j] = s[h][y][2 * j + i] + lift[y][j];
-                            top = fmaxf(top, s[h][y][2 * j + i]);
-                            top2 = fmaxf(top2, t[y][j]);
-                        }
+                        for (int j = 0; j < 2; ++j) t[y][j] = s[h][y][2 * j + i] - base;
+                    if constexpr (BOX) {                              // (one scale in each group: its largest score has the largest weight)
+                        top2 = fmaxf((top[0] - base) + lift[0][0], (top[1] - base) + lift[1][0]);
+                    } else {
+                        top2 = -INFINITY;
 #pragma unroll
-                    for (int x = 4; x < 32; x <<= 1) {
-                        top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, x));
-                        top2 = fmaxf(top2, __shfl_xor_sync(0xffffffffu, top2, x));
+                        for (int y = 0; y < 2; ++y)
+#pragma unroll
+                            for (int j = 0; j < 2; ++j) top2 = fmaxf(top2, t[y][j] + lift[y][j]);
+#pragma unroll
+                        for (int x = 4; x < 32; x <<= 1) top2 = fmaxf(top2, __shfl_xor_sync(0xffffffffu, top2, x));
                     }
-                    const float now = fmaxf(m[h][i], top), now2 = fmaxf(m2[h][i], top2 - LIFT);
-                    const float base = now == -INFINITY ? 0.f : now;  // (no token yet: every weight is 2^-inf = 0)
-                    const float base2 = now2 == -INFINITY ? 0.f : now2;
-                    fall[i] = paged_exp2(m2[h][i] - base2);
-                    l[h][i] *= paged_exp2(m[h][i] - base);
+                    const float sinks = m[h][i] - base, was2 = m2[h][i] + sinks, now2 = fmaxf(fmaxf(was2, top2), Q8_FLOOR);
+                    fall[i] = paged_exp2(was2 - now2);
+                    l[h][i] *= paged_exp2(sinks);
                     m[h][i] = now;
                     m2[h][i] = now2;
 #pragma unroll
                     for (int y = 0; y < 2; ++y)
 #pragma unroll
                         for (int j = 0; j < 2; ++j) {
-                            l[h][i] += paged_exp2(s[h][y][2 * j + i] - base);
-                            w[y][2 * j + i] = paged_exp2(t[y][j] - base2);
+                            const int x = BOX ? 0 : j;
+                            l[h][i] += paged_exp2(t[y][j]);
+                            w[y][2 * j + i] = LIFT * paged_exp2(t[y][j] + (lift[y][x] - now2));
                         }
                 }
 #pragma unroll
@@ -558,6 +574,25 @@ paged_attention_q8_kernel(const __grid_constant__ CUtensorMap map_k, const __gri
                 }
             }
         __syncthreads();
+        if (tid < PA_WARPS * PA_ROWS) {
+            const int w = tid / PA_ROWS, row = tid % PA_ROWS, hh = w & (p.side - 1);
+            float a[PA_WARPS], b[PA_WARPS], t = -INFINITY, t2 = Q8_FLOOR;
+#pragma unroll
+            for (int x = 0; x < PA_WARPS; ++x) {
+                a[x] = s_m[x][row];
+                b[x] = s_m2[x][row];
+                if ((x & (p.side - 1)) == hh) t = fmaxf(t, a[x]);
+            }
+#pragma unroll
+            for (int x = 0; x < PA_WARPS; ++x)
+                if ((x & (p.side - 1)) == hh) t2 = fmaxf(t2, b[x] + (a[x] - q8_base(t)));
+            // (a warp without tokens has maximum -infinity, sum 0 and result 0, and contributes 2^-inf = 0 times that; a NaN stays one)
+            const float sinks = s_m[w][row] - q8_base(t);
+            s_f[w][row] = paged_exp2(s_m2[w][row] + sinks - t2) * (1.f / LIFT);
+            s_l[w][row] *= paged_exp2(sinks);
+            if (w < p.side) s_top[w][row] = make_float2(t, t2);
+        }
+        __syncthreads();
         const bool began_here = !(cut_front && seg == 1);
         const bool whole = began_here && ends;
         const long long slot = 2ll * blockIdx.x + (began_here ? 1 : 0);
@@ -567,11 +602,8 @@ paged_attention_q8_kernel(const __grid_constant__ CUtensorMap map_k, const __gri
 #pragma unroll
                 for (int i = 0; i < 2; ++i) {
                     const int row = 8 * h + 2 * (lane & 3) + i;
-                    float top = s_m2[mine_head][row];
-                    for (int w = mine_head + p.side; w < PA_WARPS; w += p.side) top = fmaxf(top, s_m2[w][row]);
-                    // (a warp without tokens has maximum -infinity, sum 0 and result 0, and contributes 2^-inf = 0 times that; a NaN stays one)
-                    const float f = paged_exp2(m2[h][i] - (top == -INFINITY ? 0.f : top));
                     if (row < rows) {
+                        const float f = s_f[warp][row];
 #pragma unroll
                         for (int d = 0; d < DP / 16; ++d)             // columns 16 d + 2 g, + 1
                             if (d / (DP / 32) == half)
@@ -582,15 +614,11 @@ paged_attention_q8_kernel(const __grid_constant__ CUtensorMap map_k, const __gri
             __syncthreads();
             for (int i = tid; i < p.side * rows * (DP / 8); i += PA_THREADS) {
                 const int line = i / (DP / 8), at = (i - line * (DP / 8)) * 4, c = half * (DP / 2) + at, hh = line / rows, row = line - hh * rows;
-                float t = s_m[hh][row], t2 = s_m2[hh][row];
-                for (int w = hh + p.side; w < PA_WARPS; w += p.side) {
-                    t = fmaxf(t, s_m[w][row]);
-                    t2 = fmaxf(t2, s_m2[w][row]);
-                }
+                const float t = s_top[hh][row].x, t2 = s_top[hh][row].y;
                 float sum = 0.f;
                 float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
                 for (int w = hh; w < PA_WARPS; w += p.side) {
-                    sum += s_l[w][row] * paged_exp2(s_m[w][row] - (t == -INFINITY ? 0.f : t));
+                    sum += s_l[w][row];
                     const float4 y = *reinterpret_cast<const float4*>(sm_o + (w * p.rows + row) * C::kPitch + at);
                     x.x += y.x;
                     x.y += y.y;
@@ -599,8 +627,8 @@ paged_attention_q8_kernel(const __grid_constant__ CUtensorMap map_k, const __gri
                 }
                 const long long orow = done.r * static_cast<long long>(p.heads) + static_cast<long long>(head0 + hh) * p.group + part * p.rows + row;
                 if (whole) {
-                    // (every weight 0, or every value's scale 0: the result is 0, or NaN if x is)
-                    const float inv = sum == 0.f ? 0.f : t2 == -INFINITY ? 1.f : exp2f(t2 - (t == -INFINITY ? 0.f : t)) / sum;
+                    // (every weight 0: the result is 0.  Every value's scale 0: x is, or NaN, and 2^Q8_FLOOR is)
+                    const float inv = sum == 0.f ? 0.f : exp2f(t2) / sum;
                     if (c < p.dim)
                         *reinterpret_cast<uint2*>(p.out + orow * p.dim + c) =
                             make_uint2(pack_pair<BF16>(x.x * inv, x.y * inv), pack_pair<BF16>(x.z * inv, x.w * inv));
@@ -657,26 +685,25 @@ __global__ void __launch_bounds__(PA_JOIN_THREADS) paged_join_q8_kernel(const Pa
     if (row >= min(p.rows, p.group - part * p.rows)) return;
     const int first = blockIdx.x, n = last - first + 1;
     const auto place = [&](int i) { return (2ll * (first + i) + (i == 0 ? 1 : 0)) * p.side + hh; };
-    // the maxima, then the weights' sum
-    float top = -INFINITY, top2 = -INFINITY;
-    for (int i = tid; i < n; i += PA_JOIN_THREADS) {
-        top = fmaxf(top, p.part_ml[place(i) * 2 * PA_ROWS + row]);
-        top2 = fmaxf(top2, p.part_m2[place(i) * PA_ROWS + row]);
-    }
+    // the maxima, of the scores and then of the values' weights above it, then the weights' sum
+    const auto most = [&](float x, float (&red)[4]) {
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) {
-        top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-        top2 = fmaxf(top2, __shfl_xor_sync(0xffffffffu, top2, o));
-    }
-    if (lane == 0) {
-        s_red[warp] = top;
-        s_red2[warp] = top2;
-    }
-    __syncthreads();
-    top = fmaxf(fmaxf(s_red[0], s_red[1]), fmaxf(s_red[2], s_red[3]));
-    top2 = fmaxf(fmaxf(s_red2[0], s_red2[1]), fmaxf(s_red2[2], s_red2[3]));
-    const float base = top == -INFINITY ? 0.f : top, base2 = top2 == -INFINITY ? 0.f : top2;
-    __syncthreads();
+        for (int o = 16; o > 0; o >>= 1) x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, o));
+        if (lane == 0) red[warp] = x;
+        __syncthreads();
+        return fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
+    };
+    const auto score = [&](int i) { return i < n ? p.part_ml[place(i) * 2 * PA_ROWS + row] : -INFINITY; };
+    const auto weight = [&](int i) { return i < n ? p.part_m2[place(i) * PA_ROWS + row] : -INFINITY; };
+    const float mine = score(tid), mine2 = weight(tid);               // (all there are, but for the longest contexts)
+    float top = mine;
+    for (int i = tid + PA_JOIN_THREADS; i < n; i += PA_JOIN_THREADS) top = fmaxf(top, score(i));
+    top = most(top, s_red);
+    const float base = q8_base(top);
+    float top2 = mine2 + (mine - base);
+    for (int i = tid + PA_JOIN_THREADS; i < n; i += PA_JOIN_THREADS) top2 = fmaxf(top2, weight(i) + (score(i) - base));
+    top2 = most(top2, s_red2);
+    const float base2 = q8_base(top2);
     const int cols = p.dim / 4, lanes = cols <= 32 ? 32 : 64, groups = PA_JOIN_THREADS / lanes;
     const int g = tid / lanes, c = tid - g * lanes;
     float sum = 0.f;
@@ -685,8 +712,9 @@ __global__ void __launch_bounds__(PA_JOIN_THREADS) paged_join_q8_kernel(const Pa
         const int i = i0 + tid;
         float w = 0.f;
         if (i < n) {
-            sum += paged_exp2(p.part_ml[place(i) * 2 * PA_ROWS + row] - base) * p.part_ml[(place(i) * 2 + 1) * PA_ROWS + row];
-            w = paged_exp2(p.part_m2[place(i) * PA_ROWS + row] - base2);
+            const float above = (i0 ? score(i) : mine) - base;
+            sum += paged_exp2(above) * p.part_ml[(place(i) * 2 + 1) * PA_ROWS + row];
+            w = paged_exp2((i0 ? weight(i) : mine2) + above - base2);
         }
         s_w[tid] = w;
         __syncthreads();
@@ -716,7 +744,7 @@ __global__ void __launch_bounds__(PA_JOIN_THREADS) paged_join_q8_kernel(const Pa
             x.w += y.w;
         }
         const long long orow = r * static_cast<long long>(p.heads) + static_cast<long long>(head) * p.group + part * p.rows + row;
-        const float inv = sum == 0.f ? 0.f : top2 == -INFINITY ? 1.f : exp2f(base2 - base) / sum;
+        const float inv = sum == 0.f ? 0.f : exp2f(top2) / sum;
         *reinterpret_cast<uint2*>(p.out + orow * p.dim + c * 4) =
             make_uint2(pack_pair<BF16>(x.x * inv, x.y * inv), pack_pair<BF16>(x.z * inv, x.w * inv));
         if (c == 0 && p.lse) p.lse[orow] = sum == 0.f ? -INFINITY : (top + log2f(sum)) * 0.69314718055994531f;
