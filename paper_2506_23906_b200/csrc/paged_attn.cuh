@@ -335,7 +335,9 @@ __global__ void __launch_bounds__(PA_THREADS) paged_attention_kernel(const Paged
                 float top = fmaxf(fmaxf(s[0][2 * h], s[0][2 * h + 1]), fmaxf(s[1][2 * h], s[1][2 * h + 1]));
                 top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
                 top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
-                const float now = fmaxf(m[h], top - LIFT);
+                // (From 2^23 on fp32 does not hold every such difference: rounded up there, so that no weight passes 2^15.)
+                const float low = !BF16 && fabsf(top) >= 8388608.f ? __fadd_ru(top, -LIFT) : top - LIFT;
+                const float now = fmaxf(m[h], low);
                 const float base = now == -INFINITY ? 0.f : now;      // (no token yet: every weight is 2^-inf = 0)
                 const float fall = paged_exp2(m[h] - base);
                 m[h] = now;
