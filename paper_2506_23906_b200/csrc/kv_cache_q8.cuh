@@ -7,6 +7,8 @@
 // x / scale = X / S (integers) differs from n + 1/2 = N / 2 by |2X - NS| / 2S, which is 0 or at least 2^-19 of it (2X < 2^12 or, for a
 // held code being converted, 2 code S < 2^19).  x times the rounded reciprocal times 1 + 2^-21 is off by 2^-21 +- 2^-23: every half goes
 // away from zero and nothing else changes its side.  The product is rounded once, by the fused sum that puts it in a float's low bits.
+// A block that is continued may have any scale >= 0, of another program's making: there a quotient can lie 2^-32 of itself beside a half, and is
+// rounded to odd first (q8_pack_any), which keeps it on its side.
 #pragma once
 #include <cstdint>
 #include <cuda_bf16.h>
@@ -58,6 +60,35 @@ __device__ __forceinline__ uint32_t q8_pack(float a, float b, float c, float d, 
         const uint32_t cd = __byte_perm(__float_as_uint(fmaf(c, inv, Q8_MAGIC)), __float_as_uint(fmaf(d, inv, Q8_MAGIC)), 0x0040);
         return __byte_perm(ab, cd, 0x5410);
     }
+}
+// Whether a scale is finite and > 0 but none that q8_scale_of gives, which the two functions above are for: those lie between 2^-109 and 2^122 (2^-100 / 448, the
+// largest bfloat16 / 127) and have no more places than their masks leave.
+template <bool E4M3>
+__device__ __forceinline__ bool q8_other(float scale) {
+    const uint32_t b = __float_as_uint(scale);
+    const bool own = (b & (E4M3 ? 0x7fffffu : 0x1fffu)) == 0u && b - 0x09000000u <= 0x73800000u;
+    return b - 1u < 0x7f7fffffu && !own;
+}
+// x, which has been rounded towards zero with the rest r left out, to odd: it stays on its side of every number of fewer bits
+__device__ __forceinline__ float q8_odd(float x, float r) { return r != 0.f ? __uint_as_float(__float_as_uint(x) | 1u) : x; }
+// Four codes of x * of for any scale > 0: the product to odd (values: of = 1), its quotient by the scale to odd, then to the nearest.
+template <bool E4M3>
+__device__ __forceinline__ uint32_t q8_pack_any(float4 x, float of, float scale) {
+    const float up = scale < 9.313225746154785e-10f ? 7.922816251426434e28f : 1.f;      // below 2^-30 both times 2^96, so that fp32 holds what a rounding leaves
+    of *= up;
+    scale *= up;
+    const float y[4] = {x.x, x.y, x.z, x.w};
+    uint32_t out = 0u;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const float p = __fmul_rz(y[i], of), v = q8_odd(p, fmaf(y[i], of, -p));
+        const float d = __fdiv_rz(v, scale), q = q8_odd(d, fmaf(-d, scale, v));
+        uint32_t code;
+        if constexpr (E4M3) code = __nv_cvt_float_to_fp8(q, __NV_SATFINITE, __NV_E4M3);
+        else code = static_cast<uint32_t>(static_cast<int>(copysignf(floorf(__fadd_rz(fabsf(q), 0.5f)), q))) & 0xffu;
+        out |= code << (8 * i);
+    }
+    return out;
 }
 // the numbers that four codes are (without their scale)
 template <bool E4M3>
@@ -151,18 +182,9 @@ struct AppendQ8Params {
     long long units;
 };
 
-template <bool BF16, bool E4M3, bool WARP>
-__global__ void __launch_bounds__(Q8_THREADS, 6) kv_append_q8_kernel(const AppendQ8Params p) {
-    constexpr int G = WARP ? 32 : Q8_THREADS;
-    constexpr float top = E4M3 ? 448.f : 127.f;
-    __shared__ uint32_t s_max[2][Q8_THREADS / 32];
-    const int me = threadIdx.x % G, per = p.c.dim / 16;      // elements of 16 values per row
-    const long long unit = static_cast<long long>(blockIdx.x) * (Q8_THREADS / G) + threadIdx.x / G;
-    if (unit >= p.units) return;
-    const int groups = (p.c.heads + p.side - 1) / p.side;
-    const int head0 = static_cast<int>(unit % groups) * p.side, head1 = min(p.c.heads, head0 + p.side), kv = static_cast<int>(unit / groups % 2);
-    const int t0 = static_cast<int>(unit / (2 * groups)) * p.window, t1 = min(p.ntok, t0 + p.window);       // (below 2^31: window divides it up)
-    int turn = 0;
+// The runs that begin in a unit's window: f(first row, rows, place in the block, page) for each.
+template <typename F>
+__device__ __forceinline__ void q8_runs(const AppendQ8Params& p, int t0, int t1, F&& f) {
     // the request that token t belongs to: its rows [lo, hi), and what it holds with them (one token of every request: request t)
     int r = t0 < p.nreq ? t0 : 0, lo = p.offsets[r], hi = p.offsets[r + 1], total = p.total[r];
     for (int t = t0; t < t1;) {
@@ -191,7 +213,74 @@ __global__ void __launch_bounds__(Q8_THREADS, 6) kv_append_q8_kernel(const Appen
         if (b >= p.max_blocks) continue;
         const long long page = p.table[r * p.table_stride + b];
         if (page < 0 || page >= p.c.num_blocks) continue;
+        f(first, len, place, page);
+    }
+}
 
+// The runs of a unit that go on in blocks whose scale no write has made, which the kernel leaves out.  (It comes last and out of line: inside the kernel's loop it took
+// from a twentieth to a quarter of the time that the others need.)
+template <bool BF16, bool E4M3, bool WARP>
+static __device__ __noinline__ void kv_append_q8_any(const AppendQ8Params& p, int kv, int head0, int head1, int t0, int t1, uint32_t* s_max) {
+    constexpr int G = WARP ? 32 : Q8_THREADS;
+    constexpr float top = E4M3 ? 448.f : 127.f;
+    const int me = threadIdx.x % G, per = p.c.dim / 16;
+    q8_runs(p, t0, t1, [&](int first, int len, int place, long long page) {
+        if (place == 0) return;
+        for (int head = head0; head < head1; ++head) {
+            float* scale = p.c.scale[kv] + page * p.c.s_block + head * p.c.s_head;
+            const float old = *scale;
+            if (!q8_other<E4M3>(old)) continue;
+            const uint16_t* x = p.x[kv] + first * p.x_tok[kv] + head * p.x_head[kv];
+            uint8_t* dst = p.c.code[kv] + page * p.c.block + head * p.c.head;
+            uint32_t most = 0u;
+            for (int i = me; i < len * per; i += G) {
+                const uint32_t* in = reinterpret_cast<const uint32_t*>(x + i / per * p.x_tok[kv] + i % per * 16);
+                for (int j = 0; j < 8; ++j) most = __vmaxu2(most, in[j] & 0x7fff7fffu);
+            }
+            most = __reduce_max_sync(0xffffffffu, max(most & 0xffffu, most >> 16));
+            if constexpr (WARP) {
+                __syncwarp();                                // (every lane has read the old scale)
+            } else {
+                if ((threadIdx.x & 31) == 0) s_max[threadIdx.x / 32] = most;
+                __syncthreads();
+                for (int i = 0; i < Q8_THREADS / 32; ++i) most = max(most, s_max[i]);
+                __syncthreads();
+            }
+            const bool wild = most >= (BF16 ? 0x7f80u : 0x7c00u);
+            const float amax = q8_widen<BF16>(most).x;
+            const float now = wild ? __uint_as_float(0x7fc00000u) : amax <= __fmul_rd(old, top) ? old : q8_scale_of<E4M3>(amax);
+            if (now > old)
+                for (int i = me; i < place * per; i += G) {
+                    uint32_t* word = reinterpret_cast<uint32_t*>(dst + i / per * p.c.tok + i % per * 16);
+                    for (int j = 0; j < 4; ++j) word[j] = q8_pack_any<E4M3>(q8_unpack<E4M3>(word[j]), old, now);
+                }
+            for (int i = me; i < len * per; i += G) {
+                const uint32_t* in = reinterpret_cast<const uint32_t*>(x + i / per * p.x_tok[kv] + i % per * 16);
+                uint32_t* word = reinterpret_cast<uint32_t*>(dst + (place + i / per) * p.c.tok + i % per * 16);
+                for (int j = 0; j < 4; ++j) {
+                    const float2 a = q8_widen<BF16>(in[2 * j]), b = q8_widen<BF16>(in[2 * j + 1]);
+                    word[j] = now > 0.f ? q8_pack_any<E4M3>(make_float4(a.x, a.y, b.x, b.y), 1.f, now) : 0u;
+                }
+            }
+            if (me == 0) *scale = now;
+        }
+    });
+}
+
+template <bool BF16, bool E4M3, bool WARP>
+__global__ void __launch_bounds__(Q8_THREADS, 6) kv_append_q8_kernel(const __grid_constant__ AppendQ8Params p) {
+    constexpr int G = WARP ? 32 : Q8_THREADS;
+    constexpr float top = E4M3 ? 448.f : 127.f;
+    __shared__ uint32_t s_max[2][Q8_THREADS / 32];
+    const int me = threadIdx.x % G, per = p.c.dim / 16;      // elements of 16 values per row
+    const long long unit = static_cast<long long>(blockIdx.x) * (Q8_THREADS / G) + threadIdx.x / G;
+    if (unit >= p.units) return;
+    const int groups = (p.c.heads + p.side - 1) / p.side;
+    const int head0 = static_cast<int>(unit % groups) * p.side, head1 = min(p.c.heads, head0 + p.side), kv = static_cast<int>(unit / groups % 2);
+    const int t0 = static_cast<int>(unit / (2 * groups)) * p.window, t1 = min(p.ntok, t0 + p.window);       // (below 2^31: window divides it up)
+    int turn = 0;
+    bool others = false;                                     // blocks of other scales were left out
+    q8_runs(p, t0, t1, [&](int first, int len, int place, long long page) {
         const int n = len * per;
         uint4 w[Q8_KEEP][2];
         float old;                                           // the old scale
@@ -283,8 +372,13 @@ __global__ void __launch_bounds__(Q8_THREADS, 6) kv_append_q8_kernel(const Appen
         };
         for (int head = head0; head < head1; ++head) {
             load(head);
-            process(head);
+            if (q8_other<E4M3>(old)) others = true;
+            else process(head);
         }
+    });
+    if (others) {
+        if constexpr (!WARP) __syncthreads();
+        kv_append_q8_any<BF16, E4M3, WARP>(p, kv, head0, head1, t0, t1, s_max[0]);
     }
 }
 

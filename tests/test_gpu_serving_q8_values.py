@@ -1,4 +1,5 @@
-"""The operators on a key-value cache in 8 bits at the ends of what scores and scales can be.
+"""The operators on a key-value cache in 8 bits at the ends of what scores and scales can be: value scales of zero, scores of millions, scales
+that the write did not make itself.
 """
 import numpy as np
 import pytest
@@ -6,7 +7,7 @@ import pytest
 torch = pytest.importorskip("torch")
 pytestmark = pytest.mark.gpu
 
-from test_gpu_serving_q8 import CODES, E, TINY, TYPES, U, check_paged, inside, paged_case, paged_plain  # noqa: E402
+from test_gpu_serving_q8 import CODES, E, TINY, TOP, TYPES, U, append_plain, check_paged, empty_cache, inside, ints, numbers, paged_case, paged_plain  # noqa: E402
 
 
 @pytest.fixture(scope="module")
@@ -70,3 +71,81 @@ def test_attention_with_large_scores(mmv, dtype, code, heads, kv, block, window,
     want, _, wlse, *_ = paged_plain(*case, float(np.float32(scale)), window)
     inside(out, want, (U[dtype] + 2.0 ** -20) * want.abs() + TINY[dtype])
     inside(lse, wlse, torch.nan_to_num(8 * E * wlse.abs(), posinf=0.0))
+
+
+@pytest.mark.parametrize("code", CODES)
+@pytest.mark.parametrize("block", [16, 9])
+def test_attention_negative_scales(mmv, code, block):
+    """A negative scale of keys or of values makes the results that read its block NaN, and no others; zero of either sign is 0."""
+    q, caches, scales, table, lens = paged_case(5, [300, 200, 9000], 4, 2, 64, block, torch.float16, code)
+    good, glse = mmv.paged_attention_q8(q, *caches, *scales, table, lens)
+    for which in (0, 1):
+        changed = [s.clone() for s in scales]
+        changed[which][table[1, 3], 1] *= -1
+        changed[which][table[2, 300], 0] *= -1
+        out, lse = mmv.paged_attention_q8(q, *caches, *changed, table, lens)
+        hit = torch.zeros(3, 4, dtype=torch.bool, device="cuda")
+        hit[1, 2:] = True
+        hit[2, :2] = True
+        assert torch.isnan(out[hit]).all() and torch.equal(out[~hit], good[~hit]) and torch.equal(lse[~hit], glse[~hit])
+        zero = [s.clone() for s in scales]
+        zero[which][table[0, 2], 0] = 0.0
+        zeros = [s.clone() for s in zero]
+        zeros[which][table[0, 2], 0] = -0.0
+        assert torch.equal(mmv.paged_attention_q8(q, *caches, *zero, table, lens)[0], mmv.paged_attention_q8(q, *caches, *zeros, table, lens)[0])
+
+
+# ---------------------------------------------------------------------------------------------------------------------
+# the write
+# ---------------------------------------------------------------------------------------------------------------------
+def arbitrary_scales(gen, n, low, high):
+    """fp32 scales with all of their 24 bits, of 2^low to 2^high; ones that a write makes and their neighbours among them."""
+    s = np.exp2(gen.uniform(low, high, n)).astype(np.float32)
+    s[::5] = np.exp2(np.floor(np.log2(s[::5]))).astype(np.float32)
+    s[1::5] = np.nextafter(np.exp2(np.floor(np.log2(s[1::5]))).astype(np.float32), np.float32(0))
+    s[2::10] = ((s[2::10].view(np.uint32) & 0xffffe000).view(np.float32))
+    return s
+
+
+@pytest.mark.parametrize("dtype,low,high", [(torch.float16, -12, 4), (torch.bfloat16, -12, 6), (torch.bfloat16, -148.5, -90), (torch.bfloat16, 90, 115)])
+@pytest.mark.parametrize("code", CODES)
+@pytest.mark.parametrize("count", [1, 5, 200])
+@pytest.mark.parametrize("grows", [False, True])
+def test_append_goes_on_in_blocks_of_any_scale(mmv, dtype, low, high, code, count, grows):
+    """Blocks whose scales another program made: new codes are x / scale to the nearest (quotients next to halves, and halves, among them), and codes that are
+    converted code * old / scale to the nearest."""
+    heads, dim, block, past = 6, 64, 256, 7
+    top, gen = TOP[code], np.random.default_rng(1000 + count + int(high))
+    caches, scales = empty_cache(3, block, heads, dim, code)
+    page = 1
+    new = []
+    for s in scales:
+        mine = arbitrary_scales(gen, heads, low, high)
+        s[page] = torch.from_numpy(mine).cuda()
+        steps = gen.integers(0, int(top), (count, heads, dim)) + gen.choice([0.5, 0.0, 0.25, 0.4999, 0.5001, 0.0625], (count, heads, dim))
+        if code != torch.int8:                                         # between two neighbours of e4m3: 2^e (8 + i + 1/2) / 8
+            steps = np.exp2(gen.integers(-9, 9, steps.shape)) * (8 + gen.integers(0, 8, steps.shape) + gen.choice([0.5, 0.499, 0.501, 0.0], steps.shape)) / 8
+        x = np.minimum(steps, top) * gen.choice([-1.0, 1.0], steps.shape) * mine.astype(np.float64)[None, :, None]
+        if grows:
+            x[-1, ::2, 3] = mine.astype(np.float64)[::2] * top * 3.7
+        x = torch.from_numpy(x).to(dtype)
+        if not grows:                                                  # (what a rounding brought above the largest value that fits)
+            x = torch.where(x.double().abs() <= torch.from_numpy(mine.astype(np.float64) * top)[None, :, None], x, 0.0)
+        new.append(x.cuda())
+    want = [(numbers(c), s.double().cpu().numpy()) for c, s in zip(caches, scales)]
+    table = [[page]]
+    mmv.kv_append_q8(*new, ints([0, count]), ints([past + count]), ints(table), *caches, *scales)
+    for (codes, scale), x, c, s in zip(want, new, caches, scales):
+        append_plain(codes, scale, x.double().cpu().numpy(), [0, count], [past + count], table, block, top)
+        assert np.array_equal(s.double().cpu().numpy(), scale)
+        assert np.array_equal(numbers(c), codes)
+
+
+def test_append_one_quotient_below_a_half(mmv):
+    """0.174560546875 / 0.049874447 = 3.49999963: 3."""
+    caches, scales = empty_cache(1, 16, 1, 16, torch.int8)
+    x = torch.full((1, 1, 16), 0.174560546875, dtype=torch.float16, device="cuda")
+    for s in scales:
+        s[:] = 0.049874447
+    mmv.kv_append_q8(x, -x, ints([0, 1]), ints([2]), ints([[0]]), *caches, *scales)
+    assert (caches[0][0, 1] == 3).all() and (caches[1][0, 1] == -3).all()
