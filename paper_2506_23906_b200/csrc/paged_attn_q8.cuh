@@ -121,6 +121,8 @@ __device__ __forceinline__ float paged_log2(float x) {
     asm("lg2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
     return r;
 }
+// (a negative scale is none: NaN, as its logarithm is where it is one of values)
+__device__ __forceinline__ float q8_key_scale(float x) { return x < 0.f ? __uint_as_float(0x7fc00000u) : x; }
 // an 8 x 8 matrix of 16-bit values, as a product leaves its results, transposed
 __device__ __forceinline__ uint32_t matrix_transpose(uint32_t x) {
     uint32_t r;
@@ -419,13 +421,13 @@ paged_attention_q8_kernel(const __grid_constant__ CUtensorMap map_k, const __gri
                 }
                 float ks[2];
                 if constexpr (BOX) {
-                    ks[0] = ks[1] = lds_float(sb + y * 4);
+                    ks[0] = ks[1] = q8_key_scale(lds_float(sb + y * 4));
                     lift[y][0] = paged_log2(lds_float(sb + 8 + y * 4));
                 } else {
 #pragma unroll
                     for (int i = 0; i < 2; ++i) {
                         const uint32_t at = sb + (y * 16 + C::token((lane >> 2) + 8 * i)) * 4;
-                        ks[i] = lds_float(at);
+                        ks[i] = q8_key_scale(lds_float(at));
                         lift[y][i] = paged_log2(lds_float(at + Q8_TOKENS * 4));
                     }
                 }
