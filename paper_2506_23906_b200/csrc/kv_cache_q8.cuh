@@ -277,7 +277,7 @@ __global__ void __launch_bounds__(Q8_THREADS, 6) kv_append_q8_kernel(const __gri
     if (unit >= p.units) return;
     const int groups = (p.c.heads + p.side - 1) / p.side;
     const int head0 = static_cast<int>(unit % groups) * p.side, head1 = min(p.c.heads, head0 + p.side), kv = static_cast<int>(unit / groups % 2);
-    const int t0 = static_cast<int>(unit / (2 * groups)) * p.window, t1 = min(p.ntok, t0 + p.window);       // (below 2^31: window divides it up)
+    const int t0 = static_cast<int>(unit / (2 * groups)) * p.window, t1 = t0 + min(p.window, p.ntok - t0);  // (t0 + window may pass 2^31)
     int turn = 0;
     bool others = false;                                     // blocks of other scales were left out
     q8_runs(p, t0, t1, [&](int first, int len, int place, long long page) {

@@ -1,5 +1,5 @@
 """The operators on a key-value cache in 8 bits at the ends of what scores and scales can be: value scales of zero, scores of millions, scales
-that the write did not make itself.
+that the write did not make itself, lengths at the end of 32 bits.
 """
 import numpy as np
 import pytest
@@ -149,3 +149,17 @@ def test_append_one_quotient_below_a_half(mmv):
         s[:] = 0.049874447
     mmv.kv_append_q8(x, -x, ints([0, 1]), ints([2]), ints([[0]]), *caches, *scales)
     assert (caches[0][0, 1] == 3).all() and (caches[1][0, 1] == -3).all()
+
+
+@pytest.mark.parametrize("block", [8, 1 << 16])
+def test_append_at_the_end_of_32_bits(mmv, block):
+    """The last tokens of 2^31 - 1 (one row, seen through a stride of zero)."""
+    heads, dim, n = 1, 16, 2 ** 31 - 1
+    x = torch.randn(1, heads, dim, device="cuda").half()
+    k = x.expand(n, heads, dim)
+    caches, scales = empty_cache(2, block, heads, dim, torch.int8)
+    want = [c.clone() for c in caches], [s.clone() for s in scales]
+    mmv.kv_append_q8(x.expand(3, heads, dim), x.expand(3, heads, dim), ints([0, 3]), ints([3]), ints([[1]]), *want[0], *want[1])
+    mmv.kv_append_q8(k, k, ints([n - 3, n]), ints([3]), ints([[1]]), *caches, *scales)
+    for a, b in zip((*caches, *scales), (*want[0], *want[1])):
+        assert torch.equal(a, b)
