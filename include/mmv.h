@@ -659,7 +659,11 @@ mmv_status mmv_gated_delta(const mmv_delta_inputs *in, const int32_t *offsets, i
  * Test hook.  wait_budget_ns: time after which a device-side wait gives up
  * (<= 0 restores the default of 4 s).  skip_publish_span: index of one
  * 4096-element span of the scan that never publishes its carry, so that its
- * successors exercise the time-out path without any GPU fault (-1 = off).
+ * successors exercise the time-out path without any GPU fault (-1 = off).  The
+ * operators that wait for bulk loads take it as a block's index: in
+ * mmv_paged_attention_q8 that block leaves out a load of each of its tiles, in
+ * mmv_gated_delta the first kernel's block its loads (from 2^32 on: the second
+ * kernel's block, that index less 2^32).
  * Applies to calls made after it returns.
  */
 void mmv_debug_configure(int64_t wait_budget_ns, int64_t skip_publish_span);

@@ -23,6 +23,7 @@ namespace mmv {
 // (declared in host_state.h: the serving operators count their launches and bound their waits with the same words)
 std::atomic<long long> g_launches{0};
 std::atomic<unsigned long long> g_budget_ns{WAIT_BUDGET_NS};
+std::atomic<long long> g_debug_skip_span{-1};
 
 static EncodeTiledFn g_encode = nullptr;
 static std::once_flag g_encode_once;
@@ -40,7 +41,6 @@ EncodeTiledFn get_encode() {
 
 namespace {
 
-std::atomic<long long> g_debug_skip_span{-1};
 std::atomic<int> g_force_groups{0};
 std::atomic<int> g_force_scan_shape{-1};      // test hook: -1 = the library chooses
 

@@ -24,7 +24,7 @@ struct DeltaParams {
     float* state_out;
     // single tokens
     const int32_t* slots;                                    // request -> state; null: its own index
-    long long nreq, num_slots;
+    long long num_slots;
     int parts;                                               // column parts of a state
     // packed prompts
     const int32_t* offsets;
@@ -35,6 +35,7 @@ struct DeltaParams {
     WorkspaceHeader* hdr;
     uint8_t* chunks;                                         // [last_slot - first_slot][heads] DeltaChunk
     uint64_t budget_ns;                                      // bound of every wait
+    long long debug_skip;                                    // test hook: the first kernel's CTA that leaves its loads out, from 2^32 on the second one's (-1: none)
 };
 
 // ---------------------------------------------------------------------------------------------------------------------
@@ -292,11 +293,13 @@ __device__ __forceinline__ void delta_prep(const CUtensorMap& map_q, const CUten
     if (tid == 0) {
         mbar_init(&s_full, 1);
         mbar_fence_init();
-        mbar_arrive_expect_tx(&s_full, 2 * C::kTile);
+        if (blockIdx.x != p.debug_skip) {
+            mbar_arrive_expect_tx(&s_full, 2 * C::kTile);
 #pragma unroll
-        for (int b = 0; b < DK / 64; ++b) {
-            tma_load_3d(smem + b * DELTA_BOX, &map_k, &s_full, b * 64, hk, first);
-            tma_load_3d(smem + C::kTile + b * DELTA_BOX, &map_q, &s_full, b * 64, hk, first);
+            for (int b = 0; b < DK / 64; ++b) {
+                tma_load_3d(smem + b * DELTA_BOX, &map_k, &s_full, b * 64, hk, first);
+                tma_load_3d(smem + C::kTile + b * DELTA_BOX, &map_q, &s_full, b * 64, hk, first);
+            }
         }
     }
     // decays and betas of a value head (warp 7), on their way while the tiles land
@@ -706,7 +709,7 @@ delta_chunks_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_cons
         tma_load_1d(dst + C::kX, &from->x, sizeof(DeltaScalars), &s_full[i]);
         tma_load_1d(dst + C::kT, from->t, 2 * C::kBlocks, &s_full[i]);
     };
-    if (begin < end && tid == 0) fetch(begin);
+    if (begin < end && tid == 0 && blockIdx.x + (1ll << 32) != p.debug_skip) fetch(begin);
 
     // Of the tokens a warp has 16 (two warps of a scheduler together five of the triangles' blocks), of the state 16 M rows; of both, half of the
     // slice's columns.

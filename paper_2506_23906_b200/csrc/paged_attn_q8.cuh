@@ -40,6 +40,7 @@ struct PagedQ8Params : PagedParams {                         // (k and v of the 
     int side;                                                // key heads side by side: 1 or 2
     int tile, groups;                                        // tokens of a unit: 128 / side; groups of key heads, times parts
     uint64_t budget_ns;                                      // bound of every wait
+    long long debug_skip;                                    // test hook: the CTA that leaves out a load of each tile (-1: none)
     float* part_m2;                                          // [grid][2][side][PA_ROWS]: maximum of the values' weights, above that of the scores
 };                                                           // (part_ml: [grid][2][side][2][PA_ROWS], part_o: [grid][2][side][rows][dim])
 
@@ -96,6 +97,11 @@ static __device__ __noinline__ bool q8_wait(uint64_t* bar, uint32_t parity, uint
     while (!mbar_try_wait_for(bar, parity, 20000u))
         if (global_timer_ns() - t0 > budget_ns) return false;
     return true;
+}
+// The loads of a stage, and of the one behind it if there are any, land before the warp gives up (1 ms each at most).
+static __device__ __noinline__ void q8_land(uint64_t* bars, int stage, uint32_t turn, bool more) {
+    q8_wait(&bars[stage], turn, 1000000u);
+    if (more) q8_wait(&bars[stage ^ 1], stage ? turn ^ 1 : turn, 1000000u);
 }
 __device__ __forceinline__ void cp_async_4_or_zero(uint32_t dst, const void* src, bool on) {
     const int bytes = on ? 4 : 0;
@@ -268,7 +274,7 @@ paged_attention_q8_kernel(const __grid_constant__ CUtensorMap map_k, const __gri
                 const bool there = ld.first + ld.tile * p.tile + mine_tok + (lane & 1) * 16 < ld.len, on = there && page_ld >= 0 && page_ld < p.num_blocks;
                 if (there && !on) desc[2] = 1;                        // (every writer stores the same value)
                 cp_async_4_or_zero(scales + lane * 4, on ? static_cast<const void*>((lane & 2 ? p.vs : p.ks) + page_ld * p.s_block + head_ld * p.s_head) : p.q, on);
-                if (lane < 2) {
+                if (lane < 2 && !(lane == 0 && blockIdx.x == p.debug_skip)) {
                     uint64_t* bar = &s_full[warp][stage];
                     if (on) {
                         mbar_arrive_expect_tx(bar, 2 * C::kGroup);
@@ -380,13 +386,20 @@ paged_attention_q8_kernel(const __grid_constant__ CUtensorMap map_k, const __gri
             ++seg;
         }
         cp_async_wait<C::kStages - 1>();
-        if (BOX && u >= u0) {
-            if (!mbar_try_wait_for(&s_full[warp][stage], turn, 20000u)) late |= !q8_wait(&s_full[warp][stage], turn, p.budget_ns);
+        if (BOX && u >= u0 && !late) {
+            const bool there = mbar_try_wait_for(&s_full[warp][stage], turn, 20000u) || q8_wait(&s_full[warp][stage], turn, p.budget_ns);
+            if (__any_sync(0xffffffffu, !there)) {
+                // This warp's part ends: it fetches and works on nothing more, and comes along to where the warps meet.  The loads on their way (this tile's and the next
+                // one's) land before the CTA leaves.
+                late = true;
+                q8_land(s_full[warp], stage, turn, u + 1 < u1);
+                u_ld = u1;
+            }
             if (stage + 1 == C::kStages) turn ^= 1;
         }
         __syncwarp();
         const int tok0 = it.first + it.tile * p.tile + mine_tok;
-        if (u >= u0 && tok0 < it.len) {
+        if (u >= u0 && tok0 < it.len && !late) {
             const uint32_t sb = sm_scale + stage * C::kScales;
             const bool edge = tok0 < it.begin || tok0 + Q8_TOKENS > it.len;
             if (BOX && E4M3 && edge) {                                // codes of no token of this request: a weight of zero does not hide a NaN

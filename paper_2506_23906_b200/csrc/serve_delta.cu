@@ -111,7 +111,6 @@ mmv_status mmv_gated_delta_step(const mmv_delta_inputs* in, int64_t nreq, float 
     p.state = state;
     p.state_out = state_out;
     p.slots = slots;
-    p.nreq = nreq;
     p.num_slots = num_slots;
     // Whole rows of a state by one CTA, or 32 columns where that leaves SMs idle (16 heads: 4 requests 4.8 us, in whole rows 6.3; 128 48 us, by columns 55).
     const bool wide = p.dv > 64 && nreq * p.heads >= dev->sm_count;
@@ -153,6 +152,7 @@ mmv_status mmv_gated_delta(const mmv_delta_inputs* in, const int32_t* offsets, i
     p.ntok = static_cast<int>(ntok);
     p.hdr = static_cast<WorkspaceHeader*>(workspace);
     p.budget_ns = g_budget_ns.load();
+    p.debug_skip = g_debug_skip_span.load();
     CUtensorMap map_q, map_k;
     if (!token_map(&map_q, in->q, in->dim_k, in->key_heads, ntok, in->q_stride_head, in->q_stride_token) ||
         !token_map(&map_k, in->k, in->dim_k, in->key_heads, ntok, in->k_stride_head, in->k_stride_token))

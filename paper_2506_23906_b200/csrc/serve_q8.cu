@@ -307,6 +307,7 @@ mmv_status mmv_paged_attention_q8(const void* q, int64_t q_stride_request, int64
     p.part_o = reinterpret_cast<float*>(ws + plan.o_off);
     const int padded = paged_padded(p.dim);
     p.budget_ns = g_budget_ns.load();
+    p.debug_skip = g_debug_skip_span.load();
     p.by_block = 0;
     CodeMaps maps{};
     maps.box = cache->num_blocks > 0 && cache->block_size % 16 == 0 && code_map(&maps.k, cache->k, cache, padded) && code_map(&maps.v, cache->v, cache, padded);
