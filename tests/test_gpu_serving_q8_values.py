@@ -73,6 +73,28 @@ def test_attention_with_large_scores(mmv, dtype, code, heads, kv, block, window,
     inside(lse, wlse, torch.nan_to_num(8 * E * wlse.abs(), posinf=0.0))
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("code", CODES)
+@pytest.mark.parametrize("dim", [16, 48, 80, 112, 144, 208, 240])
+@pytest.mark.parametrize("block,window", [(16, 0), (48, 70), (80, 0)])
+def test_attention_odd_dims_and_unused_places(mmv, dtype, code, dim, block, window):
+    """Dims between the sizes of a load, in blocks that loads take whole; places behind a request's end and in front of its window hold what is no number (e4m3),
+    as do the columns behind dim."""
+    lens = [1, 17, 300, 0, 95, 1000]
+    q, caches, scales, table, lens = paged_case(dim + block, lens, 6, 2, dim, block, dtype, code, pad=16)
+    worst = 0x7f if code == torch.float8_e4m3fn else 0x80
+    for c in caches:
+        whole = c.view(torch.uint8)
+        keep = torch.zeros(whole.shape[:2], dtype=torch.bool, device="cuda")
+        for r, n in enumerate(lens.tolist()):
+            j = torch.arange(max(0, n - window) if window else 0, n, device="cuda")
+            keep[table[r, j // block].long(), j % block] = True
+        whole[~keep] = worst
+        wide = whole.as_strided((*whole.shape[:3], dim + 16), whole.stride())
+        wide[..., dim:] = worst
+    check_paged(mmv, (q, caches, scales, table, lens), dtype, dim ** -0.5, window)
+
+
 @pytest.mark.parametrize("code", CODES)
 @pytest.mark.parametrize("block", [16, 9])
 def test_attention_negative_scales(mmv, code, block):
