@@ -504,14 +504,14 @@ typedef struct {
  *                         become code * old / scale, rounded like new ones
  *     new codes           x / scale; int8: to the nearest whole number, halves away
  *                         from zero; e4m3: to the nearest, halves to even
- * so that everything but a converted code is rounded once.  Magnitudes below 2^-100 count as 0
- * (scale 0, codes 0).  A new value that is not finite, or an old scale that is
- * not >= 0 and finite, makes the scale of its block and head (of the keys or of the
- * values) NaN: they read as NaN until the block is begun anew.  Results are
- * deterministic.  k, v: ntok rows of heads x dim, fp16 or bfloat16 (dtype), token
- * and head strides of their own; they must not overlap the cache.  Rows behind
- * offsets[nreq] (a padded batch) are ignored, and so are tokens without a
- * place: a table entry outside [0, num_blocks), a block past max_blocks, a total
+ * so that everything but a converted code is rounded once, whatever old is.  A new
+ * scale of magnitudes below 2^-100 is 0 (codes 0).  A new value that is not
+ * finite, or an old scale that is not >= 0 and finite, makes the scale of its block
+ * and head (of the keys or of the values) NaN: they read as NaN until the block is
+ * begun anew.  Results are deterministic.  k, v: ntok rows of heads x dim, fp16 or
+ * bfloat16 (dtype), token and head strides of their own; they must not overlap the
+ * cache.  Rows behind offsets[nreq] (a padded batch) are ignored, and so are tokens
+ * without a place: a table entry outside [0, num_blocks), a block past max_blocks, a total
  * smaller than what is added, offsets that leave [0, ntok].  The last block of a request must
  * not be another's too.  ntok < 2^31, nreq < 2^20.  No workspace.
  */
@@ -524,9 +524,9 @@ mmv_status mmv_kv_append_q8(const void *k, int64_t k_stride_token, int64_t k_str
  * Reads the first tokens of every request back in 16 bits, packed: row
  * offsets[r] + p of k_out and v_out (ntok x heads x dim, contiguous, fp16 or
  * bfloat16) is request r's token p, for p < offsets[r + 1] - offsets[r]: code *
- * scale, rounded once.  Rows in front of offsets[0] and behind offsets[nreq] are
- * not written; a token without a page (see above) reads as zero.
- * ntok < 2^31, nreq < 2^20.  No workspace.
+ * scale in fp32 (exact for scales that the write made), rounded to 16 bits.  Rows
+ * in front of offsets[0] and behind offsets[nreq] are not written; a token without
+ * a page (see above) reads as zero.  ntok < 2^31, nreq < 2^20.  No workspace.
  */
 mmv_status mmv_kv_read_q8(const mmv_kv_cache_q8 *cache, const int32_t *table, int64_t table_stride, int64_t max_blocks,
                           const int32_t *offsets, int64_t nreq, int64_t ntok, mmv_dtype dtype, void *k_out, void *v_out,
@@ -534,13 +534,15 @@ mmv_status mmv_kv_read_q8(const mmv_kv_cache_q8 *cache, const int32_t *table, in
 
 /*
  * mmv_paged_attention over a cache in 8 bits: the same arguments, results and
- * reports, with keys and values code * scale.  dtype: q's and out's type.  Codes
- * enter the products exactly; a value's scale enters with its weight, through its
- * base-2 logarithm (which is held to 2^-22 of itself, and to 2^-22), and a
- * weight with its scale is a sum of two fp16 values (2^-22 of it, no less than
- * 2^-40 of the request's and head's largest such product), whatever the scores'
- * size.  A bfloat16 query's columns below 2^-29
- * of its head's largest one lose accuracy, and below 2^-39 count as 0.  Scales that are NaN or negative make the
+ * reports, with keys and values code * scale, except that the other places of a
+ * block that holds a stated token may be read too (what they hold reaches no
+ * result) and that a load which does not come in time is recorded as
+ * MMV_ERR_TIMEOUT.  dtype: q's and out's type.  Codes enter the products exactly.
+ * A value's scale enters with its weight, by its base-2 logarithm (held to 2^-22
+ * of itself, or to 2^-22), and a weight with its scale is a sum of two fp16 values
+ * (2^-22 of it, no less than 2^-40 of the request's and head's largest such
+ * product).  A bfloat16 query's columns below 2^-29 of its head's largest one lose
+ * accuracy, and below 2^-39 count as 0.  Scales that are NaN or negative make the
  * results that read their block NaN.
  */
 size_t mmv_paged_attention_q8_workspace_bytes(int32_t heads, const mmv_kv_cache_q8 *cache);

@@ -161,10 +161,14 @@ __global__ void __launch_bounds__(LIN_STEP_THREADS) delta_step_kernel(const Delt
 // state or to R is summed up by itself, since the tensor core cuts a sum's last digits.  With two parts everywhere, T R as one product and the sums
 // begun at S and R the state was off by 4.0e-6 of itself; it is by 0.9e-6 (fp32 throughout: 0.16e-6).
 //
-// What bounds it: the chain of chunks.  A chunk's three products follow one another through shared memory, eight warps share them and nothing else can run: 2.3 us
-// with slices of 16 columns (one prompt of 65536 tokens and 16 heads: 2.34 ms, 128 CTAs), 3.7 us with 32 (16 prompts of 32768 tokens in all: 0.84 ms, the tensor
-// pipe 47 % busy).  tcgen05.mma takes about 44 clocks and half a clock per column of such a slice for 16 rows of a product, as many as the warps' own
-// instructions take for it, and its results come back through tensor memory: nothing is gained where a slice is this narrow, and wider ones leave SMs idle.
+// What bounds it: latencies inside a chunk.  Its three products follow one another through shared memory, eight warps wait for one another three times, and an SM has
+// room for nothing else meanwhile (166 KB of shared memory): 2.2 us with slices of 16 columns, 3.1 us with 32.
+//   One prompt of 65536 tokens and 16 heads is a chain: 1024 chunks on 128 CTAs of 16 columns, 2.33 ms (the first kernels of later parts run beside it).
+//   16 prompts of 32768 tokens in all and 16 heads are a queue: 1024 CTAs of 32 columns, about 228 chunks per SM one after the other, 0.70 ms (tensor pipe 46 %
+//     busy) behind 0.14 ms of the first kernel, which ends before the second begins: 0.84 ms.
+// tcgen05.mma takes about 44 clocks and half a clock per column of a slice for 16 rows of a product, as many as the warps' own instructions take for it, and its
+// results come back through tensor memory: at these widths nothing is gained.  Whole states per CTA, whose products have its 64 and 128 rows, would fill the SMs
+// from 148 (sequence, head) pairs on, and composing chunks (S -> M S + N) would shorten the chain of a few long prompts; neither has been built.
 //
 // A chunk that holds a value that is not finite (or whose products are not) is taken token by token: zeros of the triangles would carry it to
 // tokens in front of it.
@@ -238,6 +242,7 @@ __device__ __forceinline__ uint32_t delta_word(int row, int c) { return (c >> 3)
 // diagonal blocks by substitution in fp32, warps 4 to 7 the blocks under it and those of Q K^T.  Then warp J goes down T's block column J, transposed:
 //     T_IJ^T = -(sum_K T_KJ^T L_IK^T) T_II^T,  K = J .. I - 1
 // where the results of one product are the first operand of the next as they lie in registers (all operands of three parts).
+// 512 chunks of 8 key heads of 128, two value heads to each: 143 us; bound by its warps' waits for one another from step to step (DRAM 20 %, tensor pipe 17 % busy).
 // ---------------------------------------------------------------------------------------------------------------------
 constexpr int DELTA_PREP_THREADS = 256;
 constexpr int DELTA_DIAG = 20;                               // floats of a row of a block on the diagonal
@@ -590,7 +595,7 @@ delta_prep_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_consta
 // ---------------------------------------------------------------------------------------------------------------------
 // The walk along the chunks.  Eight warps share a chunk's products and meet three times a chunk: when the state's copy, R and U are in shared
 // memory.  All of the next chunk's operands are on their way meanwhile (one CTA per SM; with Q, T and A loaded into the places that the chunk had
-// done with, two fit an SM: 750 instead of 860 us for 16 prompts of nearly one length, 1030 where one is three times as long as their mean, since
+// done with, two fit an SM: 750 instead of 840 us for 16 prompts of nearly one length, 1030 where one is three times as long as their mean, since
 // a chunk then takes 5.3 instead of 3.1 us).
 // ---------------------------------------------------------------------------------------------------------------------
 constexpr int DELTA_THREADS = 256;

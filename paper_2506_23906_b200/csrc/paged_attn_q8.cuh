@@ -20,8 +20,9 @@
 //     the score's size (of a score of 2^17 all but 7 binary places), while s_j - m is exact where the weight is large.
 //
 // What bounds it: HBM, 2 dim bytes per token and key head, and the instructions beside them (5 for four int8 codes).  8 key heads of 128, 32 query heads:
-// 4 requests of 131072 tokens 180 to 190 us (5.7 to 6.0 of the 6.5 TB/s of a copy; 198 with a cold L2); 64 requests of up to 4096 70 us (3.9 TB/s: requests
-// end inside tiles, warps meet there and a join follows); one of 777 12.3 us, two launches and the host's 9.6 us.
+// 4 requests of 131072 tokens 188 us with e4m3 codes (5.7 of the 6.5 TB/s of a copy; with a cold L2 198 to 206, int8 198 to 202); 64 requests of up to 4096 70 us
+// (3.9 TB/s: requests end inside tiles, warps meet there and a join follows); one of 777 12.3 us, two launches and the host's 9.6 us.  Blocks that are no
+// multiple of 16 tokens (copies and scales token by token): 4 of 131072 with blocks of 24, 9, 8 204, 206, 213 us; 64 of 2048 72 us with blocks of 9, 71 with 16.
 #pragma once
 #include <cstdint>
 #include "kv_cache_q8.cuh"

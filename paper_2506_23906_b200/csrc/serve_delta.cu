@@ -70,7 +70,7 @@ constexpr int64_t kMostTokens = INT32_MAX - DELTA_C;         // (positions past 
 DeltaParts parts_of(const mmv_delta_inputs* in, int64_t nseq, int64_t ntok) {
     const int64_t all = ntok / DELTA_C + nseq, most = kPlaces / in->heads;
     // One sequence whose heads leave half of the SMs idle: the chain of its chunks takes its time on few CTAs, and the first kernels of small parts all but the
-    // first hide behind it (65536 tokens, 16 heads: 2.35 ms, as one part 2.55).  Several sequences would wait for one another (2 of 8192: 0.79 ms, as one
+    // first hide behind it (65536 tokens, 16 heads: 2.33 ms, as one part 2.55).  Several sequences would wait for one another (2 of 8192: 0.79 ms, as one
     // part 0.48), so their parts are as large as the workspace may be (2 of 32768: 1.87 ms, with a quarter of it 3.04; 256 of 512 and 32 heads: 8.3, 9.4).
     const bool alone = nseq == 1 && in->heads * ((in->dim_v + 31) / 32) <= 72;
     const int64_t small = most / 16 < 1 ? 1 : most / 16;
@@ -158,7 +158,8 @@ mmv_status mmv_gated_delta(const mmv_delta_inputs* in, const int32_t* offsets, i
         !token_map(&map_k, in->k, in->dim_k, in->key_heads, ntok, in->k_stride_head, in->k_stride_token))
         return MMV_ERR_INVALID_ARG;
     // Slices of 32 columns, of 16 where those leave half of the SMs idle (4096 tokens: 1 sequence of 18 heads 173 us, with 32 columns 224; of 20 heads
-    // 228 us, with 16 columns 315).
+    // 228 us, with 16 columns 315).  This rule and parts_of's count sequences: how long each is only the device knows.  One long prompt beside short ones, or beside
+    // empty entries of a padded batch, is taken as several are (16 heads: 32768 tokens 1.19 ms, beside 1 or 15 others of a token or none 1.71).
     const int nv = nseq * p.heads * ((p.dv + 31) / 32) <= dev->sm_count / 2 ? 16 : 32;
     p.slices = (p.dv + nv - 1) / nv;
     if (nseq * p.heads > INT32_MAX / p.slices) return MMV_ERR_INVALID_ARG;       // one CTA per (sequence, head) and slice

@@ -83,7 +83,8 @@ struct Plan {
 };
 // Key heads that a CTA's four warps take beside one another: a token's codes of both are neighbours in memory, and a request's end costs half as many short
 // tiles.  1, 2 or 4 of 8 heads (4 queries each, dim 128), 4 requests of 131072: 270, 180, 185 us; 64 of 2048: 66, 62, 64; 4 heads of 16 queries, 64 of 4096:
-// 120, 122, 132; dim 256: no difference.
+// 120, 122, 132; dim 256: no difference.  An odd number takes one: 4 of 131072 with 7, 6, 5, 4, 3 heads 237, 158, 179, 118, 97 us, 64 of 4096 with 8, 7, 5, 4, 3 heads
+// 119, 105, 106, 70, 67.
 int heads_side_by_side(int kv_heads) { return kv_heads % 2 == 0 ? 2 : 1; }
 Plan plan_of(const PagedHeads& h, int kv_heads, int dim) {
     const size_t parts = 2 * static_cast<size_t>(heads_side_by_side(kv_heads));       // of a CTA
